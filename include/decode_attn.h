@@ -54,6 +54,11 @@ extern "C" {
 /* Chunk-state bytes the scratch of da_decode_attn_noalloc holds (per device,
  * for the life of the process, with DA_ARRIVAL_BYTES of counters after it). */
 #define DA_NOALLOC_STATE_BYTES (32 << 20)
+/* Bytes of one tile of the 4-bit cache: 32 keys of one KV head (see
+ * da_append_kv4). */
+#define DA_KV4_TILE_BYTES 4352
+/* Requests one da_extend_tables call takes. */
+#define DA_MAX_REQUESTS 4096
 
 typedef enum da_status {
   DA_OK = 0,
@@ -467,6 +472,150 @@ size_t da_dealt_workspace_bytes(int B, int H_Q, int H_KV, int num_cus);
  * L_K_max, or keys <= 0, the answer says nothing about the batch.  num_cus as
  * above.  Host only. */
 int da_prefers_dealt(int B, int H_Q, int H_KV, int L_K_max, int64_t keys, int num_cus);
+
+/* Decode attention with a sliding window and sinks: the last `window` keys of
+ * each sequence (the query's own key among them) and its first `sinks` keys are
+ * visible, key j of L where j < sinks or j >= L - window; the softmax of
+ * da_decode_attn over those.  Invisible keys do not reach the result, whatever
+ * they hold, and apart from rows that share a 32-key tile's descriptor nothing
+ * of them is read.
+ *   block_table == NULL: k, v fixed (cu_seqlens_k NULL) or packed, as for
+ *     da_decode_attn (page_size, max_pages, num_pages, seq_lens ignored);
+ *     otherwise paged as for da_decode_attn_paged (cu_seqlens_k ignored).
+ *     Table entries of pages that hold no visible key may be stale.
+ *   window     >= 1; sinks >= 0; together they may exceed a sequence
+ * Chunks are cut at 32-key boundaries of the tiles that hold visible keys, as
+ * in da_decode_attn_paged.  The launch is planned for da_window_keys(L_K_max,
+ * window, sinks) keys a sequence; the workspace need is da_workspace_bytes for
+ * that plan's num_splits.  Other arguments and errors as for da_decode_attn and
+ * da_decode_attn_paged, and DA_ERR_ARG for window or sinks out of range. */
+int da_decode_attn_window(const void* q, const void* k, const void* v, const int32_t* cu_seqlens_k,
+                          const int32_t* block_table, const int32_t* seq_lens, int page_size, int max_pages,
+                          int num_pages, void* out, float* lse_out, int B, int H_Q, int H_KV, int L_K_max, int d,
+                          float softmax_scale, int window, int sinks, int num_splits, int pack_gqa,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Most keys that the 32-key tiles of a window and its sinks hold, in a sequence
+ * of up to L_K_max keys: the length da_decode_attn_window plans for.  -1 for
+ * arguments it does not take.  Host only. */
+int da_window_keys(int L_K_max, int window, int sinks);
+
+/* Block tables and slots of a step, on the device, from request lengths:
+ * request b holds lens[b] keys in the first ceil(lens[b] / page_size) pages of
+ * its row of block_table and gets new_lens[b] more.  The pages it still needs
+ * come off a list of free pages, in request order.
+ *   lens, new_lens int32 [B], B <= DA_MAX_REQUESTS; negative counts as 0
+ *   free_pages     int32 [num_free] page ids; *taken of them are in use already
+ *   block_table    int32 [B, max_pages]: the entries of the new pages are
+ *                  written, no others
+ *   lens_out       int32 [B]: lens + new_lens, or lens for a request that was
+ *                  not extended
+ *   taken_out      int32 [1]: entries of free_pages in use now
+ *   cu_new         NULL or int32 [B + 1]: prefix sums of new_lens: the rows of
+ *                  request b's new tokens are [cu_new[b], cu_new[b + 1])
+ *   slots          int32 [max_tokens]: of each new token's row, the cache row
+ *                  page * page_size + offset that is its place; -1 for a token
+ *                  of a request that was not extended, for a page id outside [0,
+ *                  num_pages), and for rows past the last token
+ *   positions      NULL or int32 [max_tokens]: the token's position in its
+ *                  sequence; 0 past the last token
+ * A request is not extended (as a whole) where its table row could not hold
+ * the keys, its rows would pass max_tokens, or the list does not hold the
+ * pages that it and the extended requests before it need; later ones that need
+ * no page are extended all the same.  lens_out may be lens and taken_out may
+ * be taken (a state advanced in place by a captured step); no other output may
+ * overlap an input.  Lengths and their sums count as 2^30 beyond that.  One
+ * launch; two where outputs take their inputs' place and max_tokens > 1024.
+ * Errors: DA_ERR_SHAPE, DA_ERR_NULL, DA_ERR_ALIGN, before any HIP call. */
+int da_extend_tables(const int32_t* lens, const int32_t* new_lens, const int32_t* free_pages,
+                     const int32_t* taken, int32_t* block_table, int32_t* lens_out, int32_t* taken_out,
+                     int32_t* cu_new, int32_t* slots, int32_t* positions, int B, int page_size, int max_pages,
+                     int num_pages, int num_free, int max_tokens, void* stream);
+
+/* What a layer does between its projections and the attention, in one pass:
+ * per-head norms of q and k, the rotation by position, and the rows' way into
+ * a bf16 cache.
+ *   q          bf16 [N, H_Q, d], token n at q + n * q_stride elements; or NULL
+ *              (H_Q 0): keys and values only
+ *   k, v       bf16 [N, H_KV, d], tokens k_stride and v_stride apart (the three
+ *              may be slices of one projection's output); strides are multiples
+ *              of 8, heads d apart
+ *   q_weight, k_weight  NULL (not normalised) or bf16 [d]: x becomes x /
+ *              sqrt(mean(x^2) + eps) * weight over the head's d dims
+ *   rope       NULL or fp32 [rope_rows, rope_dim]: the cosines, then the sines,
+ *              of a position's rope_dim / 2 angles; rope_dim a multiple of 16
+ *              up to d.  The first rope_dim dims of each head turn, dim i with
+ *              dim i + rope_dim / 2, or with neighbours == 1 dims 2i and 2i + 1:
+ *              (a, b) -> (a cos - b sin, b cos + a sin), after the norm
+ *   positions  int32 [N], with rope; outside [0, rope_rows) counts as a row of
+ *              zeros
+ *   slots      int32 [N] cache rows, each at most once (a row given twice ends
+ *              with an unspecified mixture); outside [0, num_rows) the token is
+ *              not written.  NULL: token n goes to row n
+ *   q_out      bf16 [N, H_Q, d] dense; may be q where q_stride is H_Q * d
+ *   k_cache, v_cache  bf16 [num_rows, H_KV, d]: page pools (row = page *
+ *              page_size + offset), or contiguous sequences
+ * Computed in 32 bits and rounded to bf16 once; v is copied.  One launch; no
+ * row without a token is touched.  Errors: DA_ERR_NULL, DA_ERR_SHAPE,
+ * DA_ERR_ALIGN (16 bytes for bf16 and rope), DA_ERR_UNSUPPORTED (d, rope_dim),
+ * DA_ERR_ARG (eps, neighbours). */
+int da_append_kv(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                 int64_t v_stride, const void* q_weight, const void* k_weight, float eps, const float* rope,
+                 int rope_rows, int rope_dim, int neighbours, const int32_t* positions, const int32_t* slots,
+                 void* q_out, void* k_cache, void* v_cache, int64_t num_rows, int N, int H_Q, int H_KV, int d,
+                 void* stream);
+
+/* da_append_kv into a cache of 4-bit values, 0.27 of the bf16 cache's bytes.
+ *   cache      [num_pages, H_KV, page_size / 32, DA_KV4_TILE_BYTES] bytes,
+ *              page_size a multiple of 32, num_pages * page_size < 2^31: a tile
+ *              is 32 keys of one head: 32 x 64 bytes of K codes, as many of V,
+ *              256 scale bytes.  Byte i of a row holds dims 2i (low half) and 2i
+ *              + 1 as e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6; the high bit negative);
+ *              block g of 32 dims of key r has its K scale at 4 (4 (r % 16) + g)
+ *              + r / 16 and its V scale two bytes further on.  A value is its
+ *              code times 2^(scale - 127), exact in bf16; scale 255 is NaN
+ * A block's scale is the least power of two that leaves its largest magnitude
+ * at most 7 (within [2^-125, 2^125]), codes are rounded to the nearest, ties to
+ * even.  Keys are rounded to bf16 first, so the cache holds what a quantised
+ * bf16 cache would.  A block with an infinity or a NaN becomes NaN. */
+int da_append_kv4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                  int64_t v_stride, const void* q_weight, const void* k_weight, float eps, const float* rope,
+                  int rope_rows, int rope_dim, int neighbours, const int32_t* positions, const int32_t* slots,
+                  void* q_out, void* cache, int page_size, int num_pages, int N, int H_Q, int H_KV, int d,
+                  void* stream);
+
+/* Rows of a 4-bit cache as bf16 (exact): k_out, v_out [N, H_KV, d] of cache rows
+ * slots[0 .. N), or rows 0 .. N - 1 where slots is NULL; zeros for a row outside
+ * the cache.  Errors as for da_append_kv4. */
+int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_out, int N, int H_KV,
+                int page_size, int num_pages, int d, void* stream);
+
+/* Decode attention over a paged cache of 4-bit values (da_append_kv4), with or
+ * without a window: the softmax of da_decode_attn_paged over the values the
+ * cache stands for.
+ *   cache      as for da_append_kv4; a page id outside [0, num_pages) reads as
+ *              zero keys and values; codes and scales of rows past a sequence
+ *              or outside the window do not reach the result
+ *   window     0: all keys (sinks is then ignored); otherwise as for
+ *              da_decode_attn_window
+ *   num_splits <= 0: chosen; else 1..64: chunks that a sequence of L_K_max keys
+ *              is cut into.  Every sequence is cut into chunks of the same
+ *              length in 32-key tiles, so a shorter one has fewer, and one that
+ *              fits a chunk writes its output directly
+ *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, window, sinks,
+ *              num_splits, 0); 0 bytes for one chunk.  Counters in its last
+ *              DA_ARRIVAL_BYTES zero before the first call, as for da_decode_attn
+ * One launch.  Results are bit-identical across runs for the same arguments.
+ * Other arguments and errors as for da_decode_attn_paged. */
+int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* seq_lens,
+                       void* out, float* lse_out, int B, int H_Q, int H_KV, int page_size, int max_pages,
+                       int num_pages, int L_K_max, int d, float softmax_scale, int window, int sinks,
+                       int num_splits, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes da_decode_attn_kv4 needs (num_cus 0: query the current
+ * device); 0 for a shape it does not take. */
+size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int window, int sinks, int num_splits,
+                              int num_cus);
 
 /* The split step alone: the partial softmax state of every chunk (the
  * per-chunk max, sum and unnormalised output the paper's final reduction

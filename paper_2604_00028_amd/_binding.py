@@ -19,6 +19,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdecode_attn.so")
 HEAD_DIM = 128
 MAX_SPLITS = 64
+KV4_TILE_BYTES = 4352  # 32 keys of one KV head in the 4-bit cache
+MAX_REQUESTS = 4096    # of one da_extend_tables call
 DEALT_MIN_KEYS = 2561  # da_prefers_dealt never holds for shorter batches: no need to ask
 
 DA_OK = 0
@@ -44,6 +46,8 @@ EXPORTS = (
     "da_decode_attn_planned", "da_decode_attn_noalloc", "da_decode_attn_paged", "da_decode_attn_paged_planned", "da_schedule_max_bytes",
     "da_make_schedule", "da_schedule_workspace_bytes",
     "da_decode_attn_scheduled", "da_decode_attn_dealt", "da_dealt_workspace_bytes", "da_prefers_dealt",
+    "da_decode_attn_window", "da_window_keys", "da_extend_tables", "da_append_kv", "da_append_kv4", "da_read_kv4",
+    "da_decode_attn_kv4", "da_kv4_workspace_bytes",
     "da_split_partials", "da_combine_splits", "da_device_info", "da_strerror",
     "da_last_error",
 )
@@ -91,6 +95,7 @@ _I = ctypes.c_int
 _P = ctypes.c_void_p
 _F = ctypes.c_float
 _Z = ctypes.c_size_t
+_L = ctypes.c_int64
 
 
 def _hip_runtimes_loaded() -> List[str]:
@@ -156,6 +161,26 @@ def load() -> ctypes.CDLL:
     lib.da_decode_attn_dealt.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _I, _I, _I, _I, _I, _F,
                                          ctypes.c_int64, _P, _Z, _P]
     lib.da_decode_attn_dealt.restype = _I
+    lib.da_decode_attn_window.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _I, _I, _I, _I, _I, _F, _I, _I,
+                                          _I, _I, _P, _Z, _P]
+    lib.da_decode_attn_window.restype = _I
+    lib.da_window_keys.argtypes = [_I, _I, _I]
+    lib.da_window_keys.restype = _I
+    lib.da_extend_tables.argtypes = [_P] * 10 + [_I] * 6 + [_P]
+    lib.da_extend_tables.restype = _I
+    lib.da_append_kv.argtypes = [_P, _L, _P, _L, _P, _L, _P, _P, _F, _P, _I, _I, _I, _P, _P, _P, _P, _P, _L, _I, _I,
+                                 _I, _I, _P]
+    lib.da_append_kv.restype = _I
+    lib.da_append_kv4.argtypes = [_P, _L, _P, _L, _P, _L, _P, _P, _F, _P, _I, _I, _I, _P, _P, _P, _P, _I, _I, _I, _I,
+                                  _I, _I, _P]
+    lib.da_append_kv4.restype = _I
+    lib.da_read_kv4.argtypes = [_P, _P, _P, _P, _I, _I, _I, _I, _I, _P]
+    lib.da_read_kv4.restype = _I
+    lib.da_decode_attn_kv4.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I, _I, _P, _Z,
+                                       _P]
+    lib.da_decode_attn_kv4.restype = _I
+    lib.da_kv4_workspace_bytes.argtypes = [_I] * 8
+    lib.da_kv4_workspace_bytes.restype = _Z
     lib.da_split_partials.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _F, _I, _I, _P]
     lib.da_split_partials.restype = _I
     lib.da_combine_splits.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _P]
@@ -639,4 +664,266 @@ def da_combine_splits(o_part: torch.Tensor, m_part: torch.Tensor, l_part: torch.
         out = torch.empty((B, H_Q, d), dtype=torch.bfloat16, device=dev)
     _check(load().da_combine_splits(_ptr(o_part), _ptr(m_part), _ptr(l_part), _ptr(out), _ptr(lse_out), s, B, H_Q,
                                     d, _stream(dev, stream)))
+    return out
+
+
+# ---------------------------------------------------------------- a step's cache: tables, rows, windows, 4 bits
+
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _call(dev: torch.device, fn, *args) -> int:
+    """fn(*args) with `dev` the current device (the library launches on that one)."""
+    if dev.index == _get_device():
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
+
+
+def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dev: torch.device) -> None:
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+
+
+def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse_out: Optional[torch.Tensor]) -> torch.Tensor:
+    if out is None:
+        out = _new_out(q)
+    else:
+        _need("out", out, torch.bfloat16, q.shape, q.device)
+    if lse_out is not None:
+        _need("lse_out", lse_out, torch.float32, q.shape[:2], q.device)
+    return out
+
+
+def _one_device(dev: torch.device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+
+
+def da_window_keys(L_K_max: int, window: int, sinks: int = 0) -> int:
+    return int(load().da_window_keys(L_K_max, window, sinks))
+
+
+def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0,
+                          cu_seqlens_k: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                          seq_lens: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                          lse_out: Optional[torch.Tensor] = None, *, L_K_max: Optional[int] = None,
+                          softmax_scale: float = 0.0, num_splits: int = 0, pack_gqa: int = -1,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Decode attention that sees the last `window` keys of each sequence and
+    its first `sinks` keys; returns `out`.  K and V as for da_decode_attn (fixed,
+    or packed with cu_seqlens_k), or with block_table and seq_lens paged."""
+    page_size = max_pages = num_pages = 0
+    if block_table is None:
+        B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
+    else:
+        if seq_lens is None or L_K_max is None:
+            raise ValueError("seq_lens and L_K_max (the host-known longest sequence) are required with block_table")
+        B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k, v, block_table, seq_lens)
+        L = int(L_K_max)
+    dev = q.device
+    _one_device(dev, k=k, v=v, cu_seqlens_k=cu_seqlens_k, block_table=block_table, seq_lens=seq_lens)
+    out = _outputs(q, out, lse_out)
+    s_handle = _stream(dev, stream)
+    ws = _offered(workspace, dev, s_handle)
+    while True:
+        rc = _call(dev, load().da_decode_attn_window, _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(block_table),
+                   _ptr(seq_lens), page_size, max_pages, num_pages, _ptr(out), _ptr(lse_out), B, H_Q, H_KV, L, d,
+                   float(softmax_scale), int(window), int(sinks), int(num_splits), int(pack_gqa), _ptr(ws), _nbytes(ws),
+                   s_handle)
+        if rc != DA_ERR_WORKSPACE or workspace is not None:
+            break
+        with torch.cuda.device(dev):
+            plan = da_make_plan(B, H_Q, H_KV, da_window_keys(L, window, sinks), d, num_splits, pack_gqa)
+        workspace = ws = workspace_for(dev, s_handle, da_workspace_bytes(B, H_Q, d, plan.num_splits))
+    _check(rc)
+    return out
+
+
+def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: torch.Tensor, taken: torch.Tensor,
+                     block_table: torch.Tensor, page_size: int, num_pages: int, max_tokens: int,
+                     lens_out: Optional[torch.Tensor] = None, taken_out: Optional[torch.Tensor] = None,
+                     cu_new: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                     positions: Optional[torch.Tensor] = None, *, stream=None) -> Tuple[torch.Tensor, ...]:
+    """Block tables and slots of a step from request lengths; returns
+    (lens_out, taken_out, cu_new, slots, positions), new tensors where none are
+    passed.  All int32 on one device: lens and new_lens [B]; free_pages: page
+    ids, of which `taken` [1] are in use; block_table [B, max_pages], whose
+    entries of new pages are written; slots and positions [max_tokens].
+    lens_out may be lens and taken_out may be taken."""
+    dev = lens.device
+    i32 = torch.int32
+    B = lens.numel()
+    if block_table.dim() != 2 or not lens.is_cuda:
+        raise ValueError("block_table must be [B, max_pages], and all tensors on the GPU")
+    max_pages = block_table.shape[1]
+    num_free = free_pages.numel()
+    max_tokens = int(max_tokens)
+    for name, t, shape in (("lens", lens, (B,)), ("new_lens", new_lens, (B,)), ("free_pages", free_pages, (num_free,)),
+                           ("taken", taken, (1,)), ("block_table", block_table, (B, max_pages))):
+        _need(name, t, i32, shape, dev)
+    given = (lens_out, taken_out, cu_new, slots, positions)
+    sizes = [B, 1, B + 1, max_tokens, max_tokens]
+    if max_tokens < 0:
+        raise ValueError("max_tokens must not be negative")
+    for name, t, n in zip(("lens_out", "taken_out", "cu_new", "slots", "positions"), given, sizes):
+        if t is not None:
+            _need(name, t, i32, (n,), dev)
+    if any(t is None for t in given):
+        new = torch.empty(sum(n for t, n in zip(given, sizes) if t is None), dtype=i32, device=dev).split(
+            [n for t, n in zip(given, sizes) if t is None])
+        new = iter(new)
+        given = tuple(next(new) if t is None else t for t in given)
+    _check(_call(dev, load().da_extend_tables, _ptr(lens), _ptr(new_lens), _ptr(free_pages), _ptr(taken),
+                 _ptr(block_table), *(_ptr(t) for t in given), B, int(page_size), max_pages, int(num_pages), num_free,
+                 max_tokens, _stream(dev, stream)))
+    return given
+
+
+def _rows(name: str, t: torch.Tensor, heads: Optional[int], dev: torch.device) -> Tuple[int, int]:
+    """Token stride and heads of q, k or v [N, heads, d]: heads dense, tokens any distance apart."""
+    if (t.dim() != 3 or t.dtype is not torch.bfloat16 or t.device != dev or not t.is_cuda or t.stride(2) != 1
+            or (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or (heads is not None and t.shape[1] != heads)):
+        raise ValueError(f"{name} must be a bfloat16 CUDA tensor [N, heads, d] whose heads are dense")
+    return (t.stride(0) if t.shape[0] > 1 else 0), t.shape[1]
+
+
+def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours, q_out):
+    """Check what the append calls share; (their leading arguments, (N, H_Q, H_KV, d), q_out)."""
+    dev = k.device
+    k_stride, H_KV = _rows("k", k, None, dev)
+    v_stride, _ = _rows("v", v, H_KV, dev)
+    N, _, d = k.shape
+    q_stride = H_Q = 0
+    if v.shape != k.shape:
+        raise ValueError("k and v shapes differ")
+    if q is not None:
+        q_stride, H_Q = _rows("q", q, None, dev)
+        if q.shape[0] != N or q.shape[2] != d:
+            raise ValueError("q must be [N, H_Q, d] with k's N and d")
+        if q_out is None:
+            q_out = torch.empty((N, H_Q, d), dtype=torch.bfloat16, device=dev)
+        else:
+            _need("q_out", q_out, torch.bfloat16, (N, H_Q, d), dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _need(name, w, torch.bfloat16, (d,), dev)
+    rope_rows = rope_dim = 0
+    if rope is not None:
+        if rope.dim() != 2 or positions is None:
+            raise ValueError("rope must be [positions, rope_dim], and needs positions")
+        rope_rows, rope_dim = rope.shape
+        _need("rope", rope, torch.float32, (rope_rows, rope_dim), dev)
+        _need("positions", positions, torch.int32, (N,), dev)
+    if slots is not None:
+        _need("slots", slots, torch.int32, (N,), dev)
+    args = (_ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_weight), _ptr(k_weight), float(eps),
+            _ptr(rope), rope_rows, rope_dim, int(neighbours), _ptr(positions) if rope is not None else None,
+            _ptr(slots), _ptr(q_out))
+    return args, (N, H_Q, H_KV, d), q_out
+
+
+def da_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
+                 slots: Optional[torch.Tensor], k_cache: torch.Tensor, v_cache: torch.Tensor, *,
+                 rope: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, neighbours: bool = False,
+                 q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Norms of q and k per head, rotation by position, and k and v into the
+    rows `slots` of a bf16 cache; returns q_out (None without q).
+    q [N, H_Q, d], k, v [N, H_KV, d]: slices of one projection's output will do;
+    caches [..., H_KV, d] (page pools, or sequences), rows counted over the
+    leading dims; rope fp32 [positions, rope_dim]: cosines, then sines."""
+    args, (N, H_Q, H_KV, d), q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
+                                                  q_out)
+    dev = k.device
+    if k_cache.dim() < 3 or k_cache.shape[-2:] != (H_KV, d):
+        raise ValueError("k_cache must be [..., H_KV, d]")
+    _need("k_cache", k_cache, torch.bfloat16, k_cache.shape, dev)
+    _need("v_cache", v_cache, torch.bfloat16, k_cache.shape, dev)
+    _check(_call(dev, load().da_append_kv, *args, _ptr(k_cache), _ptr(v_cache), k_cache.numel() // (H_KV * d), N, H_Q,
+                 H_KV, d, _stream(dev, stream)))
+    return q_out
+
+
+def _kv4_cache(cache: torch.Tensor) -> Tuple[int, int, int]:
+    """(num_pages, H_KV, page_size) of a 4-bit cache."""
+    if (cache.dim() != 4 or cache.dtype is not torch.uint8 or cache.shape[3] != KV4_TILE_BYTES
+            or not cache.is_contiguous() or not cache.is_cuda):
+        raise ValueError(f"cache must be a contiguous uint8 CUDA tensor [num_pages, H_KV, page_size / 32, {KV4_TILE_BYTES}]")
+    return cache.shape[0], cache.shape[1], 32 * cache.shape[2]
+
+
+def da_append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
+                  slots: Optional[torch.Tensor], cache: torch.Tensor, *, rope: Optional[torch.Tensor] = None,
+                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  neighbours: bool = False, q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """da_append_kv into a 4-bit cache, uint8 [num_pages, H_KV, page_size / 32, 4352]; returns q_out."""
+    args, (N, H_Q, H_KV, d), q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
+                                                  q_out)
+    dev = k.device
+    num_pages, heads, page_size = _kv4_cache(cache)
+    if heads != H_KV:
+        raise ValueError(f"the cache has {heads} KV heads, k {H_KV}")
+    _one_device(dev, cache=cache)
+    _check(_call(dev, load().da_append_kv4, *args, _ptr(cache), page_size, num_pages, N, H_Q, H_KV, d,
+                 _stream(dev, stream)))
+    return q_out
+
+
+def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
+                stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """K and V bf16 [N, H_KV, 128] of the rows `slots` of a 4-bit cache (None: all its rows)."""
+    num_pages, H_KV, page_size = _kv4_cache(cache)
+    dev = cache.device
+    if slots is not None:
+        _need("slots", slots, torch.int32, (slots.numel(),), dev)
+    N = num_pages * page_size if slots is None else slots.numel()
+    k, v = torch.empty((2, N, H_KV, HEAD_DIM), dtype=torch.bfloat16, device=dev)
+    _check(_call(dev, load().da_read_kv4, _ptr(cache), _ptr(slots), _ptr(k), _ptr(v), N, H_KV, page_size, num_pages,
+                 HEAD_DIM, _stream(dev, stream)))
+    return k, v
+
+
+def da_kv4_workspace_bytes(B: int, H_Q: int, H_KV: int, L_K_max: int, window: int = 0, sinks: int = 0,
+                           num_splits: int = 0, num_cus: int = 0) -> int:
+    return int(load().da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, window, sinks, num_splits, num_cus))
+
+
+def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                       L_K_max: int, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
+                       lse_out: Optional[torch.Tensor] = None, *, softmax_scale: float = 0.0, num_splits: int = 0,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Decode attention over a paged cache of 4-bit values (da_append_kv4);
+    returns `out`.  block_table, seq_lens and L_K_max as for
+    da_decode_attn_paged; window (0: none) and sinks as for
+    da_decode_attn_window."""
+    dev = q.device
+    if q.dim() != 3 or q.dtype is not torch.bfloat16 or not q.is_contiguous() or not q.is_cuda:
+        raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")
+    num_pages, H_KV, page_size = _kv4_cache(cache)
+    B, H_Q, d = q.shape
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
+    max_pages = block_table.shape[1]
+    _need("block_table", block_table, torch.int32, (B, max_pages), dev)
+    _need("seq_lens", seq_lens, torch.int32, (B,), dev)
+    _one_device(dev, cache=cache)
+    out = _outputs(q, out, lse_out)
+    s_handle = _stream(dev, stream)
+    L = int(L_K_max)
+    ws = _offered(workspace, dev, s_handle)
+    while True:
+        rc = _call(dev, load().da_decode_attn_kv4, _ptr(q), _ptr(cache), _ptr(block_table), _ptr(seq_lens), _ptr(out),
+                   _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L, d, float(softmax_scale), int(window),
+                   int(sinks), int(num_splits), _ptr(ws), _nbytes(ws), s_handle)
+        if rc != DA_ERR_WORKSPACE or workspace is not None:
+            break
+        with torch.cuda.device(dev):
+            need = da_kv4_workspace_bytes(B, H_Q, H_KV, L, window, sinks, num_splits)
+        workspace = ws = workspace_for(dev, s_handle, need)
+    _check(rc)
     return out

@@ -338,6 +338,12 @@ int check_shape(int B, int H_Q, int H_KV, int L_K_max, int d) {
   return DA_OK;
 }
 
+int window_keys(int L_K_max, int window, int sinks) {
+  // the sinks' tiles, and the window's where it starts with the last key of a tile
+  const int64_t tiles = ((int64_t)sinks + 31) / 32 + ((int64_t)window + 62) / 32;
+  return (int)std::min<int64_t>(L_K_max, 32 * tiles);
+}
+
 int plan(int B, int H_Q, int H_KV, int L_K_max, int d, int num_splits, int pack_gqa, int num_cus,
          int cu_margin, int policy, da_plan* out) {
   if (!out) return fail(DA_ERR_NULL, "plan output is NULL");
@@ -871,6 +877,10 @@ int da_make_plan(int B, int H_Q, int H_KV, int L_K_max, int d, int num_splits, i
     if (rc) return rc;
   }
   return da::plan(B, H_Q, H_KV, L_K_max, d, num_splits, pack_gqa, num_cus, cu_margin, policy, out);
+}
+
+int da_window_keys(int L_K_max, int window, int sinks) {
+  return L_K_max < 0 || window < 1 || sinks < 0 ? -1 : da::window_keys(L_K_max, window, sinks);
 }
 
 double da_model_time(int policy, int B, int H_Q, int H_KV, int L_K, int heads_per_tile, int num_splits,

@@ -158,6 +158,11 @@ const TableEntry* table_entry(bool streamed, int B, int H_Q, int H_KV, int L_K);
 int plan(int B, int H_Q, int H_KV, int L_K_max, int d, int num_splits, int pack_gqa, int num_cus,
          int cu_margin, int policy, da_plan* out);
 
+// Most keys that the tiles a window of `window` keys and `sinks` first keys
+// touches hold, in a sequence of up to L_K_max keys: the length that a windowed
+// launch is planned for.
+int window_keys(int L_K_max, int window, int sinks);
+
 // Argument checks shared by the launch entry points (no HIP calls).
 int check_shape(int B, int H_Q, int H_KV, int L_K_max, int d);
 
