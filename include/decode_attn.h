@@ -602,8 +602,8 @@ int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_ou
  *              is cut into.  Every sequence is cut into chunks of the same
  *              length in 32-key tiles, so a shorter one has fewer, and one that
  *              fits a chunk writes its output directly
- *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, window, sinks,
- *              num_splits, 0); 0 bytes for one chunk.  Counters in its last
+ *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, num_pages *
+ *              page_size, window, sinks, num_splits, 0); 0 bytes for one chunk.  Counters in its last
  *              DA_ARRIVAL_BYTES zero before the first call, as for da_decode_attn
  * One launch.  Results are bit-identical across runs for the same arguments.
  * Other arguments and errors as for da_decode_attn_paged. */
@@ -612,10 +612,12 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
                        int num_pages, int L_K_max, int d, float softmax_scale, int window, int sinks,
                        int num_splits, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Workspace bytes da_decode_attn_kv4 needs (num_cus 0: query the current
- * device); 0 for a shape it does not take. */
-size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int window, int sinks, int num_splits,
-                              int num_cus);
+/* Workspace bytes da_decode_attn_kv4 needs (pool_keys: num_pages * page_size,
+ * a bound of the batch's keys that the chunk length goes by; <= 0: enough for
+ * any pool; num_cus 0: query the current device); 0 for a shape it does not
+ * take, or one chunk. */
+size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t pool_keys, int window, int sinks,
+                              int num_splits, int num_cus);
 
 /* The split step alone: the partial softmax state of every chunk (the
  * per-chunk max, sum and unnormalised output the paper's final reduction

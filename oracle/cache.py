@@ -76,15 +76,16 @@ def kv4_codes(rows: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
     finite = np.isfinite(x).all(axis=-1)
     x = np.where(finite[..., None], x, 0.0)
     top = np.abs(x).max(axis=-1)
-    # least e with top <= 7 * 2^e
-    e = np.full(top.shape, -125)
-    for k in range(-125, 125):
-        e = np.where(top > 7.0 * 2.0 ** k, k + 1, e)
+    # least e with top <= 7 * 2^e: top = f 2^x with f in [0.5, 1), 7 = 0.875 * 2^3
+    f, x2 = np.frexp(top)
+    e = np.clip(np.where(f <= 0.875, x2 - 3, x2 - 2), -125, 125)
+    e = np.where(top == 0, -125, e)
     mag = np.abs(x) / 2.0 ** e[..., None].astype(np.float64)
-    dist = np.abs(mag[..., None] - E2M1)
-    near = dist == dist.min(axis=-1, keepdims=True)
-    first, last = near.argmax(axis=-1), 7 - near[..., ::-1].argmax(axis=-1)
-    code = np.where(first % 2 == 0, first, last)  # of two equally near the even one
+    # nearest of the eight, of two equally near the even one
+    code = np.zeros(mag.shape, dtype=np.int64)
+    for n in range(1, 8):
+        mid = (E2M1[n - 1] + E2M1[n]) / 2
+        code = np.where((mag > mid) | ((mag == mid) & (n % 2 == 0)), n, code)
     code = code + 8 * np.signbit(x)
     return code.reshape(rows.shape).astype(np.uint8), np.where(finite, e + 127, 255).astype(np.uint8)
 

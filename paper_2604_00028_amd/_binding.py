@@ -179,7 +179,7 @@ def load() -> ctypes.CDLL:
     lib.da_decode_attn_kv4.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I, _I, _P, _Z,
                                        _P]
     lib.da_decode_attn_kv4.restype = _I
-    lib.da_kv4_workspace_bytes.argtypes = [_I] * 8
+    lib.da_kv4_workspace_bytes.argtypes = [_I] * 4 + [_L] + [_I] * 4
     lib.da_kv4_workspace_bytes.restype = _Z
     lib.da_split_partials.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _F, _I, _I, _P]
     lib.da_split_partials.restype = _I
@@ -888,9 +888,9 @@ def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
     return k, v
 
 
-def da_kv4_workspace_bytes(B: int, H_Q: int, H_KV: int, L_K_max: int, window: int = 0, sinks: int = 0,
-                           num_splits: int = 0, num_cus: int = 0) -> int:
-    return int(load().da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, window, sinks, num_splits, num_cus))
+def da_kv4_workspace_bytes(B: int, H_Q: int, H_KV: int, L_K_max: int, pool_keys: int = 0, window: int = 0,
+                           sinks: int = 0, num_splits: int = 0, num_cus: int = 0) -> int:
+    return int(load().da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, pool_keys, window, sinks, num_splits, num_cus))
 
 
 def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
@@ -923,7 +923,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
         with torch.cuda.device(dev):
-            need = da_kv4_workspace_bytes(B, H_Q, H_KV, L, window, sinks, num_splits)
+            need = da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size, window, sinks, num_splits)
         workspace = ws = workspace_for(dev, s_handle, need)
     _check(rc)
     return out

@@ -18,14 +18,19 @@ using da::aligned;
 using da::ensure_gfx950;
 
 constexpr int W = 4;  // waves per workgroup
+constexpr int kFp8 = 0, kFp4 = 4;  // operand formats of the scaled product: e4m3, e2m1
 
 struct Kv4Params {
   Params p;  // q, out, lse, chunk states, counters, block table, lengths, shape, window
   const unsigned char* cache;
-  int chunk_tiles;   // tiles of 32 keys a chunk holds
+  int chunk_tiles;   // tiles of 32 keys a chunk holds (even)
   int blocks;        // tiles a page holds
+  uint32_t page_bytes;
   Div div_blocks;
   Div div_tiles;     // p.tiles
+  int groups;        // dealt: shares of the batch's tiles a head tile has
+  Div div_groups;
+  int halves;        // dealt: half shares where the lengths differ much
 };
 
 constexpr int kv4_smem_bytes(int NT) {
@@ -33,8 +38,94 @@ constexpr int kv4_smem_bytes(int NT) {
 }
 static_assert(kv4_smem_bytes(1) >= (2 * (DA_MAX_SPLITS + 16) * 32 + 8 * 32) * 4, "the merge stages chunk maxima and sums");
 
-template <int NT, bool NTL>
-__global__ void __launch_bounds__(64 * W) kv4_kernel(Kv4Params a) {
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// A head's query as the 8-bit operand of the scaled product: q = 2^scale (hi +
+// lo / 16), hi and lo e4m3.  The scale brings the head's largest magnitude into
+// [2^7, 2^8), hi is q rounded to its four bits and lo what that leaves, which
+// has four bits or fewer: exact for every element within 13 powers of two of
+// the largest, off by less than 2^-20 of the largest below that.
+struct Query {
+  i32x8 hi, lo;
+  int hi_scale, lo_scale;
+};
+
+// x: the lane's 32 bf16 values (dims 16 quad + [0, 16) and 64 + 16 quad + [0,
+// 16), the operand's order).
+__device__ __forceinline__ Query split_query(const u32x4 (&x)[4]) {
+  float top = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t two = x[i / 4][i % 4];
+    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(two << 16)), fabsf(__uint_as_float(two & 0xffff0000u))));
+    bad = bad || (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u;
+  }
+  top = max_rows(bad ? INFINITY : top);
+  const int e = max((int)(__float_as_uint(top) >> 23), 16) - 7;  // biased exponent of the scale
+  const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+  Query q;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float f[4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t two = x[i / 2][(2 * i + j) % 4];
+      f[2 * j] = __uint_as_float(two << 16) * down;
+      f[2 * j + 1] = __uint_as_float(two & 0xffff0000u) * down;
+    }
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], hi, true);
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (f[0] - a[0]), 16.f * (f[1] - a[1]), 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (f[2] - b[0]), 16.f * (f[3] - b[1]), lo, true);
+    q.hi[i] = hi;
+    q.lo[i] = lo;
+  }
+  // a query with an infinity or a NaN: scale NaN
+  q.hi_scale = top < INFINITY ? e : 255;
+  q.lo_scale = top < INFINITY ? e - 4 : 255;
+  return q;
+}
+
+// Softmax of a pair of tiles (64 keys) per head column, as TileReducer::softmax
+// does it for one: sc holds the raw scores, then the probabilities as bf16
+// operands of the two tiles.
+template <int NT>
+__device__ __forceinline__ void softmax_pair(TileReducer<NT, 8>& red, f32x4 (&sc)[NT][4], bf16x8 (&pb)[2][1][NT]) {
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float top = fmaxf(sc[nt][0][0], sc[nt][0][1]);
+#pragma unroll
+    for (int e = 2; e < 16; ++e) top = fmaxf(top, sc[nt][e / 4][e % 4]);
+    const float m_new = fmaxf(red.m[nt], max_rows(top) * red.scale_log2);
+    const float alpha = __builtin_amdgcn_exp2f(red.m[nt] - m_new);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(sc[nt][e / 4][e % 4], red.scale_log2, -m_new));
+      sc[nt][e / 4][e % 4] = x;
+      sum += x;
+    }
+    red.l[nt] = red.l[nt] * alpha + sum;
+    red.m[nt] = m_new;
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int nn = 0; nn < 8; ++nn) red.o[nt][nn] *= alpha;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 pk;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pk[i] = pack_bf16x2(sc[nt][2 * h + i / 2][2 * (i % 2)], sc[nt][2 * h + i / 2][2 * (i % 2) + 1]);
+      pb[h][0][nt] = as_bf16x8(pk);
+    }
+  }
+}
+
+template <int NT, bool NTL, bool WIN, bool DEAL>
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2, 8)))
+kv4_kernel(Kv4Params a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int kv_aux = NTL ? 2 : 0;
   const Params& p = a.p;
@@ -43,140 +134,291 @@ __global__ void __launch_bounds__(64 * W) kv4_kernel(Kv4Params a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, quad = lane >> 4;
 
-  // ---- chunk and tile: all first chunks, then all second ones, ...
-  const int chunk = div_by((int)blockIdx.x, a.div_tiles);
-  const int tile = (int)blockIdx.x - chunk * p.tiles;
-  const int b = div_by(tile, p.div_tps);
-  const int head0 = (tile - b * p.tiles_per_seq) * p.hpt;
+  // ---- this workgroup's sequence, head tile and chunk
+  int b, ht, chunk, L, chunk_tiles, chunks = 0;
+  int64_t srow0, cstride;  // state row of its first head; rows between two chunks of a head
+  Window wn{};
+  if constexpr (DEAL) {
+    // The lengths decide: chunks of an even share of the batch's tiles for each
+    // of a.groups places a head tile, or half of one (at least a pair of tiles a wave, at most
+    // 64 chunks a sequence; three pairs a wave are as fast as a merge).  Sequences
+    // have as many workgroups as chunks, so none is launched for nothing but the
+    // few by which the chunks' roundings miss their bound.
+    int len = 0, tl = 0, win = 0;  // lane i: sequence win + i
+    auto window = [&](int b0) {
+      win = b0;
+      len = b0 + lane < p.B ? p.seq_lens[b0 + lane] : 0;
+      len = len < 0 ? 0 : (len > p.L_K ? p.L_K : len);
+      const int vis = WIN ? len - window_of(len, p.window, p.sinks).skip : len;
+      tl = (vis + kKeysPerTile - 1) / kKeysPerTile;
+    };
+    int sum = 0, top = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+      window(b0);
+      sum += tl;  // at most 2^30 in all
+      top = max(top, tl);
+    }
+    const int total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+    top = wave_top(top);
+    int share = div_by(total + a.groups - 1, a.div_groups);
+    // a longest sequence of more than one and a half times the mean length
+    if (a.halves && (int64_t)top * p.B * 2 > (int64_t)total * 3) share = (share + 1) / 2;
+    int per = max(max(share, 2 * W), (top + DA_MAX_SPLITS - 1) / DA_MAX_SPLITS);
+    if (top <= 6 * W) per = top;
+    per = max(2, (per + 1) & ~1);
+    chunk_tiles = per;
+    const float inv = 1.0f / (float)per;
+    auto lane_chunks = [&]() {  // below 2^24: the quotient is off by one at most
+      const int x = tl + per - 1;
+      int q = (int)((float)x * inv);
+      q += (q + 1) * per <= x ? 1 : 0;
+      q -= q * per > x ? 1 : 0;
+      return win + lane < p.B ? max(q, 1) : 0;
+    };
+    b = -1;
+    int first = 0;
+    L = 0;
+    for (int b0 = 0, before = 0; b0 < p.B; b0 += 64) {
+      if (p.B > 64) window(b0);
+      const int c = lane_chunks();
+      const int incl = wave_scan(c);
+      const uint64_t past = __ballot((before + incl) * p.tiles_per_seq > (int)blockIdx.x);
+      if (past) {
+        const int i = __ffsll((unsigned long long)past) - 1;
+        b = b0 + i;
+        first = (before + __builtin_amdgcn_readlane(incl - c, i)) * p.tiles_per_seq;
+        chunks = __builtin_amdgcn_readlane(c, i);
+        L = __builtin_amdgcn_readlane(len, i);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (b < 0) return;  // fewer chunks than the bound: the whole workgroup
+    const uint32_t at = blockIdx.x - (uint32_t)first;
+    ht = (int)(at / (uint32_t)chunks);
+    chunk = (int)at - ht * chunks;
+    srow0 = (int64_t)blockIdx.x * p.hpt;
+    cstride = p.hpt;
+    if constexpr (WIN) wn = window_of(L, p.window, p.sinks);
+  } else {
+    // all first chunks, then all second ones, ...
+    chunk = div_by((int)blockIdx.x, a.div_tiles);
+    const int tile = (int)blockIdx.x - chunk * p.tiles;
+    b = div_by(tile, p.div_tps);
+    ht = tile - b * p.tiles_per_seq;
+    chunk_tiles = a.chunk_tiles;
+    cstride = (int64_t)p.B * p.H_Q;
+    srow0 = (int64_t)chunk * cstride + (int64_t)b * p.H_Q + ht * p.hpt;
+  }
+  const int head0 = ht * p.hpt;
   const int kvh = div_by(head0, p.div_g);
-  int L = p.seq_lens[b];
-  L = L < 0 ? 0 : (L > p.L_K ? p.L_K : L);
-  const Window wn = window_of(L, p.window > 0 ? p.window : L, p.window > 0 ? p.sinks : 0);
-  const int vis = L - wn.skip;  // positions
-  const int T = (vis + kKeysPerTile - 1) / kKeysPerTile;
-  const int t0 = chunk * a.chunk_tiles;
-  if (t0 >= T && chunk > 0) return;  // the whole workgroup
-  const int chunks = max(1, (T + a.chunk_tiles - 1) / a.chunk_tiles);
-  const int t1 = min(t0 + a.chunk_tiles, T);
-
-  // ---- this wave's tiles: t0 + wave, + W, ...
-  const int n = t1 > t0 + wave ? (t1 - t0 - wave + W - 1) / W : 0;
-  // its page ids, 64 pages at a time, one per lane
-  int pg_win = 0, pg_ids = 0;
-  const int pg_last = n > 0 ? div_by(wn.key(kKeysPerTile * (t0 + wave + (n - 1) * W)) / kKeysPerTile, a.div_blocks) : -1;
-  auto pages = [&](int first) {
-    pg_win = first;
-    pg_ids = first + lane <= pg_last ? p.block_table[(int64_t)b * p.max_pages + first + lane] : 0;
-  };
-  auto tile_key = [&](int i) { return wn.key(kKeysPerTile * (t0 + wave + i * W)); };  // first key of tile i
-  if (n > 0) pages(div_by(tile_key(0) / kKeysPerTile, a.div_blocks));
-
-  struct Tile {
-    u32x4 k[2], v[2];
-    uint32_t scales;
-  };
-  auto load = [&](Tile& t, int i) {
-    const int kt = tile_key(i) / kKeysPerTile;
-    const int j = div_by(kt, a.div_blocks);
-    if (j - pg_win >= 64) pages(j);
-    const int page = __builtin_amdgcn_readlane(pg_ids, (j - pg_win) & 63);
-    const bool in = page >= 0 && page < p.num_pages;  // a page id outside the cache reads as zeros
-    const int64_t at = (((int64_t)(in ? page : 0) * p.H_KV + kvh) * a.blocks + (kt - j * a.blocks)) * DA_KV4_TILE_BYTES;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.cache + at, in ? DA_KV4_TILE_BYTES : 0u);
-    const uint32_t off = 64u * col + 16u * quad;
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) t.k[mt] = __builtin_amdgcn_raw_buffer_load_b128(r, off + 1024u * mt, 0, kv_aux);
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-      t.v[mt] = __builtin_amdgcn_raw_buffer_load_b128(r, off + 1024u * mt + (uint32_t)kKv4V, 0, kv_aux);
-    t.scales =
-        (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (uint32_t)kKv4Scales + 16u * col + 4u * quad, 0, kv_aux);
-  };
-
-  TileReducer<NT, 8> red;
-  red.scale_log2 = p.scale_log2;
-  red.quad = quad;
-  // Q in the order of the 4-bit rows: k-step j, lane group `quad` covers dims [32 quad + 8 j, +8)
+  // Q first: dims 16 quad + [0, 16) and 64 + 16 quad + [0, 16) of head column
+  // `col`; it is waited for while the first tiles are on their way
+  u32x4 qx[NT][4];
   {
     const __amdgpu_buffer_rsrc_t qr = make_rsrc(p.q + ((int64_t)b * p.H_Q + head0) * D, (uint32_t)p.hpt * (D * 2));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        red.q[nt][j] = as_bf16x8(__builtin_bit_cast(
+        qx[nt][j] = __builtin_bit_cast(
             u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                       qr, (uint32_t)(nt * 16 + col) * (D * 2) + 64u * quad + 16u * j, 0, 0)));
+                       qr, (uint32_t)(nt * 16 + col) * (D * 2) + 32u * quad + 16u * (j % 2) + 128u * (j / 2), 0, 0));
   }
-  red.reset();
-  unsigned char* vstage = smem + wave * kKeysPerTile * kVPitch;
-
-  auto reduce = [&](Tile& t, int i, bool more) {
-    const int first = tile_key(i);
-    const int nvalid = L - first;  // >= 1
-    bf16x8 kop[2][4];
+  const int t0 = chunk * chunk_tiles;
+  // this wave's pairs of tiles: 2 wave, 2 wave + 2 W, ... from t0 on
+  const int first_tile = t0 + 2 * wave;
+  auto tile_of = [&](int i, int h) { return first_tile + 2 * W * i + h; };
+  auto key_of = [&](int t) {  // first key of tile t
+    const int at = kKeysPerTile * t;
+    return WIN ? wn.key(at) : at;
+  };
+  // Page ids come by scalar loads, one pair ahead of the tiles' own loads (the
+  // table is not written while the kernel runs).
+  typedef const __attribute__((address_space(4))) int32_t* Ints;
+  const Ints table = (Ints)(uintptr_t)(p.block_table + (int64_t)b * p.max_pages);
+  struct Place {
+    int page[2], block[2];
+  };
+  // Past the wave's last tile it is some other place, which is not read.
+  auto place = [&](int i) {
+    Place pl;
+    int j[2];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      const float s = kv4_scale((t.scales >> (8 * mt)) & 0xffu);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        u32x4 y;
-        dequantise(t.k[mt][j], s, y);
-        kop[mt][j] = as_bf16x8(y);
-      }
+    for (int h = 0; h < 2; ++h) {
+      const int kt = key_of(tile_of(i, h)) / kKeysPerTile;
+      const int page = div_by(kt, a.div_blocks);
+      pl.block[h] = kt - page * a.blocks;
+      j[h] = min(page, p.max_pages - 1);
     }
-    f32x4 sc[NT][2];
-    red.scores(kop, sc);
-    const bool cut = nvalid < kKeysPerTile || wn.cuts(first);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) pl.page[h] = table[j[h]];
+    return pl;
+  };
+  // The length and, without a window, the first places come together.
+  if constexpr (!DEAL) L = ((Ints)(uintptr_t)p.seq_lens)[b];
+  Place first_place{}, next{};
+  if constexpr (!WIN || DEAL) {
+    first_place = place(0);
+    next = place(1);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  if constexpr (!DEAL) {
+    L = L < 0 ? 0 : (L > p.L_K ? p.L_K : L);
+    if constexpr (WIN) {
+      wn = window_of(L, p.window, p.sinks);
+      first_place = place(0);
+      next = place(1);
+    }
+  }
+  const int vis = L - wn.skip;  // positions
+  const int T = (vis + kKeysPerTile - 1) / kKeysPerTile;
+  if constexpr (!DEAL) chunks = max(1, (T + chunk_tiles - 1) / chunk_tiles);
+  const int t1 = min(t0 + chunk_tiles, T);
+  const int n = t1 > first_tile ? (t1 - first_tile + 2 * W - 1) / (2 * W) : 0;
+  const unsigned char* const heads = a.cache + (int64_t)kvh * a.blocks * DA_KV4_TILE_BYTES;
+  struct Tile {
+    u32x4 k[2], v[2];
+    uint32_t scales;
+    __amdgpu_buffer_rsrc_t at;
+  } tiles[2];
+  const uint32_t off = 64u * col + 16u * quad;
+  // K codes and scales of pair i, at `pl`; a tile past the wave's last: reads
+  // of no bytes (the number of loads in flight stays known).  V codes apart.
+  auto load_k = [&](const Place& pl, int i) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // a page id outside the cache reads as zeros
+      const bool in = (int)((uint32_t)pl.page[h] < (uint32_t)p.num_pages) & (int)(tile_of(i, h) < t1);
+      const unsigned char* at = heads + (uint64_t)(uint32_t)(in ? pl.page[h] : 0) * a.page_bytes +
+                                (uint32_t)pl.block[h] * (uint32_t)DA_KV4_TILE_BYTES;
+      Tile& t = tiles[h];
+      t.at = make_rsrc(at, in ? DA_KV4_TILE_BYTES : 0u);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) t.k[mt] = __builtin_amdgcn_raw_buffer_load_b128(t.at, off, 1024 * mt, kv_aux);
+      t.scales = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(t.at, 16u * col + 4u * quad, kKv4Scales, kv_aux);
+    }
+  };
+  auto load_v = [&](int h) {
+    Tile& t = tiles[h];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+      t.v[mt] = __builtin_amdgcn_raw_buffer_load_b128(t.at, off, 1024 * mt + kKv4V, kv_aux);
+  };
+
+  TileReducer<NT, 8> red;
+  red.scale_log2 = p.scale_log2;
+  red.quad = quad;
+  // The loads before the loop keep the order of those in it: what the loop may
+  // leave in flight at its top is counted over both.
+  __builtin_amdgcn_sched_barrier(0);
+  load_k(first_place, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  load_v(0);
+  __builtin_amdgcn_sched_barrier(0);
+  load_v(1);
+  __builtin_amdgcn_sched_barrier(0);
+  // a chunk past the sequence's end: the whole workgroup (its loads read nothing;
+  // leaving before them would put them behind the wait for the length)
+  if (!DEAL && t0 >= T && chunk > 0) return;
+  Query query[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) query[nt] = split_query(qx[nt]);
+  red.reset();
+  // V as bf16 rows of kVPitch bytes.  The 16-byte pieces of rows with bit 2 set
+  // change places in pairs: eight lanes that write one piece of eight rows then
+  // meet eight bank groups (without, 16 cycles a write instead of 8), and the
+  // transposing reads, which take both pieces of a pair, are as they were.
+  unsigned char* vstage = smem + wave * kKeysPerTile * kVPitch;
+  const int swap = 16 * ((col >> 2) & 1);
+  unsigned char* const vput[2] = {vstage + col * kVPitch + 64 * quad + swap,
+                                  vstage + col * kVPitch + 64 * quad + (swap ^ 16)};
+  auto stage_v = [&](const Tile& t, uint32_t scales) {
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
-      float s = kv4_scale((t.scales >> (16 + 8 * mt)) & 0xffu);
-      // whatever an invisible row holds, its values come out finite: a zero probability cancels them
-      const int row = 16 * mt + col;
-      if (cut && (row >= nvalid || wn.hides(first, row))) s = 1.f;
+      const float s = kv4_scale((scales >> (16 + 8 * mt)) & 0xffu);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         u32x4 y;
         dequantise(t.v[mt][j], s, y);
-        *reinterpret_cast<u32x4*>(vstage + row * kVPitch + 64 * quad + 16 * j) = y;
+        *reinterpret_cast<u32x4*>(vput[j & 1] + 16 * mt * kVPitch + 32 * (j >> 1)) = y;
       }
     }
-    if (more) load(t, i + 2);
-    if (cut) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = mt * 16 + quad * 4 + e;
-            sc[nt][mt][e] = row < nvalid && !wn.hides(first, row) ? sc[nt][mt][e] : -INFINITY;
-          }
-    }
-    bf16x8 pb[1][NT];
-    red.softmax(sc, kKeysPerTile, std::false_type{}, pb);
-    __builtin_amdgcn_wave_barrier();
-    const unsigned char* vrow = vstage + (quad * 4 + (col >> 2)) * kVPitch + 8 * (col & 3);
-    red.pv(pb, [&](int mt, int nn) { return vrow + mt * 16 * kVPitch + 32 * nn; }, std::false_type{});
-    __builtin_amdgcn_wave_barrier();
   };
-  // two tiles in flight
-  Tile even, odd;
-  if (n > 0) load(even, 0);
-  if (n > 1) load(odd, 1);
-  for (int i = 0; i < n; i += 2) {
-    reduce(even, i, i + 2 < n);
-    if (i + 1 < n) reduce(odd, i + 1, i + 3 < n);
+  const unsigned char* vrow = vstage + (quad * 4 + (col >> 2)) * kVPitch + ((8 * (col & 3)) ^ (16 * (quad & 1)));
+  constexpr std::integral_constant<int, 0> m0{};
+  constexpr std::integral_constant<int, 1> m1{};
+  constexpr std::false_type no{};
+
+  for (int i = 0; i < n; ++i) {
+    // S^T[16 keys x 16 heads]: codes and scales go into the product as they are
+    f32x4 sc[NT][4];
+    auto product = [&](f32x4 c, const Tile& t, auto mt, const i32x8& q, int q_scale) {
+      constexpr int M = decltype(mt)::value;
+      const i32x8 k = {(int)t.k[M][0], (int)t.k[M][1], (int)t.k[M][2], (int)t.k[M][3], 0, 0, 0, 0};
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, c, kFp4, kFp8, M, (int)t.scales, 0, q_scale);
+    };
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const Query& q = query[nt];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sc[nt][2 * h] = product(zero, tiles[h], m0, q.lo, q.lo_scale);
+        sc[nt][2 * h + 1] = product(zero, tiles[h], m1, q.lo, q.lo_scale);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sc[nt][2 * h] = product(sc[nt][2 * h], tiles[h], m0, q.hi, q.hi_scale);
+        sc[nt][2 * h + 1] = product(sc[nt][2 * h + 1], tiles[h], m1, q.hi, q.hi_scale);
+      }
+    }
+    uint32_t scales[2] = {tiles[0].scales, tiles[1].scales};
+    const int first[2] = {key_of(tile_of(i, 0)), key_of(tile_of(i, 1))};
+    const bool cut = L - first[1] < kKeysPerTile || (WIN && (wn.cuts(first[0]) || wn.cuts(first[1])));
+    if (cut) {
+      // invisible keys and those past the sequence
+      auto dead = [&](int h, int row) -> bool {
+        return (int)(first[h] + row >= L) | (int)(WIN && wn.hides(first[h], row));
+      };
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // whatever such a row holds, its values come out finite: a zero probability cancels them
+        if (dead(h, col)) scales[h] = (scales[h] & 0xff00ffffu) | 0x007f0000u;
+        if (dead(h, 16 + col)) scales[h] = (scales[h] & 0x00ffffffu) | 0x7f000000u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool d = dead(h, (e / 4) * 16 + quad * 4 + e % 4);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            sc[nt][2 * h + e / 4][e % 4] = d ? -INFINITY : sc[nt][2 * h + e / 4][e % 4];
+        }
+      }
+    }
+    stage_v(tiles[0], scales[0]);
+    const Tile second = tiles[1];
+    load_k(next, i + 1);
+    load_v(0);
+    next = place(i + 2);
+    bf16x8 pb[2][1][NT];
+    softmax_pair(red, sc, pb);
+    __builtin_amdgcn_wave_barrier();
+    red.pv(pb[0], [&](int mt, int nn) { return vrow + mt * 16 * kVPitch + 32 * nn; }, no);
+    __builtin_amdgcn_wave_barrier();
+    stage_v(second, scales[1]);
+    load_v(1);
+    __builtin_amdgcn_wave_barrier();
+    red.pv(pb[1], [&](int mt, int nn) { return vrow + mt * 16 * kVPitch + 32 * nn; }, no);
+    __builtin_amdgcn_wave_barrier();
   }
 
-  const int64_t rows = (int64_t)p.B * p.H_Q;
   const int64_t row0 = (int64_t)b * p.H_Q + head0;
   const bool direct = chunks == 1;
   red.close();
   __syncthreads();  // every wave is done with its stage
   publish_wave(red, reinterpret_cast<float*>(smem), wave, lane);
   __syncthreads();
-  finish_chunk<NT, 8, W>(p, reinterpret_cast<const float*>(smem), direct, row0,
-                         direct ? 0 : (int64_t)chunk * rows + row0, 0, wave, lane);
+  finish_chunk<NT, 8, W>(p, reinterpret_cast<const float*>(smem), direct, row0, direct ? 0 : srow0, 0, wave, lane);
   if (direct) return;
 
   // The merge inside the launch: the hand-off of split_partial_kernel
@@ -185,7 +427,7 @@ __global__ void __launch_bounds__(64 * W) kv4_kernel(Kv4Params a) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (tid == 0) {
-    uint32_t* counter = p.arrivals + (size_t)tile * da::kArrivalStride;
+    uint32_t* counter = p.arrivals + ((size_t)b * p.tiles_per_seq + ht) * da::kArrivalStride;
     const bool last =
         __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == (uint32_t)chunks;
     if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -193,32 +435,67 @@ __global__ void __launch_bounds__(64 * W) kv4_kernel(Kv4Params a) {
   }
   __syncthreads();
   if (!s_last) return;
-  merge_tile<NT, W>(p, reinterpret_cast<float*>(smem), row0, rows, chunks, row0, tid);
+  merge_tile<NT, W>(p, reinterpret_cast<float*>(smem), srow0 - chunk * cstride, cstride, chunks, row0, tid);
 }
 
 // ---------------------------------------------------------------- host side
 
+constexpr double kStreamBytes = 64 << 20;  // a quarter of the last-level cache
+
 struct Kv4Plan {
-  int heads_per_tile, tiles, chunk_tiles, chunks;
+  int heads_per_tile, tiles;
+  int chunk_tiles;  // tiles of a chunk; 0: dealt
+  int groups;       // dealt: shares of a head tile
+  int halves;
+  int grid;         // workgroups
+  int rows, heads;  // chunk states: rows x heads (0: none)
 };
 
-// num_splits <= 0: chosen.
-Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int num_splits, int cus) {
-  Kv4Plan pl;
+// num_splits <= 0: chosen.  `pool`: keys the cache holds, a bound of the batch's.
+Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int64_t pool, int num_splits, int cus) {
+  Kv4Plan pl{};
   pl.heads_per_tile = da::heads_per_tile(H_Q, H_KV, 1);
-  pl.tiles = (int)((int64_t)B * H_Q / pl.heads_per_tile);
+  const int tps = H_Q / pl.heads_per_tile;
+  pl.tiles = B * tps;
   const int T = std::max(1, (keys + kKeysPerTile - 1) / kKeysPerTile);
-  // chunk states below 2 GiB, and a counter for every tile
-  const int64_t most = std::min<int64_t>(DA_MAX_SPLITS, (((int64_t)1 << 31) - 1) / ((int64_t)B * H_Q * D * 4));
-  int s = num_splits;
-  if (s <= 0) {
-    const int64_t want = (2ll * cus + pl.tiles - 1) / pl.tiles;  // two workgroups a CU
-    s = (int)std::min<int64_t>(want, (T + 2 * W - 1) / (2 * W));  // two tiles a wave at least
+  // a counter for every tile, and chunk states below 2 GiB
+  const int64_t most = pl.tiles > da::kMaxArrivalTiles
+                           ? 1
+                           : std::max<int64_t>(1, std::min<int64_t>(DA_MAX_SPLITS, (((int64_t)1 << 31) - 1) /
+                                                                                       ((int64_t)B * H_Q * D * 4)));
+  // Lengths that differ decide the chunks on the device (dealt).  That costs
+  // about 1 us before the first load, so one sequence, and batches whose longest
+  // takes a few microseconds anyway, have chunks of a length chosen here.
+  if (num_splits <= 0 && B > 1 && T > 8 * 2 * W && most == DA_MAX_SPLITS && (int64_t)B * T <= (1 << 30)) {
+    pl.groups = std::max(1, cus / tps);
+    // the shares, and a chunk's rounding for each sequence
+    // Where lengths differ, whole and partial chunks meet on a CU, and half shares
+    // even that out if there are head tiles enough for few chunks of each: 32
+    // sequences of 1024-16384 keys (64/8 heads) 66.8 -> 63.1 us, 16 of which two
+    // have 32768 and the rest 1024 27.1 -> 22.4, 24 of 1-16000 (16/16) 90.3 -> 81.5;
+    // 32-column tiles (128/2) 23.6 -> 33.9, and equal lengths 0-19% slower.
+    pl.halves = pl.heads_per_tile <= 16 && pl.tiles >= cus / 2;
+    const int64_t chunks =
+        std::min<int64_t>((int64_t)pl.groups * (1 + pl.halves) + B, (int64_t)B * DA_MAX_SPLITS);
+    pl.grid = (int)(chunks * tps);
+    pl.rows = pl.grid;
+    pl.heads = pl.heads_per_tile;
+    if ((int64_t)pl.rows * pl.heads * D * 4 < ((int64_t)1 << 31)) return pl;
   }
-  if (pl.tiles > da::kMaxArrivalTiles) s = 1;
-  s = (int)std::max<int64_t>(1, std::min<int64_t>(s, most));
-  pl.chunk_tiles = (T + s - 1) / s;
-  pl.chunks = (T + pl.chunk_tiles - 1) / pl.chunk_tiles;
+  int64_t chunk;
+  if (num_splits > 0) {
+    chunk = (T + num_splits - 1) / num_splits;
+  } else {
+    const int64_t mean = std::min<int64_t>(T, (pool / B + kKeysPerTile - 1) / kKeysPerTile);
+    chunk = T <= 6 * W ? T : std::max<int64_t>(mean * pl.tiles / cus, 2 * W);
+  }
+  chunk = std::max<int64_t>(chunk, (T + most - 1) / most);
+  pl.chunk_tiles = 2 * (int)((std::min<int64_t>(chunk, T) + 1) / 2);  // whole pairs
+  const int chunks = (T + pl.chunk_tiles - 1) / pl.chunk_tiles;
+  pl.grid = (int)std::min<int64_t>((int64_t)pl.tiles * chunks, INT32_MAX);
+  pl.groups = 0;
+  pl.rows = chunks > 1 ? chunks * B : 0;
+  pl.heads = H_Q;
   return pl;
 }
 
@@ -230,12 +507,13 @@ int kv4_keys(int L_K_max, int window, int sinks) {
 
 extern "C" {
 
-size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int window, int sinks, int num_splits,
-                              int num_cus) {
+size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t pool_keys, int window, int sinks,
+                              int num_splits, int num_cus) {
   if (da::check_shape(B, H_Q, H_KV, L_K_max, D) || window < 0 || sinks < 0 || num_splits > DA_MAX_SPLITS) return 0;
   if (num_cus <= 0 && ensure_gfx950(&num_cus)) return 0;
-  const Kv4Plan pl = kv4_plan(B, H_Q, H_KV, kv4_keys(L_K_max, window, sinks), num_splits, num_cus);
-  return pl.chunks > 1 ? da::workspace_layout(B, H_Q, D, pl.chunks).total : 0;
+  const Kv4Plan pl = kv4_plan(B, H_Q, H_KV, kv4_keys(L_K_max, window, sinks),
+                               pool_keys > 0 ? pool_keys : 1, num_splits, num_cus);
+  return pl.rows ? da::workspace_layout(pl.rows, pl.heads, D, 1).total : 0;
 }
 
 int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* seq_lens, void* out,
@@ -260,16 +538,19 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
   if (num_splits > DA_MAX_SPLITS)
     return da::fail(DA_ERR_SPLITS, "num_splits=%d exceeds %d", num_splits, DA_MAX_SPLITS);
   if (workspace && !aligned(workspace, 16)) return da::fail(DA_ERR_ALIGN, "workspace must be 16-byte aligned");
+  const int64_t page_bytes = (int64_t)H_KV * (page_size / kKeysPerTile) * DA_KV4_TILE_BYTES;
+  if (page_bytes >= ((int64_t)1 << 32))
+    return da::fail(DA_ERR_SHAPE, "a page of %d keys of %d heads exceeds 4 GiB", page_size, H_KV);
   int cus = 0;
   rc = ensure_gfx950(&cus);
   if (rc) return rc;
   const int keys = kv4_keys(L_K_max, window, sinks);
-  const Kv4Plan pl = kv4_plan(B, H_Q, H_KV, keys, num_splits, cus);
-  if ((int64_t)pl.tiles * pl.chunks >= (1 << 24))
-    return da::fail(DA_ERR_SHAPE, "%d head tiles in %d chunks are too many workgroups", pl.tiles, pl.chunks);
+  const int64_t pool = (int64_t)num_pages * page_size;
+  const Kv4Plan pl = kv4_plan(B, H_Q, H_KV, keys, pool, num_splits, cus);
+  if (pl.grid >= (1 << 24)) return da::fail(DA_ERR_SHAPE, "%d head tiles are too many workgroups", pl.tiles);
   Kv4Params a{};
   da_plan dp{};
-  dp.num_splits = pl.chunks;
+  dp.num_splits = 1;
   dp.heads_per_tile = pl.heads_per_tile;
   dp.tiles = pl.tiles;
   fill_params(a.p, B, H_Q, H_KV, L_K_max, softmax_scale, dp);
@@ -286,12 +567,16 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
   a.cache = static_cast<const unsigned char*>(cache);
   a.chunk_tiles = pl.chunk_tiles;
   a.blocks = page_size / kKeysPerTile;
+  a.page_bytes = (uint32_t)page_bytes;
   a.div_blocks = make_div((uint32_t)a.blocks);
   a.div_tiles = make_div((uint32_t)pl.tiles);
-  if (pl.chunks > 1) {
-    const da::WorkspaceLayout wl = da::workspace_layout(B, H_Q, D, pl.chunks);
+  a.groups = pl.groups;
+  a.div_groups = make_div((uint32_t)std::max(1, pl.groups));
+  a.halves = pl.halves;
+  if (pl.rows) {
+    const da::WorkspaceLayout wl = da::workspace_layout(pl.rows, pl.heads, D, 1);
     if (!workspace || workspace_bytes < wl.total)
-      return da::fail(DA_ERR_WORKSPACE, "%d chunks need %zu workspace bytes, got %zu", pl.chunks, wl.total,
+      return da::fail(DA_ERR_WORKSPACE, "the 4-bit launch needs %zu workspace bytes, got %zu", wl.total,
                       workspace ? workspace_bytes : (size_t)0);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     a.p.o_part = reinterpret_cast<float*>(ws + wl.o_off);
@@ -299,20 +584,28 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
     a.p.l_part = reinterpret_cast<float*>(ws + wl.l_off);
     a.p.arrivals = reinterpret_cast<uint32_t*>(ws + da::arrival_offset(workspace_bytes));
   }
-  const bool ntl = (double)B * keys * H_KV * (DA_KV4_TILE_BYTES / kKeysPerTile) > (double)DA_RESIDENT_BYTES &&
-                   pl.heads_per_tile == H_Q / H_KV;
-  const void* fn;
-  int smem;
-  if (pl.heads_per_tile <= 16) {
-    fn = ntl ? reinterpret_cast<const void*>(&kv4_kernel<1, true>) : reinterpret_cast<const void*>(&kv4_kernel<1, false>);
-    smem = kv4_smem_bytes(1);
-  } else {
-    fn = ntl ? reinterpret_cast<const void*>(&kv4_kernel<2, true>) : reinterpret_cast<const void*>(&kv4_kernel<2, false>);
-    smem = kv4_smem_bytes(2);
-  }
+  // The caches of a step's layers follow each other, so one call's keys are seldom
+  // near when it reads them, and streaming loads read faster from HBM: with three
+  // caches in turn 140 MB took 32.1 us and 28.8 streamed, 286 MB 57 and 51; one
+  // cache again and again 27.5 and 27.9, 47.7 and 50.0 (up to 72 MB no difference).
+  const double bytes = (double)std::min<int64_t>((int64_t)B * keys, pool) * H_KV * (DA_KV4_TILE_BYTES / kKeysPerTile);
+  const bool ntl = bytes > kStreamBytes && pl.heads_per_tile == H_Q / H_KV;
+  auto pick = [&](auto nt, auto deal) -> const void* {
+    constexpr int N = decltype(nt)::value;
+    constexpr bool DEAL = decltype(deal)::value;
+    if (window > 0)
+      return ntl ? reinterpret_cast<const void*>(&kv4_kernel<N, true, true, DEAL>)
+                 : reinterpret_cast<const void*>(&kv4_kernel<N, false, true, DEAL>);
+    return ntl ? reinterpret_cast<const void*>(&kv4_kernel<N, true, false, DEAL>)
+               : reinterpret_cast<const void*>(&kv4_kernel<N, false, false, DEAL>);
+  };
+  auto pick_deal = [&](auto nt) { return pl.groups ? pick(nt, std::true_type{}) : pick(nt, std::false_type{}); };
+  const bool narrow = pl.heads_per_tile <= 16;
+  const void* fn = narrow ? pick_deal(std::integral_constant<int, 1>{}) : pick_deal(std::integral_constant<int, 2>{});
+  const int smem = narrow ? kv4_smem_bytes(1) : kv4_smem_bytes(2);
   void* args[] = {&a};
   const hipError_t e =
-      hipLaunchKernel(fn, dim3(pl.tiles * pl.chunks), dim3(64 * W), args, smem, static_cast<hipStream_t>(stream));
+      hipLaunchKernel(fn, dim3(pl.grid), dim3(64 * W), args, smem, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return da::fail(DA_ERR_HIP, "4-bit attention launch: %s", hipGetErrorString(e));
   return DA_OK;
 }

@@ -102,6 +102,19 @@ def test_invisible_rows_do_not_reach_the_result(fill):
         check_attention(out, lse, batch.reference(window, sinks), f"filled {fill:#x}")
 
 
+@pytest.mark.parametrize("H_Q,H_KV", [(8, 1), (128, 2), (6, 3)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2500, 40)])
+def test_mixed_batches_cut_by_their_lengths(H_Q, H_KV, window, sinks):
+    """Batches whose lengths decide the chunks on the device: empty ones first, last and between, one long, all short."""
+    for seed, lengths in enumerate([[0, 5000, 0, 33, 4097, 1, 0], [1, 31, 64], [3000] * 5, [0, 0], [9000, 9000],
+                                    list(range(0, 140, 2)) + [6000]]):
+        batch = Batch(lengths, H_Q, H_KV, "kv4", page=64, seed=seed, max_pages=150)
+        out = run(batch, f"dealt {H_Q}/{H_KV} {lengths[:7]}", window, sinks, L=9000)
+        check_attention(*out, batch.reference(window, sinks), f"dealt {lengths[:7]}")
+    again = run(batch, "dealt again", window, sinks, L=9000)
+    assert torch.equal(again[0].view(torch.int16), out[0].view(torch.int16)) and torch.equal(again[1], out[1])
+
+
 def test_a_nan_block_reaches_its_own_sequence_only():
     batch = Batch([100, 100], 4, 2, "kv4", page=32, seed=6)
     row = int(batch.rows[0][50])
