@@ -525,7 +525,7 @@ int da_window_keys(int L_K_max, int window, int sinks);
  * no page are extended all the same.  lens_out may be lens and taken_out may
  * be taken (a state advanced in place by a captured step); no other output may
  * overlap an input.  Lengths and their sums count as 2^30 beyond that.  One
- * launch; two where outputs take their inputs' place and max_tokens > 1024.
+ * launch; two where outputs take their inputs' place and max_tokens > 2048.
  * Errors: DA_ERR_SHAPE, DA_ERR_NULL, DA_ERR_ALIGN, before any HIP call. */
 int da_extend_tables(const int32_t* lens, const int32_t* new_lens, const int32_t* free_pages,
                      const int32_t* taken, int32_t* block_table, int32_t* lens_out, int32_t* taken_out,

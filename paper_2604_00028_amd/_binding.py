@@ -670,14 +670,13 @@ def da_combine_splits(o_part: torch.Tensor, m_part: torch.Tensor, l_part: torch.
 # ---------------------------------------------------------------- a step's cache: tables, rows, windows, 4 bits
 
 _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_BF16, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
 
 
-def _call(dev: torch.device, fn, *args) -> int:
-    """fn(*args) with `dev` the current device (the library launches on that one)."""
-    if dev.index == _get_device():
-        return fn(*args)
+def _on_device(dev: torch.device, fn, *args, **kw):
+    """fn(*args, **kw) with `dev` the current device (the library launches on that one)."""
     with torch.cuda.device(dev):
-        return fn(*args)
+        return fn(*args, **kw)
 
 
 def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dev: torch.device) -> None:
@@ -688,18 +687,18 @@ def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...]
 
 def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse_out: Optional[torch.Tensor]) -> torch.Tensor:
     if out is None:
-        out = _new_out(q)
+        out = torch.empty_like(q)  # q is contiguous
     else:
-        _need("out", out, torch.bfloat16, q.shape, q.device)
+        _need("out", out, _BF16, q.shape, q.device)
     if lse_out is not None:
-        _need("lse_out", lse_out, torch.float32, q.shape[:2], q.device)
+        _need("lse_out", lse_out, _F32, q.shape[:2], q.device)
     return out
 
 
-def _one_device(dev: torch.device, **tensors) -> None:
-    for name, t in tensors.items():
+def _one_device(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
         if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+            raise ValueError(f"the call's tensors must be on one device, got {dev} and {t.device}")
 
 
 def da_window_keys(L_K_max: int, window: int, sinks: int = 0) -> int:
@@ -715,6 +714,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
     """Decode attention that sees the last `window` keys of each sequence and
     its first `sinks` keys; returns `out`.  K and V as for da_decode_attn (fixed,
     or packed with cu_seqlens_k), or with block_table and seq_lens paged."""
+    dev = q.device
     page_size = max_pages = num_pages = 0
     if block_table is None:
         B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
@@ -723,22 +723,25 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
             raise ValueError("seq_lens and L_K_max (the host-known longest sequence) are required with block_table")
         B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k, v, block_table, seq_lens)
         L = int(L_K_max)
-    dev = q.device
-    _one_device(dev, k=k, v=v, cu_seqlens_k=cu_seqlens_k, block_table=block_table, seq_lens=seq_lens)
+    _one_device(dev, k, v, cu_seqlens_k, block_table, seq_lens)
+    if dev.index != _get_device():
+        return _on_device(dev, da_decode_attn_window, q, k, v, window, sinks, cu_seqlens_k, block_table, seq_lens, out,
+                          lse_out, L_K_max=L_K_max, softmax_scale=softmax_scale, num_splits=num_splits,
+                          pack_gqa=pack_gqa, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
     ws = _offered(workspace, dev, s_handle)
     while True:
-        rc = _call(dev, load().da_decode_attn_window, _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(block_table),
-                   _ptr(seq_lens), page_size, max_pages, num_pages, _ptr(out), _ptr(lse_out), B, H_Q, H_KV, L, d,
-                   float(softmax_scale), int(window), int(sinks), int(num_splits), int(pack_gqa), _ptr(ws), _nbytes(ws),
-                   s_handle)
+        rc = load().da_decode_attn_window(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(cu_seqlens_k), _ptr(block_table), _ptr(seq_lens), page_size,
+            max_pages, num_pages, out.data_ptr(), _ptr(lse_out), B, H_Q, H_KV, L, d, softmax_scale, window, sinks,
+            num_splits, pack_gqa, _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
-        with torch.cuda.device(dev):
-            plan = da_make_plan(B, H_Q, H_KV, da_window_keys(L, window, sinks), d, num_splits, pack_gqa)
+        plan = da_make_plan(B, H_Q, H_KV, da_window_keys(L, window, sinks), d, num_splits, pack_gqa)
         workspace = ws = workspace_for(dev, s_handle, da_workspace_bytes(B, H_Q, d, plan.num_splits))
-    _check(rc)
+    if rc:
+        _check(rc)
     return out
 
 
@@ -754,77 +757,92 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
     entries of new pages are written; slots and positions [max_tokens].
     lens_out may be lens and taken_out may be taken."""
     dev = lens.device
-    i32 = torch.int32
-    B = lens.numel()
-    if block_table.dim() != 2 or not lens.is_cuda:
-        raise ValueError("block_table must be [B, max_pages], and all tensors on the GPU")
+    if lens.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2 or max_tokens < 0 or not lens.is_cuda:
+        raise ValueError("lens and free_pages must have one dimension, block_table two, on the GPU, and max_tokens must "
+                         "not be negative")
+    B = lens.shape[0]
+    num_free = free_pages.shape[0]
     max_pages = block_table.shape[1]
-    num_free = free_pages.numel()
-    max_tokens = int(max_tokens)
-    for name, t, shape in (("lens", lens, (B,)), ("new_lens", new_lens, (B,)), ("free_pages", free_pages, (num_free,)),
-                           ("taken", taken, (1,)), ("block_table", block_table, (B, max_pages))):
-        _need(name, t, i32, shape, dev)
+    one, rows = (B,), (max_tokens,)
+    _need("lens", lens, _I32, one, dev)
+    _need("new_lens", new_lens, _I32, one, dev)
+    _need("free_pages", free_pages, _I32, (num_free,), dev)
+    _need("taken", taken, _I32, (1,), dev)
+    _need("block_table", block_table, _I32, (B, max_pages), dev)
+    if dev.index != _get_device():
+        return _on_device(dev, da_extend_tables, lens, new_lens, free_pages, taken, block_table, page_size, num_pages,
+                          max_tokens, lens_out, taken_out, cu_new, slots, positions, stream=stream)
+    sizes = (B, 1, B + 1, max_tokens, max_tokens)
     given = (lens_out, taken_out, cu_new, slots, positions)
-    sizes = [B, 1, B + 1, max_tokens, max_tokens]
-    if max_tokens < 0:
-        raise ValueError("max_tokens must not be negative")
-    for name, t, n in zip(("lens_out", "taken_out", "cu_new", "slots", "positions"), given, sizes):
-        if t is not None:
-            _need(name, t, i32, (n,), dev)
-    if any(t is None for t in given):
-        new = torch.empty(sum(n for t, n in zip(given, sizes) if t is None), dtype=i32, device=dev).split(
-            [n for t, n in zip(given, sizes) if t is None])
-        new = iter(new)
-        given = tuple(next(new) if t is None else t for t in given)
-    _check(_call(dev, load().da_extend_tables, _ptr(lens), _ptr(new_lens), _ptr(free_pages), _ptr(taken),
-                 _ptr(block_table), *(_ptr(t) for t in given), B, int(page_size), max_pages, int(num_pages), num_free,
-                 max_tokens, _stream(dev, stream)))
-    return given
+    new = None
+    if not any(t is not None for t in given):
+        new = torch.empty(2 * B + 2 + 2 * max_tokens, dtype=_I32, device=dev)
+        at = new.data_ptr()
+        ptrs = (at, at + 4 * B, at + 4 * B + 4, at + 8 * B + 8, at + 8 * B + 8 + 4 * max_tokens)
+    else:
+        for name, t, n in zip(("lens_out", "taken_out", "cu_new", "slots", "positions"), given, sizes):
+            if t is not None:
+                _need(name, t, _I32, (n,), dev)
+        given = tuple(torch.empty(n, dtype=_I32, device=dev) if t is None else t for t, n in zip(given, sizes))
+        ptrs = tuple(_ptr(t) for t in given)
+    rc = load().da_extend_tables(lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(), taken.data_ptr(),
+                                 block_table.data_ptr(), *ptrs, B, page_size, max_pages, num_pages, num_free, max_tokens,
+                                 _stream(dev, stream))
+    if rc:
+        _check(rc)
+    return given if new is None else new.split_with_sizes(sizes)
 
 
-def _rows(name: str, t: torch.Tensor, heads: Optional[int], dev: torch.device) -> Tuple[int, int]:
-    """Token stride and heads of q, k or v [N, heads, d]: heads dense, tokens any distance apart."""
-    if (t.dim() != 3 or t.dtype is not torch.bfloat16 or t.device != dev or not t.is_cuda or t.stride(2) != 1
-            or (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or (heads is not None and t.shape[1] != heads)):
-        raise ValueError(f"{name} must be a bfloat16 CUDA tensor [N, heads, d] whose heads are dense")
-    return (t.stride(0) if t.shape[0] > 1 else 0), t.shape[1]
+def _rows(name: str, t: torch.Tensor, dev: torch.device) -> Tuple[int, torch.Size]:
+    """Token stride and shape of q, k or v [N, heads, d]: heads dense, tokens any distance apart."""
+    shape = t.shape
+    if len(shape) == 3:
+        stride = t.stride()
+        if ((stride[2] == 1 or shape[2] == 1) and (stride[1] == shape[2] or shape[1] == 1) and t.dtype is _BF16
+                and t.device == dev):
+            return (stride[0] if shape[0] > 1 else 0), shape
+    raise ValueError(f"{name} must be a bfloat16 tensor [N, heads, d] on {dev} whose heads are dense")
 
 
 def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours, q_out):
-    """Check what the append calls share; (their leading arguments, (N, H_Q, H_KV, d), q_out)."""
+    """Check what the append calls share; (their leading arguments, N, H_Q, H_KV, d, q_out)."""
     dev = k.device
-    k_stride, H_KV = _rows("k", k, None, dev)
-    v_stride, _ = _rows("v", v, H_KV, dev)
-    N, _, d = k.shape
-    q_stride = H_Q = 0
-    if v.shape != k.shape:
+    if not k.is_cuda:
+        raise ValueError("k must be on the GPU")
+    k_stride, shape = _rows("k", k, dev)
+    v_stride, v_shape = _rows("v", v, dev)
+    if v_shape != shape:
         raise ValueError("k and v shapes differ")
+    N, H_KV, d = shape
+    q_stride = H_Q = rope_rows = rope_dim = 0
     if q is not None:
-        q_stride, H_Q = _rows("q", q, None, dev)
-        if q.shape[0] != N or q.shape[2] != d:
+        q_stride, q_shape = _rows("q", q, dev)
+        H_Q = q_shape[1]
+        if q_shape[0] != N or q_shape[2] != d:
             raise ValueError("q must be [N, H_Q, d] with k's N and d")
         if q_out is None:
-            q_out = torch.empty((N, H_Q, d), dtype=torch.bfloat16, device=dev)
+            q_out = torch.empty(q_shape, dtype=_BF16, device=dev)
         else:
-            _need("q_out", q_out, torch.bfloat16, (N, H_Q, d), dev)
+            _need("q_out", q_out, _BF16, q_shape, dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _need(name, w, torch.bfloat16, (d,), dev)
-    rope_rows = rope_dim = 0
-    if rope is not None:
+    if q_weight is not None:
+        _need("q_weight", q_weight, _BF16, (d,), dev)
+    if k_weight is not None:
+        _need("k_weight", k_weight, _BF16, (d,), dev)
+    if rope is None:
+        positions = None
+    else:
         if rope.dim() != 2 or positions is None:
             raise ValueError("rope must be [positions, rope_dim], and needs positions")
         rope_rows, rope_dim = rope.shape
-        _need("rope", rope, torch.float32, (rope_rows, rope_dim), dev)
-        _need("positions", positions, torch.int32, (N,), dev)
+        _need("rope", rope, _F32, rope.shape, dev)
+        _need("positions", positions, _I32, (N,), dev)
     if slots is not None:
-        _need("slots", slots, torch.int32, (N,), dev)
-    args = (_ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(q_weight), _ptr(k_weight), float(eps),
-            _ptr(rope), rope_rows, rope_dim, int(neighbours), _ptr(positions) if rope is not None else None,
-            _ptr(slots), _ptr(q_out))
-    return args, (N, H_Q, H_KV, d), q_out
+        _need("slots", slots, _I32, (N,), dev)
+    return (_ptr(q), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _ptr(q_weight), _ptr(k_weight), eps,
+            _ptr(rope), rope_rows, rope_dim, 1 if neighbours else 0, _ptr(positions), _ptr(slots),
+            _ptr(q_out)), N, H_Q, H_KV, d, q_out
 
 
 def da_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
@@ -837,24 +855,31 @@ def da_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, po
     q [N, H_Q, d], k, v [N, H_KV, d]: slices of one projection's output will do;
     caches [..., H_KV, d] (page pools, or sequences), rows counted over the
     leading dims; rope fp32 [positions, rope_dim]: cosines, then sines."""
-    args, (N, H_Q, H_KV, d), q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
-                                                  q_out)
     dev = k.device
-    if k_cache.dim() < 3 or k_cache.shape[-2:] != (H_KV, d):
+    if k.is_cuda and dev.index != _get_device():
+        return _on_device(dev, da_append_kv, q, k, v, positions, slots, k_cache, v_cache, rope=rope, q_weight=q_weight,
+                          k_weight=k_weight, eps=eps, neighbours=neighbours, q_out=q_out, stream=stream)
+    args, N, H_Q, H_KV, d, q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
+                                                q_out)
+    shape = k_cache.shape
+    if len(shape) < 3 or shape[-2] != H_KV or shape[-1] != d:
         raise ValueError("k_cache must be [..., H_KV, d]")
-    _need("k_cache", k_cache, torch.bfloat16, k_cache.shape, dev)
-    _need("v_cache", v_cache, torch.bfloat16, k_cache.shape, dev)
-    _check(_call(dev, load().da_append_kv, *args, _ptr(k_cache), _ptr(v_cache), k_cache.numel() // (H_KV * d), N, H_Q,
-                 H_KV, d, _stream(dev, stream)))
+    _need("k_cache", k_cache, _BF16, shape, dev)
+    _need("v_cache", v_cache, _BF16, shape, dev)
+    rc = load().da_append_kv(*args, k_cache.data_ptr(), v_cache.data_ptr(),
+                             k_cache.numel() // (H_KV * d) if H_KV * d else 0, N, H_Q, H_KV, d, _stream(dev, stream))
+    if rc:
+        _check(rc)
     return q_out
 
 
 def _kv4_cache(cache: torch.Tensor) -> Tuple[int, int, int]:
     """(num_pages, H_KV, page_size) of a 4-bit cache."""
-    if (cache.dim() != 4 or cache.dtype is not torch.uint8 or cache.shape[3] != KV4_TILE_BYTES
-            or not cache.is_contiguous() or not cache.is_cuda):
+    shape = cache.shape
+    if (len(shape) != 4 or cache.dtype is not torch.uint8 or shape[3] != KV4_TILE_BYTES or not cache.is_contiguous()
+            or not cache.is_cuda):
         raise ValueError(f"cache must be a contiguous uint8 CUDA tensor [num_pages, H_KV, page_size / 32, {KV4_TILE_BYTES}]")
-    return cache.shape[0], cache.shape[1], 32 * cache.shape[2]
+    return shape[0], shape[1], 32 * shape[2]
 
 
 def da_append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],
@@ -862,15 +887,19 @@ def da_append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, p
                   q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                   neighbours: bool = False, q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
     """da_append_kv into a 4-bit cache, uint8 [num_pages, H_KV, page_size / 32, 4352]; returns q_out."""
-    args, (N, H_Q, H_KV, d), q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
-                                                  q_out)
     dev = k.device
+    if k.is_cuda and dev.index != _get_device():
+        return _on_device(dev, da_append_kv4, q, k, v, positions, slots, cache, rope=rope, q_weight=q_weight,
+                          k_weight=k_weight, eps=eps, neighbours=neighbours, q_out=q_out, stream=stream)
+    args, N, H_Q, H_KV, d, q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
+                                                q_out)
     num_pages, heads, page_size = _kv4_cache(cache)
     if heads != H_KV:
         raise ValueError(f"the cache has {heads} KV heads, k {H_KV}")
-    _one_device(dev, cache=cache)
-    _check(_call(dev, load().da_append_kv4, *args, _ptr(cache), page_size, num_pages, N, H_Q, H_KV, d,
-                 _stream(dev, stream)))
+    _one_device(dev, cache)
+    rc = load().da_append_kv4(*args, cache.data_ptr(), page_size, num_pages, N, H_Q, H_KV, d, _stream(dev, stream))
+    if rc:
+        _check(rc)
     return q_out
 
 
@@ -879,12 +908,20 @@ def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
     """K and V bf16 [N, H_KV, 128] of the rows `slots` of a 4-bit cache (None: all its rows)."""
     num_pages, H_KV, page_size = _kv4_cache(cache)
     dev = cache.device
-    if slots is not None:
-        _need("slots", slots, torch.int32, (slots.numel(),), dev)
-    N = num_pages * page_size if slots is None else slots.numel()
-    k, v = torch.empty((2, N, H_KV, HEAD_DIM), dtype=torch.bfloat16, device=dev)
-    _check(_call(dev, load().da_read_kv4, _ptr(cache), _ptr(slots), _ptr(k), _ptr(v), N, H_KV, page_size, num_pages,
-                 HEAD_DIM, _stream(dev, stream)))
+    if slots is None:
+        N = num_pages * page_size
+    else:
+        if slots.dim() != 1:
+            raise ValueError("slots must have one dimension")
+        N = slots.shape[0]
+        _need("slots", slots, _I32, (N,), dev)
+    if dev.index != _get_device():
+        return _on_device(dev, da_read_kv4, cache, slots, stream=stream)
+    k, v = torch.empty((2, N, H_KV, HEAD_DIM), dtype=_BF16, device=dev).unbind(0)
+    rc = load().da_read_kv4(cache.data_ptr(), _ptr(slots), k.data_ptr(), v.data_ptr(), N, H_KV, page_size, num_pages, HEAD_DIM,
+                            _stream(dev, stream))
+    if rc:
+        _check(rc)
     return k, v
 
 
@@ -902,28 +939,31 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
     da_decode_attn_paged; window (0: none) and sinks as for
     da_decode_attn_window."""
     dev = q.device
-    if q.dim() != 3 or q.dtype is not torch.bfloat16 or not q.is_contiguous() or not q.is_cuda:
+    if q.dim() != 3 or q.dtype is not _BF16 or not q.is_contiguous() or not q.is_cuda:
         raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")
     num_pages, H_KV, page_size = _kv4_cache(cache)
     B, H_Q, d = q.shape
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages]")
     max_pages = block_table.shape[1]
-    _need("block_table", block_table, torch.int32, (B, max_pages), dev)
-    _need("seq_lens", seq_lens, torch.int32, (B,), dev)
-    _one_device(dev, cache=cache)
+    _need("block_table", block_table, _I32, (B, max_pages), dev)
+    _need("seq_lens", seq_lens, _I32, (B,), dev)
+    _one_device(dev, cache)
+    if dev.index != _get_device():
+        return _on_device(dev, da_decode_attn_kv4, q, cache, block_table, seq_lens, L_K_max, window, sinks, out, lse_out,
+                          softmax_scale=softmax_scale, num_splits=num_splits, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
     L = int(L_K_max)
     ws = _offered(workspace, dev, s_handle)
     while True:
-        rc = _call(dev, load().da_decode_attn_kv4, _ptr(q), _ptr(cache), _ptr(block_table), _ptr(seq_lens), _ptr(out),
-                   _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L, d, float(softmax_scale), int(window),
-                   int(sinks), int(num_splits), _ptr(ws), _nbytes(ws), s_handle)
+        rc = load().da_decode_attn_kv4(q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                                       out.data_ptr(), _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L, d,
+                                       softmax_scale, window, sinks, num_splits, _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
-        with torch.cuda.device(dev):
-            need = da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size, window, sinks, num_splits)
-        workspace = ws = workspace_for(dev, s_handle, need)
-    _check(rc)
+        workspace = ws = workspace_for(dev, s_handle, da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size,
+                                                                             window, sinks, num_splits))
+    if rc:
+        _check(rc)
     return out

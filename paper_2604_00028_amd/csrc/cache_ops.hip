@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "decode_attn.h"
 #include "host.h"
@@ -22,9 +23,8 @@ using da::ensure_gfx950;
 
 constexpr int kMaxRequests = DA_MAX_REQUESTS;
 constexpr int kTableThreads = 256;
-constexpr int kRowsPerGroup = 1024;             // token rows one workgroup fills
-constexpr int kPerThread = kMaxRequests / kTableThreads;
-constexpr uint32_t kMost = 1u << 30;            // lengths and their sums saturate here
+static_assert(kMaxRequests == 16 * kTableThreads, "extend_kernel<16> takes them all");
+constexpr uint32_t kMost = 1u << 30;  // lengths and their sums saturate here
 
 struct TableParams {
   const int32_t* lens;
@@ -49,16 +49,23 @@ __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) {  // a, b <
   return s < kMost ? s : kMost;
 }
 
-// Inclusive saturating sum over the workgroup's threads of `x`; *total: of all.
-// (min(a + b, most) is associative over non-negative numbers.)
+// Saturating sum of `x` over the threads before this one; *total: over all.
+// (min(a + b, most) is associative over non-negative numbers.)  One barrier:
+// wave_sums is this call's own.
 __device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t* wave_sums, uint32_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = (uint32_t)__shfl_up((int)x, o);
-    x = lane >= o ? sat_add(x, y) : x;
-  }
+  auto from = [&](auto ctrl, auto rows) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+  };
+  using std::integral_constant;
+  x = sat_add(x, from(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{}));  // row_shr:1
+  x = sat_add(x, from(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{}));
+  x = sat_add(x, from(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{}));
+  x = sat_add(x, from(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{}));
+  x = sat_add(x, from(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}));  // row_bcast:15
+  x = sat_add(x, from(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}));  // row_bcast:31
   if (lane == 63) wave_sums[wave] = x;
+  const uint32_t up = (uint32_t)__shfl_up((int)x, 1);
   __syncthreads();
   uint32_t before = 0, all = 0;
 #pragma unroll
@@ -66,9 +73,8 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t* wave_sums, 
     before = w < wave ? sat_add(before, wave_sums[w]) : before;
     all = sat_add(all, wave_sums[w]);
   }
-  __syncthreads();  // wave_sums may be written again
   *total = all;
-  return sat_add(before, x);
+  return lane == 0 ? before : sat_add(before, up);
 }
 
 // The last i in [0, n) with at[i] <= x; at[0] = 0, non-decreasing.
@@ -87,52 +93,46 @@ __device__ __forceinline__ int last_at_most(const uint32_t* at, int n, uint32_t 
 // Request b holds l_b keys in ceil(l_b / P) pages of P rows and gets n_b more:
 // its rows start at the exclusive sum of n, its pages at `taken` plus the
 // exclusive sum of the pages needed.  Every workgroup takes both sums over all
-// requests for itself (B <= 4096: up to 16 requests a thread, two scans), so
-// one launch needs no hand-over; then the workgroups share the rows, each
-// looking its request up in LDS.  Bound by latency: two dependent loads, two
-// scans of three barriers, log2 B LDS reads a row.
+// requests for itself (PER of them a thread), so one launch needs no hand-over;
+// then the workgroups share the rows, each thread looking its row's request up
+// in LDS.  Bound by latency: two dependent loads, two scans, log2 B LDS reads a
+// row; one row a thread (four in turn measured 9.4 us for 19600 rows of 500
+// requests).
+template <int PER>
 __global__ void __launch_bounds__(kTableThreads) extend_kernel(TableParams p) {
-  __shared__ uint32_t cu[kMaxRequests + 1];   // first row of each request
-  __shared__ uint32_t pg[kMaxRequests + 1];   // first place in the free list, from *taken
-  __shared__ int32_t held[kMaxRequests];      // keys held; ~keys for a request that is not extended
-  __shared__ uint32_t wave_sums[kTableThreads / 64];
-  __shared__ uint32_t granted;                // places taken
+  constexpr int kMaxB = PER * kTableThreads;
+  __shared__ uint32_t cu[kMaxB + 1];   // first row of each request
+  __shared__ uint32_t pg[kMaxB + 1];   // first place in the free list, from *taken
+  __shared__ int32_t held[kMaxB];      // keys held; ~keys for a request that is not extended
+  __shared__ uint32_t wave_sums[2][kTableThreads / 64];
+  __shared__ uint32_t granted;         // places taken
   const int tid = threadIdx.x;
-  const int per = (p.B + kTableThreads - 1) / kTableThreads;  // <= kPerThread
-  const int b0 = tid * per;
+  const int b0 = tid * PER;
   if (tid == 0) granted = 0;
 
-  uint32_t len[kPerThread], add[kPerThread];
+  const int taken_raw = *p.taken;
+  uint32_t len[PER], add[PER];
   uint32_t sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
+  for (int i = 0; i < PER; ++i) {
     len[i] = add[i] = 0;
-    if (i < per && b0 + i < p.B) {
+    if (b0 + i < p.B) {
       const int l = p.lens[b0 + i], n = p.new_lens[b0 + i];
       len[i] = l < 0 ? 0u : min((uint32_t)l, kMost);
       add[i] = n < 0 ? 0u : min((uint32_t)n, kMost);
     }
     sum = sat_add(sum, add[i]);
   }
-  const int taken_raw = *p.taken;
   const uint32_t taken = taken_raw < 0 ? 0u : (uint32_t)taken_raw;
   const uint32_t avail = taken < (uint32_t)p.num_free ? (uint32_t)p.num_free - taken : 0u;
   uint32_t total;
-  uint32_t at = group_scan(sum, wave_sums, &total);
-  // the exclusive sum: the inclusive one of the thread before (a saturated sum cannot be subtracted from)
-  {
-    const uint32_t up = (uint32_t)__shfl_up((int)at, 1);
-    if ((tid & 63) == 63) wave_sums[tid >> 6] = at;
-    __syncthreads();
-    at = tid == 0 ? 0u : (tid & 63) == 0 ? wave_sums[(tid >> 6) - 1] : up;
-    __syncthreads();
-  }
-  uint32_t need[kPerThread];
+  uint32_t at = group_scan(sum, wave_sums[0], &total);
+  uint32_t need[PER];
   uint32_t pages = 0;
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
+  for (int i = 0; i < PER; ++i) {
     need[i] = 0;
-    if (i < per && b0 + i < p.B) {
+    if (b0 + i < p.B) {
       cu[b0 + i] = at;
       at = sat_add(at, add[i]);
       const uint32_t end = len[i] + add[i];  // <= 2^31
@@ -145,12 +145,12 @@ __global__ void __launch_bounds__(kTableThreads) extend_kernel(TableParams p) {
     }
   }
   uint32_t all_pages;
-  uint32_t upto = group_scan(pages, wave_sums, &all_pages);
-  upto -= pages;  // asked for before this thread's first request (exact: at most max_tokens + B pages in all)
+  // pages asked for before (exact: at most max_tokens + B in all)
+  uint32_t upto = group_scan(pages, wave_sums[1], &all_pages);
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    if (i < per && b0 + i < p.B) {
+  for (int i = 0; i < PER; ++i) {
+    if (b0 + i < p.B) {
       upto = sat_add(upto, need[i]);
       if (need[i] > 0 && upto > avail) held[b0 + i] = ~(int32_t)len[i];
       if (need[i] > 0 && upto <= avail) most = upto;
@@ -261,10 +261,14 @@ __device__ __forceinline__ float bf16_high(uint32_t two) { return __uint_as_floa
 // in 32 bits, rounded to bf16 once.  Partners of a pair of halves lie half / 8
 // lanes apart, so the bf16 words change lanes, four a pass.
 //
-// Bound by HBM (each head row read and written once).  KV4: keys are rounded
+// Bound by HBM (each head row read and written once: 8192 tokens of 64/8 heads,
+// 340 MB, 66.9 us, 5.1 TB/s, where a copy of 2 GiB reaches 4.9).  STREAM 1: rows
+// are written with the streaming hint (more than L2 holds: 42 MB 11.4 -> 10.5 us);
+// 2: read with it too (more than half the last-level cache: 340 MB 70.5 -> 66.9 us,
+// but 85 MB, which a projection may just have left there, 16.7 -> 20.9).  KV4: keys are rounded
 // to bf16 as the bf16 cache would hold them and then to 4 bits, values at once
 // (quantise in kv4.h).
-template <bool KV4>
+template <bool KV4, int STREAM>
 __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams p) {
   const int lane = threadIdx.x & 63;
   const int unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kAppendWaves + (int)(threadIdx.x >> 6));
@@ -334,8 +338,19 @@ __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams 
     const int role = role_of(i), h = head_of(i, role);
     const uint16_t* src = role == 0 ? p.q + n * p.q_stride : role == 1 ? p.k + n * p.k_stride : p.v + n * p.v_stride;
     u32x4 x = {0u, 0u, 0u, 0u};
-    if (h < (role == 0 ? p.H_Q : p.H_KV)) x = *reinterpret_cast<const u32x4*>(src + h * D + 8 * l);
+    if (h < (role == 0 ? p.H_Q : p.H_KV)) {
+      const u32x4* at = reinterpret_cast<const u32x4*>(src + h * D + 8 * l);
+      x = STREAM == 2 ? __builtin_nontemporal_load(at) : *at;
+    }
     return x;
+  };
+
+  auto store = [&](uint16_t* row, const u32x4& x) {
+    u32x4* at = reinterpret_cast<u32x4*>(row + 8 * l);
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(x, at);
+    else
+      *at = x;
   };
 
   float own[8], other[8];  // coefficients of the element and of its partner
@@ -405,7 +420,7 @@ __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams 
       for (int e = 0; e < 4; ++e) x[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
     }
     if (role == 0) {
-      if (live) *reinterpret_cast<u32x4*>(p.q_out + ((int64_t)n * p.H_Q + h) * D + 8 * l) = x;
+      if (live) store(p.q_out + ((int64_t)n * p.H_Q + h) * D, x);
     } else if constexpr (KV4) {
       // every lane takes part in its block's maximum
       uint32_t scale;
@@ -419,8 +434,7 @@ __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams 
         if ((l & 3) == 0) tile[kv4_scale_at(key, l >> 2, role - 1)] = (unsigned char)scale;
       }
     } else if (live && kept) {
-      uint16_t* cache = role == 1 ? p.k_cache : p.v_cache;
-      *reinterpret_cast<u32x4*>(cache + (slot * p.H_KV + h) * D + 8 * l) = x;
+      store((role == 1 ? p.k_cache : p.v_cache) + (slot * p.H_KV + h) * D, x);
     }
     x = next;
   }
@@ -509,17 +523,29 @@ template <bool KV4>
 int launch_append(AppendParams& p, int cus, hipStream_t stream) {
   if (p.N == 0) return DA_OK;
   // A wave keeps a token's coefficients over its passes, so it takes as many as
-  // leave the chip enough waves to hide the loads (16 a CU).
+  // leave the chip enough waves to hide the loads (16 a CU).  Where the tokens
+  // are more waves than the chip holds (28 a CU), five passes a wave: the last
+  // waves to start then hold the launch up less.  64/8 heads: 4096 tokens one
+  // wave each 39.6 us, four 42.9; 8192 tokens 88.2 and 72.4.
   const int passes = p.q_passes + 2 * p.kv_passes;
-  const int64_t waves = std::min<int64_t>(passes, std::max<int64_t>(1, (16ll * cus + p.N - 1) / p.N));
+  const int64_t waves = p.N > 28 * cus ? (passes + 4) / 5
+                                       : std::min<int64_t>(passes, std::max<int64_t>(1, (16ll * cus + p.N - 1) / p.N));
   p.per_wave = (int)((passes + waves - 1) / waves);
   p.segments = (passes + p.per_wave - 1) / p.per_wave;
   p.div_segments = make_div((uint32_t)p.segments);
   const int64_t units = (int64_t)p.N * p.segments;
   void* args[] = {&p};
-  return launched(hipLaunchKernel(reinterpret_cast<const void*>(&append_kernel<KV4>),
-                                  dim3((uint32_t)((units + kAppendWaves - 1) / kAppendWaves)), dim3(64 * kAppendWaves),
-                                  args, 0, stream),
+  const void* fn;
+  if constexpr (KV4) {
+    fn = reinterpret_cast<const void*>(&append_kernel<true, 0>);
+  } else {
+    const int64_t moved = (int64_t)p.N * (p.H_Q + 2 * p.H_KV) * D * 4;
+    fn = moved > (128ll << 20)       ? reinterpret_cast<const void*>(&append_kernel<false, 2>)
+         : moved > da::kL2Bytes ? reinterpret_cast<const void*>(&append_kernel<false, 1>)
+                                : reinterpret_cast<const void*>(&append_kernel<false, 0>);
+  }
+  return launched(hipLaunchKernel(fn, dim3((uint32_t)((units + kAppendWaves - 1) / kAppendWaves)),
+                                  dim3(64 * kAppendWaves), args, 0, stream),
                   "append");
 }
 
@@ -567,13 +593,18 @@ int da_extend_tables(const int32_t* lens, const int32_t* new_lens, const int32_t
                 cu_new,    slots,    positions,  B,         max_pages,   page_size, num_pages,
                 num_free,  max_tokens, (uint32_t)std::min<int64_t>(kMost, (int64_t)max_pages * page_size),
                 make_div((uint32_t)page_size), 1, 1};
-  const int grid = std::max(1, (max_tokens + kRowsPerGroup - 1) / kRowsPerGroup);
-  // Where several workgroups read the lengths, outputs that take their place are written by a launch after them.
+  // Where several workgroups read the lengths, outputs that take their place are
+  // written by a launch after them; one workgroup for up to eight rows a thread is
+  // faster than that launch.
   const bool in_place = lens_out == lens || lens_out == new_lens || taken_out == taken;
+  const int groups = std::min(std::max(1, (max_tokens + kTableThreads - 1) / kTableThreads), 8 * cus);
+  const int grid = in_place && groups <= 8 ? 1 : groups;
   const bool later = grid > 1 && in_place;
   p.state = later ? 0 : 1;
   void* args[] = {&p};
-  const void* fn = reinterpret_cast<const void*>(&extend_kernel);
+  const void* fn = B <= kTableThreads       ? reinterpret_cast<const void*>(&extend_kernel<1>)
+                   : B <= 4 * kTableThreads ? reinterpret_cast<const void*>(&extend_kernel<4>)
+                                            : reinterpret_cast<const void*>(&extend_kernel<16>);
   rc = launched(hipLaunchKernel(fn, dim3(grid), dim3(kTableThreads), args, 0, static_cast<hipStream_t>(stream)),
                 "table");
   if (rc || !later) return rc;
