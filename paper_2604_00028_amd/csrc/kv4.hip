@@ -36,7 +36,8 @@ struct Kv4Params {
 constexpr int kv4_smem_bytes(int NT) {
   return W * kKeysPerTile * kVPitch > W * merge_slot_bytes(NT) ? W * kKeysPerTile * kVPitch : W * merge_slot_bytes(NT);
 }
-static_assert(kv4_smem_bytes(1) >= (2 * (DA_MAX_SPLITS + 16) * 32 + 8 * 32) * 4, "the merge stages chunk maxima and sums");
+static_assert(kv4_smem_bytes(1) >= (2 * (DA_MAX_SPLITS + 16) * 32 + 8 * 32) * 4,
+              "the merge stages chunk maxima and sums in LDS");
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -117,12 +118,34 @@ __device__ __forceinline__ void softmax_pair(TileReducer<NT, 8>& red, f32x4 (&sc
     for (int h = 0; h < 2; ++h) {
       u32x4 pk;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pk[i] = pack_bf16x2(sc[nt][2 * h + i / 2][2 * (i % 2)], sc[nt][2 * h + i / 2][2 * (i % 2) + 1]);
+      for (int i = 0; i < 4; ++i) {
+        const f32x4& x = sc[nt][2 * h + i / 2];
+        pk[i] = pack_bf16x2(x[2 * (i % 2)], x[2 * (i % 2) + 1]);
+      }
       pb[h][0][nt] = as_bf16x8(pk);
     }
   }
 }
 
+// One workgroup: a head tile (the query heads of one KV head, up to 16 NT of
+// them) of a sequence, and a chunk of its 32-key tiles.  A pair of tiles (64
+// keys) is a wave's step, W pairs side by side.
+//   * S^T[key, head] = K . Q^T on v_mfma_scale_f32_16x16x128_f8f6f4, whose first
+//     operand is the cache as it lies there: lane (key, block of 32 dims) gives 16
+//     bytes of e2m1 codes and one scale byte.  The query is the other operand, in
+//     two 8-bit parts (Query): two products for 16 keys, and no instruction that
+//     unpacks K.  (The step from K unpacked to bf16, with the waits for the loads
+//     put in order at the same time: 74 -> 55 us for 32 sequences of 8192 keys,
+//     64/8 heads, one workgroup a CU.)
+//   * V has its scales per key, the index that the second product sums over, so
+//     it is unpacked, 64 conversions a pair that are exact in bf16, and goes
+//     through the transposing LDS reads of TileReducer::pv.
+//   * One softmax for the pair: half the row reductions, rescalings and branches
+//     (the same work resident in L2: 36 -> 33 us).
+// Bound by HBM over long batches: 32 sequences of 8192 keys, 64/8 heads (286 MB)
+// 45-52 us by the run, 43 from the first workgroup's start to the last one's end,
+// 6.6 TB/s; resident in L2 the same work takes 33 us at three workgroups a CU.
+// Bound by latency where a wave has few pairs (1.1 us each alone).
 template <int NT, bool NTL, bool WIN, bool DEAL>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2, 8)))
 kv4_kernel(Kv4Params a) {
@@ -139,11 +162,15 @@ kv4_kernel(Kv4Params a) {
   int64_t srow0, cstride;  // state row of its first head; rows between two chunks of a head
   Window wn{};
   if constexpr (DEAL) {
-    // The lengths decide: chunks of an even share of the batch's tiles for each
-    // of a.groups places a head tile, or half of one (at least a pair of tiles a wave, at most
-    // 64 chunks a sequence; three pairs a wave are as fast as a merge).  Sequences
-    // have as many workgroups as chunks, so none is launched for nothing but the
-    // few by which the chunks' roundings miss their bound.
+    // The lengths decide: chunks of an even share of the batch's tiles for each of
+    // a.groups places a head tile, or half of one (at least a pair of tiles a wave,
+    // at most 64 chunks a sequence; three pairs a wave are as fast as a merge).
+    // Sequences have as many workgroups as chunks, so none is launched for nothing
+    // but those by which the chunks' roundings stay below their bound.  (One split
+    // count for all: 128 MQA sequences of 16-32768 keys 29 us at the best count,
+    // 20 so.  Runs of equal length over sequence ends, as dealt_kernel gives its
+    // workgroups, balance the CUs better and pay for the ends: over 250 MB 4-12%
+    // faster, below it up to 45% slower.)
     int len = 0, tl = 0, win = 0;  // lane i: sequence win + i
     auto window = [&](int b0) {
       win = b0;
@@ -175,6 +202,13 @@ kv4_kernel(Kv4Params a) {
       q -= q * per > x ? 1 : 0;
       return win + lane < p.B ? max(q, 1) : 0;
     };
+    // Items: a sequence's chunks, the head tiles of each next to one another.
+    // Workgroup i starts on XCD i % 8, and patterns in the lengths (two chunks
+    // each, one whole and one short) could give some XCDs all the long ones (80
+    // sequences of 1-8192 keys, chunks of a head tile next to one another: twice
+    // the tiles on every other XCD), so each eight items are given out one place
+    // further on.
+    const int item = (int)((blockIdx.x & ~7u) + ((blockIdx.x + (blockIdx.x >> 3)) & 7u));
     b = -1;
     int first = 0;
     L = 0;
@@ -182,7 +216,7 @@ kv4_kernel(Kv4Params a) {
       if (p.B > 64) window(b0);
       const int c = lane_chunks();
       const int incl = wave_scan(c);
-      const uint64_t past = __ballot((before + incl) * p.tiles_per_seq > (int)blockIdx.x);
+      const uint64_t past = __ballot((before + incl) * p.tiles_per_seq > item);
       if (past) {
         const int i = __ffsll((unsigned long long)past) - 1;
         b = b0 + i;
@@ -194,11 +228,10 @@ kv4_kernel(Kv4Params a) {
       before += __builtin_amdgcn_readlane(incl, 63);
     }
     if (b < 0) return;  // fewer chunks than the bound: the whole workgroup
-    const uint32_t at = blockIdx.x - (uint32_t)first;
-    ht = (int)(at / (uint32_t)chunks);
-    chunk = (int)at - ht * chunks;
-    srow0 = (int64_t)blockIdx.x * p.hpt;
-    cstride = p.hpt;
+    chunk = div_by(item - first, p.div_tps);
+    ht = item - first - chunk * p.tiles_per_seq;
+    srow0 = (int64_t)item * p.hpt;
+    cstride = (int64_t)p.tiles_per_seq * p.hpt;
     if constexpr (WIN) wn = window_of(L, p.window, p.sinks);
   } else {
     // all first chunks, then all second ones, ...
@@ -477,7 +510,7 @@ Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int64_t pool, int num_split
     pl.halves = pl.heads_per_tile <= 16 && pl.tiles >= cus / 2;
     const int64_t chunks =
         std::min<int64_t>((int64_t)pl.groups * (1 + pl.halves) + B, (int64_t)B * DA_MAX_SPLITS);
-    pl.grid = (int)(chunks * tps);
+    pl.grid = (int)((chunks * tps + 7) / 8 * 8);
     pl.rows = pl.grid;
     pl.heads = pl.heads_per_tile;
     if ((int64_t)pl.rows * pl.heads * D * 4 < ((int64_t)1 << 31)) return pl;
