@@ -476,9 +476,9 @@ int da_prefers_dealt(int B, int H_Q, int H_KV, int L_K_max, int64_t keys, int nu
 /* Decode attention with a sliding window and sinks: the last `window` keys of
  * each sequence (the query's own key among them) and its first `sinks` keys are
  * visible, key j of L where j < sinks or j >= L - window; the softmax of
- * da_decode_attn over those.  Invisible keys do not reach the result, whatever
- * they hold, and apart from rows that share a 32-key tile's descriptor nothing
- * of them is read.
+ * da_decode_attn over those.  Invisible keys are not read and do not reach the
+ * result, whatever they hold; a NaN in a visible one reaches the output and lse
+ * of the heads that read it.
  *   block_table == NULL: k, v fixed (cu_seqlens_k NULL) or packed, as for
  *     da_decode_attn (page_size, max_pages, num_pages, seq_lens ignored);
  *     otherwise paged as for da_decode_attn_paged (cu_seqlens_k ignored).
@@ -598,15 +598,21 @@ int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_ou
  *              or outside the window do not reach the result
  *   window     0: all keys (sinks is then ignored); otherwise as for
  *              da_decode_attn_window
- *   num_splits <= 0: chosen; else 1..64: chunks that a sequence of L_K_max keys
- *              is cut into.  Every sequence is cut into chunks of the same
- *              length in 32-key tiles, so a shorter one has fewer, and one that
- *              fits a chunk writes its output directly
+ *   num_splits 1..64: chunks that a sequence of L_K_max keys is cut into (fewer
+ *              where chunk states would reach 2 GiB, or for more than
+ *              DA_ARRIVAL_BYTES / DA_ARRIVAL_STRIDE head tiles); <= 0: a chunk
+ *              length chosen by the batch's lengths on the device, or for one
+ *              sequence and short batches by L_K_max.  Every sequence is cut into
+ *              chunks of the same length, a multiple of 64 keys, so a shorter one
+ *              has fewer, and one that fits a chunk writes its output directly
  *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, num_pages *
  *              page_size, window, sinks, num_splits, 0); 0 bytes for one chunk.  Counters in its last
  *              DA_ARRIVAL_BYTES zero before the first call, as for da_decode_attn
- * One launch.  Results are bit-identical across runs for the same arguments.
- * Other arguments and errors as for da_decode_attn_paged. */
+ * One launch; replays of a captured call follow the lengths the device then
+ * holds.  Results are bit-identical across runs for the same arguments and
+ * lengths of the whole batch.  A NaN among the visible keys, or an infinity or a
+ * NaN in a query, makes the output and lse of the heads that read it NaN.  Other arguments and errors as for da_decode_attn_paged, and
+ * DA_ERR_SHAPE for pages of 4 GiB or more. */
 int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* seq_lens,
                        void* out, float* lse_out, int B, int H_Q, int H_KV, int page_size, int max_pages,
                        int num_pages, int L_K_max, int d, float softmax_scale, int window, int sinks,

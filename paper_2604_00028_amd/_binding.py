@@ -21,6 +21,7 @@ HEAD_DIM = 128
 MAX_SPLITS = 64
 KV4_TILE_BYTES = 4352  # 32 keys of one KV head in the 4-bit cache
 MAX_REQUESTS = 4096    # of one da_extend_tables call
+INT_MAX = 2 ** 31 - 1
 DEALT_MIN_KEYS = 2561  # da_prefers_dealt never holds for shorter batches: no need to ask
 
 DA_OK = 0
@@ -715,6 +716,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
     its first `sinks` keys; returns `out`.  K and V as for da_decode_attn (fixed,
     or packed with cu_seqlens_k), or with block_table and seq_lens paged."""
     dev = q.device
+    window, sinks = min(window, INT_MAX), min(sinks, INT_MAX)
     page_size = max_pages = num_pages = 0
     if block_table is None:
         B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
@@ -943,6 +945,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
         raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")
     num_pages, H_KV, page_size = _kv4_cache(cache)
     B, H_Q, d = q.shape
+    window, sinks = min(window, INT_MAX), min(sinks, INT_MAX)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages]")
     max_pages = block_table.shape[1]

@@ -532,6 +532,10 @@ int launch_append(AppendParams& p, int cus, hipStream_t stream) {
                                        : std::min<int64_t>(passes, std::max<int64_t>(1, (16ll * cus + p.N - 1) / p.N));
   p.per_wave = (int)((passes + waves - 1) / waves);
   p.segments = (passes + p.per_wave - 1) / p.per_wave;
+  if ((int64_t)p.N * p.segments > (1 << 25)) {  // a launch holds fewer than 2^26 waves
+    p.per_wave = passes;
+    p.segments = 1;
+  }
   p.div_segments = make_div((uint32_t)p.segments);
   const int64_t units = (int64_t)p.N * p.segments;
   void* args[] = {&p};

@@ -504,7 +504,7 @@ split_partial_kernel(Params p) {
   __syncthreads();  // every wave is done with its stages
   publish_wave(red, reinterpret_cast<float*>(smem), wave, lane);
   __syncthreads();
-  finish_chunk<NT, NB, W>(p, reinterpret_cast<const float*>(smem), direct, row0_tile, srow0, nb0, wave, lane);
+  finish_chunk<NT, NB, W, WIN>(p, reinterpret_cast<const float*>(smem), direct, row0_tile, srow0, nb0, wave, lane);
 
   // Two-wave kernels never merge in the launch (their plans use the second
   // launch; the merge's batches are sized for four waves).
@@ -552,7 +552,7 @@ split_partial_kernel(Params p) {
     }
     __syncthreads();
     if (!s_last) return;
-    merge_tile<NT, W>(p, reinterpret_cast<float*>(smem), srow_m, cstride, s_m, row0_tile, tid);
+    merge_tile<NT, W, false, WIN>(p, reinterpret_cast<float*>(smem), srow_m, cstride, s_m, row0_tile, tid);
   }
 }
 
@@ -937,8 +937,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1, 
 // Log-sum-exp combine launch: one wave64 per (b, h) row, 2 dims per lane
 // (merge_rows), so the result is bit-identical across runs, producers of the
 // same chunk states, and the single-launch merge.  SEQ: per-sequence chunk
-// counts and state rows from `seqs`.
-template <bool SEQ>
+// counts and state rows from `seqs`.  NANS: as `holds`.
+template <bool SEQ, bool NANS>
 __global__ void __launch_bounds__(256) split_combine_kernel(const float* __restrict__ o_part,
                                                             const float* __restrict__ m_part,
                                                             const float* __restrict__ l_part,
@@ -966,7 +966,7 @@ __global__ void __launch_bounds__(256) split_combine_kernel(const float* __restr
   }
   const int64_t bases[1] = {base};
   const int64_t orows[1] = {row};
-  merge_rows<1, false>(o_part, m_part, l_part, bases, orows, 1, srow, s, out, lse, lane);
+  merge_rows<1, false, NANS>(o_part, m_part, l_part, bases, orows, 1, srow, s, out, lse, lane);
 }
 
 // ---------------------------------------------------------------- host side
@@ -1151,12 +1151,13 @@ int launch_partial(const Params& prm, const da_plan& pl, hipStream_t stream) {
 
 int launch_combine(const float* o_part, const float* m_part, const float* l_part, uint16_t* out, float* lse,
                    int s, int64_t rows, hipStream_t stream, const int32_t* seqs = nullptr, int state_rows = 0,
-                   int H_Q = 1) {
+                   int H_Q = 1, bool nans = false) {
   const int grid = (int)((rows + 3) / 4);
   Div div_hq = make_div((uint32_t)H_Q);
   void* args[] = {&o_part, &m_part, &l_part, &out, &lse, &s, &rows, &seqs, &state_rows, &H_Q, &div_hq};
-  const void* fn = seqs ? reinterpret_cast<const void*>(&split_combine_kernel<true>)
-                        : reinterpret_cast<const void*>(&split_combine_kernel<false>);
+  const void* fn = seqs   ? reinterpret_cast<const void*>(&split_combine_kernel<true, false>)
+                   : nans ? reinterpret_cast<const void*>(&split_combine_kernel<false, true>)
+                          : reinterpret_cast<const void*>(&split_combine_kernel<false, false>);
   hipError_t e = hipLaunchKernel(fn, dim3(grid), dim3(256), args, 0, stream);
   if (e != hipSuccess) return da::fail(DA_ERR_HIP, "combine launch: %s", hipGetErrorString(e));
   return DA_OK;
@@ -1258,7 +1259,7 @@ int run_decode(Params p, int B, int H_Q, int H_KV, int L_K_max, int d, float sof
   rc = launch_partial(p, pl, static_cast<hipStream_t>(stream));
   if (rc) return rc;
   return launch_combine(p.o_part, p.m_part, p.l_part, static_cast<uint16_t*>(out), lse_out, s, (int64_t)B * H_Q,
-                        static_cast<hipStream_t>(stream));
+                        static_cast<hipStream_t>(stream), nullptr, 0, 1, p.window > 0);
 }
 
 // The dealt launch of `groups` workgroups per head tile (dealt_kernel).

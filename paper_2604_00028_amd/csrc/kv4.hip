@@ -451,7 +451,7 @@ kv4_kernel(Kv4Params a) {
   __syncthreads();  // every wave is done with its stage
   publish_wave(red, reinterpret_cast<float*>(smem), wave, lane);
   __syncthreads();
-  finish_chunk<NT, 8, W>(p, reinterpret_cast<const float*>(smem), direct, row0, direct ? 0 : srow0, 0, wave, lane);
+  finish_chunk<NT, 8, W, true>(p, reinterpret_cast<const float*>(smem), direct, row0, direct ? 0 : srow0, 0, wave, lane);
   if (direct) return;
 
   // The merge inside the launch: the hand-off of split_partial_kernel
@@ -468,7 +468,7 @@ kv4_kernel(Kv4Params a) {
   }
   __syncthreads();
   if (!s_last) return;
-  merge_tile<NT, W>(p, reinterpret_cast<float*>(smem), srow0 - chunk * cstride, cstride, chunks, row0, tid);
+  merge_tile<NT, W, false, true>(p, reinterpret_cast<float*>(smem), srow0 - chunk * cstride, cstride, chunks, row0, tid);
 }
 
 // ---------------------------------------------------------------- host side

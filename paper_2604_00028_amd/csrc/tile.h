@@ -214,6 +214,14 @@ __device__ __forceinline__ float lane_value(float x, int i) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i));
 }
 
+// Whether a chunk of probability sum `l` holds a key.  NANS: a sum that is NaN (a
+// key or a query that is not finite) counts too, so that the NaN reaches the
+// output and the log-sum-exp instead of leaving its chunk out.
+template <bool NANS>
+__device__ __forceinline__ bool holds(float l) {
+  return NANS ? !(l == 0.f) : l > 0.f;
+}
+
 // The log-sum-exp merge of s <= 64 chunk states (the paper's final
 // reduction, Sections 3.1 and 5.3) for up to NR rows, by one wave: the lane
 // holds output dims 2*lane and 2*lane + 1 of each row, and lane i holds the
@@ -227,7 +235,7 @@ __device__ __forceinline__ float lane_value(float x, int i) {
 // single-launch merge give the same bits.  COH: the states were written in
 // this launch by other workgroups with device-scope stores and are read with
 // device-scope loads.  State offsets are below 2 GiB (checked on the host).
-template <int NR, bool COH>
+template <int NR, bool COH, bool NANS = false>
 __device__ __forceinline__ void merge_rows(const float* o_part, const float* m_part, const float* l_part,
                                            const int64_t (&base)[NR], const int64_t (&orow)[NR], int nr,
                                            int64_t srow, int s, uint16_t* out, float* lse, int lane) {
@@ -258,7 +266,7 @@ __device__ __forceinline__ void merge_rows(const float* o_part, const float* m_p
   float wi[NR], M[NR], L[NR], o0[NR], o1[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const bool live = li[r] > 0.f;
+    const bool live = holds<NANS>(li[r]);
     M[r] = wave_max(live ? mi[r] : -INFINITY);
     wi[r] = live ? __builtin_amdgcn_exp2f((mi[r] - M[r]) * kLog2e) : 0.f;
     L[r] = 0.f;
@@ -283,7 +291,7 @@ __device__ __forceinline__ void merge_rows(const float* o_part, const float* m_p
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
           const float w = lane_value(wi[r], i0 + u);
-          const bool live = lane_value(li[r], i0 + u) > 0.f;
+          const bool live = holds<NANS>(lane_value(li[r], i0 + u));
           o0[r] = fmaf(w, live ? a[r][u].x : 0.f, o0[r]);
           o1[r] = fmaf(w, live ? a[r][u].y : 0.f, o1[r]);
         }
@@ -294,7 +302,7 @@ __device__ __forceinline__ void merge_rows(const float* o_part, const float* m_p
     if (r >= nr) continue;
     const float inv = L[r] > 0.f ? 1.0f / L[r] : 0.f;
     *reinterpret_cast<uint32_t*>(out + orow[r] * D + 2 * lane) = pack_bf16x2(o0[r] * inv, o1[r] * inv);
-    if (lse && lane == 0) lse[orow[r]] = L[r] > 0.f ? M[r] + logf(L[r]) : -INFINITY;
+    if (lse && lane == 0) lse[orow[r]] = holds<NANS>(L[r]) ? M[r] + logf(L[r]) : -INFINITY;
   }
 }
 
@@ -317,7 +325,7 @@ __device__ __forceinline__ void merge_rows(const float* o_part, const float* m_p
 // which are not stored.  s <= CB merges in registers; more chunks stage their
 // maxima and sums in `lds` (at least 2 x (64 + 16) x 32 + 8 x 32 floats) and
 // take the columns in batches of CB.
-template <int W, int J, int CB, bool FIRST>
+template <int W, int J, int CB, bool FIRST, bool NANS>
 __device__ __forceinline__ void merge_columns(const Params& p, float* lds, int64_t srow0, int64_t cstride, int s,
                                               int64_t orow0, int tid, uint32_t first_rows) {
   constexpr int T = 64 * W;    // threads
@@ -346,7 +354,7 @@ __device__ __forceinline__ void merge_columns(const Params& p, float* lds, int64
     const float inv = L > 0.f ? 1.0f / L : 0.f;
     *reinterpret_cast<uint2*>(p.out + row * D + 4 * c) =
         make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-    if (p.lse && c == 0) p.lse[row] = L > 0.f ? M + logf(L) : -INFINITY;
+    if (p.lse && c == 0) p.lse[row] = holds<NANS>(L) ? M + logf(L) : -INFINITY;
   };
   float M[J], L[J];
   f32x4 o[J];
@@ -365,7 +373,7 @@ __device__ __forceinline__ void merge_columns(const Params& p, float* lds, int64
         for (int j = 0; j < J; ++j) {
           // an empty chunk's output is exactly zero here (w = 0 and O~ = 0 add nothing), as the
           // combine's guard on empty chunks makes it
-          const float w = bl[j][u] > 0.f ? __builtin_amdgcn_exp2f((bm[j][u] - M[j]) * kLog2e) : 0.f;
+          const float w = holds<NANS>(bl[j][u]) ? __builtin_amdgcn_exp2f((bm[j][u] - M[j]) * kLog2e) : 0.f;
           L[j] = fmaf(w, bl[j][u], L[j]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[j][e] = fmaf(w, a[j][u][e], o[j][e]);
@@ -389,7 +397,7 @@ __device__ __forceinline__ void merge_columns(const Params& p, float* lds, int64
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int u = 0; u < CB; ++u) M[j] = u < s && bl[j][u] > 0.f ? fmaxf(M[j], bm[j][u]) : M[j];
+      for (int u = 0; u < CB; ++u) M[j] = u < s && holds<NANS>(bl[j][u]) ? fmaxf(M[j], bm[j][u]) : M[j];
     add(a, bm, bl, 0);
   } else {
     // chunk rows are padded to 64 + CB so that a batch reads them unconditionally
@@ -415,7 +423,7 @@ __device__ __forceinline__ void merge_columns(const Params& p, float* lds, int64
         const int i = i0 + R * u;  // < 64; rows past s are never used
         lm[i * 32 + h] = mv[u];
         ll[i * 32 + h] = lv[u];
-        pm = i < s && lv[u] > 0.f ? fmaxf(pm, mv[u]) : pm;
+        pm = i < s && holds<NANS>(lv[u]) ? fmaxf(pm, mv[u]) : pm;
       }
       lp[i0 * 32 + h] = pm;
     }
@@ -445,7 +453,7 @@ __device__ __forceinline__ void merge_columns(const Params& p, float* lds, int64
 }
 
 // merge_columns by the rows and chunks in use.
-template <int NT, int W, bool FIRST = false>
+template <int NT, int W, bool FIRST = false, bool NANS = false>
 __device__ __forceinline__ void merge_tile(const Params& p, float* lds, int64_t srow0, int64_t cstride, int s,
                                            int64_t orow0, int tid, uint32_t first_rows = 0) {
   constexpr int T = 64 * W;              // threads
@@ -461,17 +469,17 @@ __device__ __forceinline__ void merge_tile(const Params& p, float* lds, int64_t 
   // a batch of 8 ran at 0.96-0.98x of a loop over the chunks there are, in a
   // batch of 4 at 1.04-1.07x (5-8 chunks of up to 8 heads in one of 8: 0.97-1.02x).
   if (p.hpt <= R && s <= 4)
-    merge_columns<W, 1, 4, FIRST>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
+    merge_columns<W, 1, 4, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
   else if (p.hpt <= R && (s <= 8 || s > 16))
-    merge_columns<W, 1, 8, FIRST>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
+    merge_columns<W, 1, 8, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
   else if (p.hpt <= R)
-    merge_columns<W, 1, 16, FIRST>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
+    merge_columns<W, 1, 16, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
   else if (IPT == 2 && s <= 4)
-    merge_columns<W, 2, 4, FIRST>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
+    merge_columns<W, 2, 4, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
   else if (IPT > 2 && p.hpt <= 2 * R)
-    merge_columns<W, 2, 8, FIRST>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
+    merge_columns<W, 2, 8, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
   else
-    merge_columns<W, IPT, CB, FIRST>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
+    merge_columns<W, IPT, CB, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
 }
 
 // One wave's running state over the 32-key tiles of a chunk: the packed query
@@ -683,7 +691,7 @@ __device__ __forceinline__ void publish_wave(const TileReducer<NT, NB>& red, flo
 // h), with device-scope stores where p.mode is kFused.  nb0: first 16-dim
 // block of this workgroup's V slice.  With fewer blocks than waves (V slices)
 // waves 0 .. NB - 1 merge one block each.
-template <int NT, int NB, int W>
+template <int NT, int NB, int W, bool NANS = false>
 __device__ __forceinline__ void finish_chunk(const Params& p, const float* slots, bool direct, int64_t row0_tile,
                                              int64_t srow0, int nb0, int wave, int lane) {
   static_assert(NB % W == 0 || W % NB == 0, "blocks must divide among the waves");
@@ -733,7 +741,7 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const float* slots
         *reinterpret_cast<uint2*>(p.out + row * D + 16 * nn + 4 * quad) =
             make_uint2(pack_bf16x2(o[bb][0] * inv, o[bb][1] * inv), pack_bf16x2(o[bb][2] * inv, o[bb][3] * inv));
       }
-      if (p.lse && wave == 0 && quad == 0 && nb0 == 0) p.lse[row] = Lw > 0.f ? mval + logf(Lw) : -INFINITY;
+      if (p.lse && wave == 0 && quad == 0 && nb0 == 0) p.lse[row] = holds<NANS>(Lw) ? mval + logf(Lw) : -INFINITY;
     } else if (p.mode == kPartials) {
 #pragma unroll
       for (int bb = 0; bb < NBW; ++bb) {

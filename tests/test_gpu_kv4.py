@@ -6,9 +6,10 @@ import torch
 
 import paper_2604_00028_amd as da
 from oracle import bf16_bits_to_f64
-from oracle.cache import attend, kv4_unpack
-from tests.cache_helpers import Batch, check_attention, new_lse
+from oracle.cache import attend, kv4_pack, kv4_unpack
+from tests.cache_helpers import Batch, check_attention, new_lse, normal_bits
 from tests.gpu_helpers import say, to_dev, to_f64
+from workloads import f32_to_bf16_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -193,3 +194,80 @@ def test_another_stream():
     da.da_decode_attn_kv4(q, cache, table, lens, 3000, out=out, stream=side)
     side.synchronize()
     assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("magnitude", [1e-30, 1e-3, 1e3, 1e25])
+def test_query_magnitudes(magnitude):
+    """The query's two 8-bit parts over the whole range of exponents, and elements far below the largest one."""
+    batch = Batch([300, 64], 8, 2, "kv4", page=64, seed=14)
+    rng = np.random.default_rng(15)
+    spread = 2.0 ** -rng.integers(0, 25, batch.q.shape).astype(np.float64)
+    spread[1] = 1.0
+    q = magnitude * spread * rng.standard_normal(batch.q.shape)
+    batch.q = f32_to_bf16_bits(q.astype(np.float32))
+    # scores around one whatever the magnitude
+    check_attention(*run(batch, f"magnitude {magnitude}", softmax_scale=0.1 / magnitude),
+                    batch.reference(0, 0, 0.1 / magnitude), f"magnitude {magnitude}")
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+def test_queries_that_are_not_finite(splits):
+    batch = Batch([400], 8, 2, "kv4", page=64, seed=16)
+    want, _ = run(batch, "finite", num_splits=splits)
+    batch.q[0, 1, 5], batch.q[0, 6, 127] = 0x7F80, 0x7FC0
+    out, lse = run(batch, "not finite", num_splits=splits)
+    got = to_f64(out)[0]
+    assert np.isnan(got[[1, 6]]).all() and np.isnan(lse.cpu().numpy()[0, [1, 6]]).all()
+    keep = [0, 2, 3, 4, 5, 7]
+    assert np.array_equal(got[keep], to_f64(want)[0][keep]) and np.isfinite(lse.cpu().numpy()[0, keep]).all()
+
+
+@pytest.mark.parametrize("splits", [0, 1, 3, 20])
+def test_a_nan_key_reaches_its_heads(splits):
+    """A visible key with a NaN block: the heads that read it give NaN, in whichever chunk it lies; others do not."""
+    batch = Batch([2000, 2000], 8, 2, "kv4", page=64, seed=18)
+    row = int(batch.rows[1][1500])
+    batch.cache[row // 64, 0, row % 64 // 32, 4096 + 4 * (4 * (row % 16) + 3) + row % 32 // 16] = 255  # K, head 0
+    out, lse = run(batch, f"NaN key s={splits}", num_splits=splits)
+    got, l = to_f64(out), lse.cpu().numpy()
+    assert np.isnan(got[1, :4]).all() and np.isnan(l[1, :4]).all()
+    assert np.isfinite(got[1, 4:]).all() and np.isfinite(got[0]).all() and np.isfinite(l[0]).all()
+
+
+def test_far_rows_of_a_large_cache():
+    """Rows past 4 GiB: written, read back and attended to, in the 4-bit and the bf16 cache."""
+    H_KV, page = 8, 1024
+    rng = np.random.default_rng(17)
+    N = 100
+    k, v, q = (normal_bits(rng, (N, H_KV, 128)), normal_bits(rng, (N, H_KV, 128)), normal_bits(rng, (1, 16, 128), 2.0))
+    num = 4200                                       # 4.7 GB in 4 bits
+    row0 = (num - 1) * page + 7 * 32 + 5
+    slots = torch.arange(row0, row0 + N, dtype=torch.int32, device="cuda")
+    cache = torch.empty(num, H_KV, page // 32, 4352, dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 1 << 32
+    say("far rows, 4 bits")
+    da.da_append_kv4(None, to_dev(k), to_dev(v), None, slots, cache)
+    gk, gv = da.da_read_kv4(cache, slots)
+    torch.cuda.synchronize()
+    kk, vv = kv4_unpack(kv4_pack(np.pad(k, ((0, 28), (0, 0), (0, 0))), np.pad(v, ((0, 28), (0, 0), (0, 0))), 128))
+    assert np.array_equal(to_f64(gk), kk[:N]) and np.array_equal(to_f64(gv), vv[:N])
+    # the sequence ends in the last page: its visible window is exactly the rows written
+    table = torch.tensor([[num - 1]], dtype=torch.int32, device="cuda")
+    L = 7 * 32 + 5 + N
+    lens = torch.tensor([L], dtype=torch.int32, device="cuda")
+    lse = torch.empty(1, 16, dtype=torch.float32, device="cuda")
+    out = da.da_decode_attn_kv4(to_dev(q), cache, table, lens, L, N, 0, lse_out=lse)
+    torch.cuda.synchronize()
+    check_attention(out, lse, attend(bf16_bits_to_f64(q), [kk[:N]], [vv[:N]]), "far rows, 4 bits")
+    del cache
+    num = 2100                                       # 4.4 GB of K in bf16
+    row0 = (num - 1) * page + 7 * 32 + 5
+    slots = torch.arange(row0, row0 + N, dtype=torch.int32, device="cuda")
+    kc, vc = (torch.empty(num, page, H_KV, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert kc.numel() * 2 > 1 << 32
+    say("far rows, bf16")
+    da.da_append_kv(None, to_dev(k), to_dev(v), None, slots, kc, vc)
+    out = da.da_decode_attn_window(to_dev(q), kc, vc, N, 0, None, table - table + num - 1, lens, L_K_max=L, lse_out=lse)
+    torch.cuda.synchronize()
+    assert torch.equal(kc.view(-1, H_KV, 128)[row0:row0 + N].view(torch.int16), to_dev(k).view(torch.int16))
+    check_attention(out, lse, attend(bf16_bits_to_f64(q), [bf16_bits_to_f64(k)], [bf16_bits_to_f64(v)]), "far, bf16")

@@ -131,3 +131,34 @@ def test_steps_in_a_captured_graph():
         assert np.array_equal(db.cpu().numpy(), table) and np.array_equal(dl.cpu().numpy(), lens) and int(dt) == taken
         for g, w in zip(outs, (cu, slots, positions)):
             assert np.array_equal(g.cpu().numpy(), w)
+
+
+def test_pages_that_are_none():
+    """Table entries and list entries outside the cache: no slot for the tokens they would hold."""
+    lens, new, free, taken, table, num = state([10, 20, 0, 7], [30, 3, 40, 1], 16, seed=8)
+    table[0, 0], table[1, 1], table[3, 0] = -1, num, 2 ** 31 - 1
+    free[taken + 1], free[taken + 3] = -7, num + 5
+    for in_place in (False, True):
+        check(lens, new, free, taken, table, num, 16, 80, "bad pages", in_place)
+
+
+def test_two_streams_at_once():
+    """The same tables from two streams, with outputs of their own."""
+    rng = np.random.default_rng(9)
+    s = state(rng.integers(0, 900, 200), rng.integers(0, 50, 200), 32, seed=9)
+    lens, new, free, taken, table, num = s
+    want = extend_tables(lens, new, free, taken, table, 32, num, 6000)
+    dev = [torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda() for a in (lens, new, free, [taken])]
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    tabs = [torch.from_numpy(table).cuda() for _ in sides]
+    torch.cuda.synchronize()
+    say("tables on two streams")
+    got = []
+    for side, tab in zip(sides, tabs):
+        with torch.cuda.stream(side):
+            got.append(da.da_extend_tables(*dev, tab, 32, num, 6000))
+    torch.cuda.synchronize()
+    for out, tab in zip(got, tabs):
+        assert np.array_equal(tab.cpu().numpy(), want[0])
+        for g, w in zip(out, (want[1], [want[2]], want[3], want[4], want[5])):
+            assert np.array_equal(g.cpu().numpy(), w)

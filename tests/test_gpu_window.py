@@ -119,3 +119,15 @@ def test_captured_call_follows_the_lengths():
         eager = torch.empty_like(q)
         da.da_decode_attn_window(q, k, v, 300, 8, None, table, lens, eager, L_K_max=2048)
         assert torch.equal(eager.view(torch.int16), out.view(torch.int16))
+
+
+@pytest.mark.parametrize("splits,heads", [(1, (8, 2)), (3, (8, 2)), (20, (64, 2)), (7, (128, 2)), (64, (8, 2))])
+def test_a_visible_nan_reaches_its_heads(splits, heads):
+    """A NaN in a visible key: the heads that read it give NaN, in whichever chunk it lies; others do not."""
+    batch = Batch([3000, 3000], *heads, "packed", seed=13)
+    batch.k[3000 + 2990, 1, 7] = 0x7FC0
+    out, lse = run(batch, 2000, 64, f"visible NaN s={splits}", num_splits=splits)
+    got, l = out.float().cpu().numpy(), lse.cpu().numpy()
+    g = heads[0] // 2
+    assert np.isnan(got[1, g:]).all() and np.isnan(l[1, g:]).all()
+    assert np.isfinite(got[1, :g]).all() and np.isfinite(got[0]).all() and np.isfinite(l[0]).all()
