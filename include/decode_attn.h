@@ -606,13 +606,15 @@ int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_ou
  *              chunks of the same length, a multiple of 64 keys, so a shorter one
  *              has fewer, and one that fits a chunk writes its output directly
  *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, num_pages *
- *              page_size, window, sinks, num_splits, 0); 0 bytes for one chunk.  Counters in its last
- *              DA_ARRIVAL_BYTES zero before the first call, as for da_decode_attn
+ *              page_size, window, sinks, num_splits, 0); 0 bytes for one chunk.
+ *              Counters in its last DA_ARRIVAL_BYTES zero before the first call,
+ *              as for da_decode_attn
  * One launch; replays of a captured call follow the lengths the device then
  * holds.  Results are bit-identical across runs for the same arguments and
  * lengths of the whole batch.  A NaN among the visible keys, or an infinity or a
- * NaN in a query, makes the output and lse of the heads that read it NaN.  Other arguments and errors as for da_decode_attn_paged, and
- * DA_ERR_SHAPE for pages of 4 GiB or more. */
+ * NaN in a query, makes the output and lse of the heads that read it NaN.
+ * Other arguments and errors as for da_decode_attn_paged, and DA_ERR_SHAPE for
+ * pages of 4 GiB or 2^24 head tiles and more. */
 int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* seq_lens,
                        void* out, float* lse_out, int B, int H_Q, int H_KV, int page_size, int max_pages,
                        int num_pages, int L_K_max, int d, float softmax_scale, int window, int sinks,

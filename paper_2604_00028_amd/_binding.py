@@ -21,6 +21,7 @@ HEAD_DIM = 128
 MAX_SPLITS = 64
 KV4_TILE_BYTES = 4352  # 32 keys of one KV head in the 4-bit cache
 MAX_REQUESTS = 4096    # of one da_extend_tables call
+ARRIVAL_BYTES = 1 << 20  # counters at the end of a workspace
 INT_MAX = 2 ** 31 - 1
 DEALT_MIN_KEYS = 2561  # da_prefers_dealt never holds for shorter batches: no need to ask
 
@@ -680,6 +681,44 @@ def _on_device(dev: torch.device, fn, *args, **kw):
         return fn(*args, **kw)
 
 
+_captures = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
+# (device, stream) -> (capture, workspace): of the capture that is under way there, or was last
+_graph_workspaces: Dict[Tuple[int, int], Tuple[int, torch.Tensor]] = {}
+
+
+class _Scratch:
+    """Workspace of a call on the current device that passes none: outside graph
+    capture the one cached for its stream.  A captured call takes one that its
+    graph owns, shared by the calls captured on that stream and cleared by each
+    replay, so that graphs can be replayed in any order, beside each other and
+    beside the stream's own calls."""
+
+    def __init__(self, dev: torch.device, stream, handle: int) -> None:
+        self.dev, self.handle = dev, handle
+        self.capture = 0
+        if _captures() if stream is None else _capturing(dev, stream):
+            status, number = ctypes.c_int(), ctypes.c_ulonglong()
+            if load().hipStreamGetCaptureInfo(_P(handle), ctypes.byref(status), ctypes.byref(number)):
+                raise DecodeAttnError(DA_ERR_HIP, "the stream's capture has no number")
+            self.capture = number.value + 1
+
+    def offered(self) -> Optional[torch.Tensor]:
+        """What there is already."""
+        if not self.capture:
+            return _workspaces.get((self.dev.index, self.handle))
+        capture, ws = _graph_workspaces.get((self.dev.index, self.handle), (0, None))
+        return ws if capture == self.capture else None
+
+    def grown(self, nbytes: int) -> torch.Tensor:
+        if not self.capture:
+            return workspace_for(self.dev, self.handle, nbytes)
+        with torch.cuda.stream(_on(self.dev, self.handle)):
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
+            ws[-ARRIVAL_BYTES:].zero_()
+        _graph_workspaces[self.dev.index, self.handle] = (self.capture, ws)
+        return ws
+
+
 def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dev: torch.device) -> None:
     if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {dev}, got {t.dtype} "
@@ -732,7 +771,8 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
                           pack_gqa=pack_gqa, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
-    ws = _offered(workspace, dev, s_handle)
+    scratch = None if workspace is not None else _Scratch(dev, stream, s_handle)
+    ws = workspace if scratch is None else scratch.offered()
     while True:
         rc = load().da_decode_attn_window(
             q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(cu_seqlens_k), _ptr(block_table), _ptr(seq_lens), page_size,
@@ -741,7 +781,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
         plan = da_make_plan(B, H_Q, H_KV, da_window_keys(L, window, sinks), d, num_splits, pack_gqa)
-        workspace = ws = workspace_for(dev, s_handle, da_workspace_bytes(B, H_Q, d, plan.num_splits))
+        workspace = ws = scratch.grown(da_workspace_bytes(B, H_Q, d, plan.num_splits))
     if rc:
         _check(rc)
     return out
@@ -958,15 +998,16 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
     L = int(L_K_max)
-    ws = _offered(workspace, dev, s_handle)
+    scratch = None if workspace is not None else _Scratch(dev, stream, s_handle)
+    ws = workspace if scratch is None else scratch.offered()
     while True:
         rc = load().da_decode_attn_kv4(q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
                                        out.data_ptr(), _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L, d,
                                        softmax_scale, window, sinks, num_splits, _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
-        workspace = ws = workspace_for(dev, s_handle, da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size,
-                                                                             window, sinks, num_splits))
+        workspace = ws = scratch.grown(da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size, window, sinks,
+                                                              num_splits))
     if rc:
         _check(rc)
     return out

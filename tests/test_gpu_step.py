@@ -10,7 +10,7 @@ import paper_2604_00028_amd as da
 from oracle import bf16_bits_to_f64
 from oracle.cache import attend, extend_tables, kv4_unpack, norm_rotate, visible_keys
 from paper_2604_00028_amd import _binding as bnd
-from tests.cache_helpers import Batch, check_attention, normal_bits
+from tests.cache_helpers import Batch, check_attention, new_lse, normal_bits
 from tests.gpu_helpers import say, to_dev, to_f64
 from tests.test_gpu_append import EPS, cache_rows, close, row_bytes
 
@@ -266,3 +266,50 @@ def test_empty_calls():
                                    z(2, t=torch.int32), L_K_max=0)
     torch.cuda.synchronize()
     assert not out.any()
+
+
+@pytest.mark.parametrize("kind", ["kv4", "window"])
+def test_graphs_without_a_workspace(kind):
+    """Captured without a call before, replayed in the other order, beside each other and beside their stream's own calls."""
+    batches = [Batch([1500], 8, 2, "kv4" if kind == "kv4" else "paged", page=64, seed=s) for s in (31, 32, 33)]
+    calls, refs, outs = [], [], []
+    for batch in batches:
+        if kind == "kv4":
+            q, cache = to_dev(batch.q), torch.from_numpy(batch.cache).cuda()
+            table, lens = torch.from_numpy(batch.table).cuda(), batch.seq_lens()
+            fn = lambda o, l, q=q, c=cache, t=table, n=lens: da.da_decode_attn_kv4(  # noqa: E731
+                q, c, t, n, 1500, 0, 0, o, l, num_splits=9)
+            refs.append(batch.reference(0, 0))
+        else:
+            q, k, v = to_dev(batch.q), to_dev(batch.k), to_dev(batch.v)
+            table, lens = torch.from_numpy(batch.table).cuda(), batch.seq_lens()
+            fn = lambda o, l, q=q, k=k, v=v, t=table, n=lens: da.da_decode_attn_window(  # noqa: E731
+                q, k, v, 900, 100, None, t, n, o, l, L_K_max=1500, num_splits=9)
+            refs.append(batch.reference(900, 100))
+        calls.append(fn)
+        outs.append((torch.empty_like(q), new_lse(batch)))
+    side = torch.cuda.Stream()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for graph, fn, out in zip(graphs, calls, outs):
+        say(f"{kind} capture")
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            fn(*out)
+            fn(*out)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream(), side]
+    for turn in range(6):
+        say(f"{kind} replays {turn}")
+        for out, lse in outs:
+            out.fill_(7.0)
+            lse.fill_(7.0)
+        torch.cuda.synchronize()
+        for i in (1, 2, 0) if turn % 2 else (2, 0, 1):
+            if turn == 0 and i == 0:
+                continue  # the second graph's first replay comes before the first one's
+            with torch.cuda.stream(streams[i]):
+                for _ in range(4):
+                    graphs[i].replay() if i < 2 else calls[2](*outs[2])
+        torch.cuda.synchronize()
+        for i in (1, 2) if turn == 0 else (0, 1, 2):
+            check_attention(*outs[i], refs[i], f"{kind} turn {turn} call {i}")
+    del graphs
