@@ -48,7 +48,8 @@ METRIC = "decode-attention µs/call + achieved HBM GB/s (% of peak), heuristic v
 HBM_PEAK_GBS = 8000.0
 PROFILE_TRAFFIC = os.path.join(ROOT, "profiles", "traffic.json")
 KERNEL_SOURCES = [os.path.join(ROOT, "paper_2604_00028_amd", "csrc", f)
-                  for f in ("decode_attn.hip", "plan.cpp", "plan.h", "cost_model.inc", "split_table.inc")]
+                  for f in ("decode_attn.hip", "tile.h", "host.h", "plan.cpp", "plan.h", "cost_model.inc",
+                            "split_table.inc")]
 SWEEP = (1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64)
 HIGHLOAD_SWEEP = (1, 2, 3, 4, 6, 8, 12, 16)
 LONG_SWEEP = (1, 2, 4, 8, 12, 16, 24)

@@ -451,7 +451,8 @@ kv4_kernel(Kv4Params a) {
   __syncthreads();  // every wave is done with its stage
   publish_wave(red, reinterpret_cast<float*>(smem), wave, lane);
   __syncthreads();
-  finish_chunk<NT, 8, W, true>(p, reinterpret_cast<const float*>(smem), direct, row0, direct ? 0 : srow0, 0, wave, lane);
+  finish_chunk<NT, 8, W, true>(p, reinterpret_cast<const float*>(smem), direct, row0, direct ? 0 : srow0, 0, wave,
+                               lane);
   if (direct) return;
 
   // The merge inside the launch: the hand-off of split_partial_kernel
@@ -468,11 +469,13 @@ kv4_kernel(Kv4Params a) {
   }
   __syncthreads();
   if (!s_last) return;
-  merge_tile<NT, W, false, true>(p, reinterpret_cast<float*>(smem), srow0 - chunk * cstride, cstride, chunks, row0, tid);
+  merge_tile<NT, W, false, true>(p, reinterpret_cast<float*>(smem), srow0 - chunk * cstride, cstride, chunks, row0,
+                                 tid);
 }
 
 // ---------------------------------------------------------------- host side
 
+constexpr int kDealtSequences = 1024;      // most of a batch that is dealt
 constexpr double kStreamBytes = 64 << 20;  // a quarter of the last-level cache
 
 struct Kv4Plan {
@@ -498,8 +501,12 @@ Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int64_t pool, int num_split
                                                                                        ((int64_t)B * H_Q * D * 4)));
   // Lengths that differ decide the chunks on the device (dealt).  That costs
   // about 1 us before the first load, so one sequence, and batches whose longest
-  // takes a few microseconds anyway, have chunks of a length chosen here.
-  if (num_splits <= 0 && B > 1 && T > 8 * 2 * W && most == DA_MAX_SPLITS && (int64_t)B * T <= (1 << 30)) {
+  // takes a few microseconds anyway, have chunks of a length chosen here; so do
+  // batches of so many sequences that each workgroup's two passes over the lengths
+  // cost more than even chunks give (8/1 heads, lognormal lengths up to 16384: 1024
+  // sequences 78 us whole, 45 dealt; 4096 sequences 125 and 226).
+  if (num_splits <= 0 && B > 1 && B <= kDealtSequences && T > 8 * 2 * W && most == DA_MAX_SPLITS &&
+      (int64_t)B * T <= (1 << 30)) {
     pl.groups = std::max(1, cus / tps);
     // the shares, and a chunk's rounding for each sequence
     // Where lengths differ, whole and partial chunks meet on a CU, and half shares

@@ -116,6 +116,15 @@ def test_mixed_batches_cut_by_their_lengths(H_Q, H_KV, window, sinks):
     assert torch.equal(again[0].view(torch.int16), out[0].view(torch.int16)) and torch.equal(again[1], out[1])
 
 
+@pytest.mark.parametrize("B", [1024, 1025])
+def test_many_sequences_and_a_long_one(B):
+    """On either side of the most sequences whose lengths decide the chunks."""
+    lengths = [int(n) for n in np.random.default_rng(B).integers(0, 120, B)]
+    lengths[B - 2] = 4000
+    batch = Batch(lengths, 4, 1, "kv4", page=32, seed=19, max_pages=125)
+    check_attention(*run(batch, f"B={B}"), batch.reference(0, 0), f"B={B}")
+
+
 def test_a_nan_block_reaches_its_own_sequence_only():
     batch = Batch([100, 100], 4, 2, "kv4", page=32, seed=6)
     row = int(batch.rows[0][50])
