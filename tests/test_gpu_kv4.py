@@ -207,7 +207,7 @@ def test_another_stream():
 
 @pytest.mark.parametrize("magnitude", [1e-30, 1e-3, 1e3, 1e25])
 def test_query_magnitudes(magnitude):
-    """The query's two 8-bit parts over the whole range of exponents, and elements far below the largest one."""
+    """The query's 8-bit parts over the whole range of exponents, and elements far below the largest one."""
     batch = Batch([300, 64], 8, 2, "kv4", page=64, seed=14)
     rng = np.random.default_rng(15)
     spread = 2.0 ** -rng.integers(0, 25, batch.q.shape).astype(np.float64)
@@ -217,6 +217,31 @@ def test_query_magnitudes(magnitude):
     # scores around one whatever the magnitude
     check_attention(*run(batch, f"magnitude {magnitude}", softmax_scale=0.1 / magnitude),
                     batch.reference(0, 0, 0.1 / magnitude), f"magnitude {magnitude}")
+
+
+@pytest.mark.parametrize("large", [1.0, 16.0, 256.0, 4096.0])
+@pytest.mark.parametrize("length", [1, 20, 300])
+def test_scores_hold_beside_a_large_query_element(length, large):
+    """Log-sum-exps to 32 bits, also where one element of the query is far larger than the others.
+
+    An element within 11 powers of two of the largest is exact, a smaller one off by
+    2^-19 of the largest's power of two; three products of 16 partial sums each, cut
+    at 2^-23 of sums below sum |q k|, and the cut of the codes' own sums, 2^-23 each;
+    the exponent's scale, its logarithm and the sum of 300 probabilities 2^-20 more."""
+    batch = Batch([length], 8, 2, "kv4", page=32, seed=20)
+    q = bf16_bits_to_f64(batch.q) * np.where(np.arange(128) == 21, large, 1.0)
+    batch.q = f32_to_bf16_bits(q.astype(np.float32))
+    q = bf16_bits_to_f64(batch.q)[0]
+    _, lse = run(batch, f"large {large} L={length}")
+    want = batch.reference(0, 0)[1][0]
+    keys = np.abs(kv4_unpack(batch.cache)[0][batch.rows[0]])
+    top = 2.0 ** np.floor(np.log2(np.abs(q).max(1)))
+    for h in range(8):
+        lost = np.where(np.abs(q[h]) < 2.0 ** -11 * top[h], 2.0 ** -19 * top[h], 0.0)
+        k = keys[:, h // 4]
+        tol = (k @ (lost + 3 * 17 * 2.0 ** -23 * np.abs(q[h]))).max() / np.sqrt(128) + 2.0 ** -20 * (1 + abs(want[h]))
+        err = abs(float(lse[0, h]) - want[h])
+        assert err <= tol, f"head {h}: off by {err:.2e}, tolerance {tol:.2e}"
 
 
 @pytest.mark.parametrize("splits", [1, 3])
