@@ -686,37 +686,31 @@ _captures = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.c
 _graph_workspaces: Dict[Tuple[int, int], Tuple[int, torch.Tensor]] = {}
 
 
-class _Scratch:
-    """Workspace of a call on the current device that passes none: outside graph
-    capture the one cached for its stream.  A captured call takes one that its
-    graph owns, shared by the calls captured on that stream and cleared by each
-    replay, so that graphs can be replayed in any order, beside each other and
-    beside the stream's own calls."""
+def _offered_now(dev: torch.device, stream, handle: int) -> Tuple[Optional[torch.Tensor], int]:
+    """The workspace to offer a call on the current device that passes none, and
+    the number of the capture it is part of, or 0.  Outside graph capture it is
+    the one cached for the stream.  A captured call takes one that its graph
+    owns, shared by the calls captured on that stream and cleared by each replay,
+    so that graphs can be replayed in any order, beside each other and beside the
+    stream's own calls."""
+    if not (_captures() if stream is None else _capturing(dev, stream)):
+        return _workspaces.get((dev.index, handle)), 0
+    status, number = ctypes.c_int(), ctypes.c_ulonglong()
+    if load().hipStreamGetCaptureInfo(_P(handle), ctypes.byref(status), ctypes.byref(number)):
+        raise DecodeAttnError(DA_ERR_HIP, "the stream's capture has no number")
+    capture, ws = _graph_workspaces.get((dev.index, handle), (0, None))
+    return (ws if capture == number.value + 1 else None), number.value + 1
 
-    def __init__(self, dev: torch.device, stream, handle: int) -> None:
-        self.dev, self.handle = dev, handle
-        self.capture = 0
-        if _captures() if stream is None else _capturing(dev, stream):
-            status, number = ctypes.c_int(), ctypes.c_ulonglong()
-            if load().hipStreamGetCaptureInfo(_P(handle), ctypes.byref(status), ctypes.byref(number)):
-                raise DecodeAttnError(DA_ERR_HIP, "the stream's capture has no number")
-            self.capture = number.value + 1
 
-    def offered(self) -> Optional[torch.Tensor]:
-        """What there is already."""
-        if not self.capture:
-            return _workspaces.get((self.dev.index, self.handle))
-        capture, ws = _graph_workspaces.get((self.dev.index, self.handle), (0, None))
-        return ws if capture == self.capture else None
-
-    def grown(self, nbytes: int) -> torch.Tensor:
-        if not self.capture:
-            return workspace_for(self.dev, self.handle, nbytes)
-        with torch.cuda.stream(_on(self.dev, self.handle)):
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.dev)
-            ws[-ARRIVAL_BYTES:].zero_()
-        _graph_workspaces[self.dev.index, self.handle] = (self.capture, ws)
-        return ws
+def _grown(dev: torch.device, handle: int, capture: int, nbytes: int) -> torch.Tensor:
+    """A larger workspace than the one offered."""
+    if not capture:
+        return workspace_for(dev, handle, nbytes)
+    with torch.cuda.stream(_on(dev, handle)):
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        ws[-ARRIVAL_BYTES:].zero_()
+    _graph_workspaces[dev.index, handle] = (capture, ws)
+    return ws
 
 
 def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dev: torch.device) -> None:
@@ -771,8 +765,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
                           pack_gqa=pack_gqa, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
-    scratch = None if workspace is not None else _Scratch(dev, stream, s_handle)
-    ws = workspace if scratch is None else scratch.offered()
+    ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
         rc = load().da_decode_attn_window(
             q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(cu_seqlens_k), _ptr(block_table), _ptr(seq_lens), page_size,
@@ -781,7 +774,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
         plan = da_make_plan(B, H_Q, H_KV, da_window_keys(L, window, sinks), d, num_splits, pack_gqa)
-        workspace = ws = scratch.grown(da_workspace_bytes(B, H_Q, d, plan.num_splits))
+        workspace = ws = _grown(dev, s_handle, capture, da_workspace_bytes(B, H_Q, d, plan.num_splits))
     if rc:
         _check(rc)
     return out
@@ -800,8 +793,8 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
     lens_out may be lens and taken_out may be taken."""
     dev = lens.device
     if lens.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2 or max_tokens < 0 or not lens.is_cuda:
-        raise ValueError("lens and free_pages must have one dimension, block_table two, on the GPU, and max_tokens must "
-                         "not be negative")
+        raise ValueError("lens and free_pages must have one dimension, block_table two, on the GPU, and max_tokens "
+                         "must not be negative")
     B = lens.shape[0]
     num_free = free_pages.shape[0]
     max_pages = block_table.shape[1]
@@ -828,8 +821,8 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
         given = tuple(torch.empty(n, dtype=_I32, device=dev) if t is None else t for t, n in zip(given, sizes))
         ptrs = tuple(_ptr(t) for t in given)
     rc = load().da_extend_tables(lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(), taken.data_ptr(),
-                                 block_table.data_ptr(), *ptrs, B, page_size, max_pages, num_pages, num_free, max_tokens,
-                                 _stream(dev, stream))
+                                 block_table.data_ptr(), *ptrs, B, page_size, max_pages, num_pages, num_free,
+                                 max_tokens, _stream(dev, stream))
     if rc:
         _check(rc)
     return given if new is None else new.split_with_sizes(sizes)
@@ -920,7 +913,8 @@ def _kv4_cache(cache: torch.Tensor) -> Tuple[int, int, int]:
     shape = cache.shape
     if (len(shape) != 4 or cache.dtype is not torch.uint8 or shape[3] != KV4_TILE_BYTES or not cache.is_contiguous()
             or not cache.is_cuda):
-        raise ValueError(f"cache must be a contiguous uint8 CUDA tensor [num_pages, H_KV, page_size / 32, {KV4_TILE_BYTES}]")
+        raise ValueError("cache must be a contiguous uint8 CUDA tensor [num_pages, H_KV, page_size / 32, "
+                         f"{KV4_TILE_BYTES}]")
     return shape[0], shape[1], 32 * shape[2]
 
 
@@ -960,8 +954,8 @@ def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
     if dev.index != _get_device():
         return _on_device(dev, da_read_kv4, cache, slots, stream=stream)
     k, v = torch.empty((2, N, H_KV, HEAD_DIM), dtype=_BF16, device=dev).unbind(0)
-    rc = load().da_read_kv4(cache.data_ptr(), _ptr(slots), k.data_ptr(), v.data_ptr(), N, H_KV, page_size, num_pages, HEAD_DIM,
-                            _stream(dev, stream))
+    rc = load().da_read_kv4(cache.data_ptr(), _ptr(slots), k.data_ptr(), v.data_ptr(), N, H_KV, page_size, num_pages,
+                            HEAD_DIM, _stream(dev, stream))
     if rc:
         _check(rc)
     return k, v
@@ -998,16 +992,15 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
     L = int(L_K_max)
-    scratch = None if workspace is not None else _Scratch(dev, stream, s_handle)
-    ws = workspace if scratch is None else scratch.offered()
+    ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
         rc = load().da_decode_attn_kv4(q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
                                        out.data_ptr(), _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L, d,
                                        softmax_scale, window, sinks, num_splits, _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
-        workspace = ws = scratch.grown(da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size, window, sinks,
-                                                              num_splits))
+        workspace = ws = _grown(dev, s_handle, capture,
+                                da_kv4_workspace_bytes(B, H_Q, H_KV, L, num_pages * page_size, window, sinks, num_splits))
     if rc:
         _check(rc)
     return out

@@ -157,8 +157,8 @@ __device__ __forceinline__ void softmax_pair(TileReducer<NT, 8>& red, f32x4 (&sc
 //   * One softmax for the pair: half the row reductions, rescalings and branches
 //     (the same work resident in L2: 36 -> 33 us).
 // Bound by HBM over long batches: 32 sequences of 8192 keys, 64/8 heads (286 MB)
-// 45-52 us by the run, 43 from the first workgroup's start to the last one's end,
-// 6.6 TB/s; resident in L2 the same work takes 33 us at three workgroups a CU.
+// 46-53 us by the run, 44 from the first workgroup's start to the last one's end,
+// 6.5 TB/s; resident in L2 the same work takes 34 us at three workgroups a CU.
 // Bound by latency where a wave has few pairs (1.1 us each alone).
 template <int NT, bool NTL, bool WIN, bool DEAL>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2, 8)))
