@@ -16,6 +16,8 @@ Contents
               max subtraction, for tiny inputs (a pin for `attention`).
   policy      the paper's sequence-aware split rule (Section 4), as stated in
               its prose.
+  cache       what surrounds the attention in a decode step: block tables,
+              norm and rotation, the 4-bit format, windows.
 
 Every function is pinned by tests that do not reuse its own formula (brute
 force, closed forms, invariants, library routines, the paper's table).
