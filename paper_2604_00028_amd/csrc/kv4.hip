@@ -18,6 +18,10 @@ using da::aligned;
 using da::ensure_gfx950;
 
 constexpr int W = 4;  // waves per workgroup
+// Most chunks of a sequence where their length is chosen: more cost the merge more
+// than they save (one sequence of 16000 keys, 32/4 heads, 63 chunks 13.0 us, 32 10.7;
+// three of 1-30000, 32/2, 19.6 and 17.1; larger batches do not reach it).
+constexpr int kChosenChunks = 32;
 constexpr int kFp8 = 0, kFp4 = 4;  // operand formats of the scaled product: e4m3, e2m1
 
 struct Kv4Params {
@@ -178,7 +182,7 @@ kv4_kernel(Kv4Params a) {
   if constexpr (DEAL) {
     // The lengths decide: chunks of an even share of the batch's tiles for each of
     // a.groups places a head tile, or half of one (at least a pair of tiles a wave,
-    // at most 64 chunks a sequence; three pairs a wave are as fast as a merge).
+    // at most 32 chunks a sequence; three pairs a wave are as fast as a merge).
     // Sequences have as many workgroups as chunks, so none is launched for nothing
     // but those by which the chunks' roundings stay below their bound.  (One split
     // count for all: 128 MQA sequences of 16-32768 keys 29 us at the best count,
@@ -204,7 +208,7 @@ kv4_kernel(Kv4Params a) {
     int share = div_by(total + a.groups - 1, a.div_groups);
     // a longest sequence of more than one and a half times the mean length
     if (a.halves && (int64_t)top * p.B * 2 > (int64_t)total * 3) share = (share + 1) / 2;
-    int per = max(max(share, 2 * W), (top + DA_MAX_SPLITS - 1) / DA_MAX_SPLITS);
+    int per = max(max(share, 2 * W), (top + kChosenChunks - 1) / kChosenChunks);
     if (top <= 6 * W) per = top;
     per = max(2, (per + 1) & ~1);
     chunk_tiles = per;
@@ -535,7 +539,7 @@ Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int64_t pool, int num_split
     // 32-column tiles (128/2) 23.6 -> 33.9, and equal lengths 0-19% slower.
     pl.halves = pl.heads_per_tile <= 16 && pl.tiles >= cus / 2;
     const int64_t chunks =
-        std::min<int64_t>((int64_t)pl.groups * (1 + pl.halves) + B, (int64_t)B * DA_MAX_SPLITS);
+        std::min<int64_t>((int64_t)pl.groups * (1 + pl.halves) + B, (int64_t)B * kChosenChunks);
     pl.grid = (int)((chunks * tps + 7) / 8 * 8);
     pl.rows = pl.grid;
     pl.heads = pl.heads_per_tile;
@@ -546,7 +550,7 @@ Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int64_t pool, int num_split
     chunk = (T + num_splits - 1) / num_splits;
   } else {
     const int64_t mean = std::min<int64_t>(T, (pool / B + kKeysPerTile - 1) / kKeysPerTile);
-    chunk = T <= 6 * W ? T : std::max<int64_t>(mean * pl.tiles / cus, 2 * W);
+    chunk = T <= 6 * W ? T : std::max<int64_t>({mean * pl.tiles / cus, 2 * W, (T + kChosenChunks - 1) / kChosenChunks});
   }
   chunk = std::max<int64_t>(chunk, (T + most - 1) / most);
   pl.chunk_tiles = 2 * (int)((std::min<int64_t>(chunk, T) + 1) / 2);  // whole pairs
