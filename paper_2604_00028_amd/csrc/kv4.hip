@@ -189,19 +189,30 @@ kv4_kernel(Kv4Params a) {
     // 20 so.  Runs of equal length over sequence ends, as dealt_kernel gives its
     // workgroups, balance the CUs better and pay for the ends: over 250 MB 4-12%
     // faster, below it up to 45% slower.)
-    int len = 0, tl = 0, win = 0;  // lane i: sequence win + i
-    auto window = [&](int b0) {
-      win = b0;
-      len = b0 + lane < p.B ? p.seq_lens[b0 + lane] : 0;
-      len = len < 0 ? 0 : (len > p.L_K ? p.L_K : len);
-      const int vis = WIN ? len - window_of(len, p.window, p.sinks).skip : len;
-      tl = (vis + kKeysPerTile - 1) / kKeysPerTile;
+    // Lengths and tiles of 256 sequences, loaded together (one after the other they
+    // took 4 us of 80 sequences): lane i has b0 + 64 w + i, none past the batch.
+    constexpr int kPasses = 4;
+    const __amdgpu_buffer_rsrc_t lens = make_rsrc(p.seq_lens, 4u * (uint32_t)p.B);
+    int len[kPasses], tl[kPasses];
+    auto load_lengths = [&](int b0) {
+#pragma unroll
+      for (int w = 0; w < kPasses; ++w)
+        len[w] = (int)__builtin_amdgcn_raw_buffer_load_b32(lens, 4u * (uint32_t)(b0 + 64 * w + lane), 0, 0);
+#pragma unroll
+      for (int w = 0; w < kPasses; ++w) {
+        len[w] = len[w] < 0 ? 0 : (len[w] > p.L_K ? p.L_K : len[w]);
+        const int vis = WIN ? len[w] - window_of(len[w], p.window, p.sinks).skip : len[w];
+        tl[w] = (vis + kKeysPerTile - 1) / kKeysPerTile;
+      }
     };
     int sum = 0, top = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-      window(b0);
-      sum += tl;  // at most 2^30 in all
-      top = max(top, tl);
+    for (int b0 = 0; b0 < p.B; b0 += 64 * kPasses) {
+      load_lengths(b0);
+#pragma unroll
+      for (int w = 0; w < kPasses; ++w) {
+        sum += tl[w];  // at most 2^30 in all
+        top = max(top, tl[w]);
+      }
     }
     const int total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
     top = wave_top(top);
@@ -213,12 +224,12 @@ kv4_kernel(Kv4Params a) {
     per = max(2, (per + 1) & ~1);
     chunk_tiles = per;
     const float inv = 1.0f / (float)per;
-    auto lane_chunks = [&]() {  // below 2^24: the quotient is off by one at most
-      const int x = tl + per - 1;
+    auto lane_chunks = [&](int at, int tiles_of) {  // small: the quotient is off by one at most
+      const int x = tiles_of + per - 1;
       int q = (int)((float)x * inv);
       q += (q + 1) * per <= x ? 1 : 0;
       q -= q * per > x ? 1 : 0;
-      return win + lane < p.B ? max(q, 1) : 0;
+      return at + lane < p.B ? max(q, 1) : 0;
     };
     // Items: a sequence's chunks, the head tiles of each next to one another.
     // Workgroup i starts on XCD i % 8, and patterns in the lengths (two chunks
@@ -230,20 +241,24 @@ kv4_kernel(Kv4Params a) {
     b = -1;
     int first = 0;
     L = 0;
-    for (int b0 = 0, before = 0; b0 < p.B; b0 += 64) {
-      if (p.B > 64) window(b0);
-      const int c = lane_chunks();
-      const int incl = wave_scan(c);
-      const uint64_t past = __ballot((before + incl) * p.tiles_per_seq > item);
-      if (past) {
-        const int i = __ffsll((unsigned long long)past) - 1;
-        b = b0 + i;
-        first = (before + __builtin_amdgcn_readlane(incl - c, i)) * p.tiles_per_seq;
-        chunks = __builtin_amdgcn_readlane(c, i);
-        L = __builtin_amdgcn_readlane(len, i);
-        break;
+    for (int b0 = 0, before = 0; b0 < p.B && b < 0; b0 += 64 * kPasses) {
+      if (p.B > 64 * kPasses) load_lengths(b0);
+#pragma unroll
+      for (int w = 0; w < kPasses; ++w) {
+        const int at = b0 + 64 * w;
+        if (b >= 0 || at >= p.B) continue;
+        const int c = lane_chunks(at, tl[w]);
+        const int incl = wave_scan(c);
+        const uint64_t past = __ballot((before + incl) * p.tiles_per_seq > item);
+        if (past) {
+          const int i = __ffsll((unsigned long long)past) - 1;
+          b = at + i;
+          first = (before + __builtin_amdgcn_readlane(incl - c, i)) * p.tiles_per_seq;
+          chunks = __builtin_amdgcn_readlane(c, i);
+          L = __builtin_amdgcn_readlane(len[w], i);
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
       }
-      before += __builtin_amdgcn_readlane(incl, 63);
     }
     if (b < 0) return;  // fewer chunks than the bound: the whole workgroup
     chunk = div_by(item - first, p.div_tps);
