@@ -217,8 +217,10 @@ kv4_kernel(Kv4Params a) {
     const int total = __builtin_amdgcn_readlane(wave_scan(sum), 63);
     top = wave_top(top);
     int share = div_by(total + a.groups - 1, a.div_groups);
-    // a longest sequence of more than one and a half times the mean length
-    if (a.halves && (int64_t)top * p.B * 2 > (int64_t)total * 3) share = (share + 1) / 2;
+    // a longest sequence of more than one and a half times the mean length, and of
+    // more than a share by an eighth (80 sequences of 1-8192 keys, 64/8 heads, none
+    // of which fills a share: halves 87 us, whole 81; 48 such: 49 and 53)
+    if (a.halves && (int64_t)top * p.B * 2 > (int64_t)total * 3 && top > share + share / 8) share = (share + 1) / 2;
     int per = max(max(share, 2 * W), (top + kChosenChunks - 1) / kChosenChunks);
     if (top <= 6 * W) per = top;
     per = max(2, (per + 1) & ~1);
