@@ -602,7 +602,8 @@ int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_ou
  *              where chunk states would reach 2 GiB, or for more than
  *              DA_ARRIVAL_BYTES / DA_ARRIVAL_STRIDE head tiles); <= 0: a chunk
  *              length chosen by the batch's lengths on the device, or for one
- *              sequence and short batches by L_K_max.  Every sequence is cut into
+ *              sequence, short ones and more than 1024 by L_K_max and the pool's
+ *              size.  Every sequence is cut into
  *              chunks of the same length, a multiple of 64 keys, so a shorter one
  *              has fewer, and one that fits a chunk writes its output directly
  *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, num_pages *
