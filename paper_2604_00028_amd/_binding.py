@@ -714,7 +714,8 @@ def _grown(dev: torch.device, handle: int, capture: int, nbytes: int) -> torch.T
 
 
 def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], dev: torch.device) -> None:
-    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+    # dev: a CUDA device (get_device: -1 on the CPU), and cheaper to compare by its number
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev.index or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {dev}, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
 
@@ -730,8 +731,9 @@ def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse_out: Optional[tor
 
 
 def _one_device(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
+    index = dev.index
     for t in tensors:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"the call's tensors must be on one device, got {dev} and {t.device}")
 
 
@@ -834,7 +836,7 @@ def _rows(name: str, t: torch.Tensor, dev: torch.device) -> Tuple[int, torch.Siz
     if len(shape) == 3:
         stride = t.stride()
         if ((stride[2] == 1 or shape[2] == 1) and (stride[1] == shape[2] or shape[1] == 1) and t.dtype is _BF16
-                and t.device == dev):
+                and t.get_device() == dev.index):
             return (stride[0] if shape[0] > 1 else 0), shape
     raise ValueError(f"{name} must be a bfloat16 tensor [N, heads, d] on {dev} whose heads are dense")
 
@@ -868,16 +870,19 @@ def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neigh
     if rope is None:
         positions = None
     else:
-        if rope.dim() != 2 or positions is None:
-            raise ValueError("rope must be [positions, rope_dim], and needs positions")
+        if rope.dim() != 2 or rope.numel() == 0 or positions is None:
+            raise ValueError("rope must be [positions, rope_dim], not empty, and needs positions")
         rope_rows, rope_dim = rope.shape
         _need("rope", rope, _F32, rope.shape, dev)
         _need("positions", positions, _I32, (N,), dev)
     if slots is not None:
         _need("slots", slots, _I32, (N,), dev)
-    return (_ptr(q), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _ptr(q_weight), _ptr(k_weight), eps,
-            _ptr(rope), rope_rows, rope_dim, 1 if neighbours else 0, _ptr(positions), _ptr(slots),
-            _ptr(q_out)), N, H_Q, H_KV, d, q_out
+    return (q.data_ptr() if H_Q and N else None, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
+            q_weight.data_ptr() if q_weight is not None else None,
+            k_weight.data_ptr() if k_weight is not None else None, eps,
+            rope.data_ptr() if rope is not None else None, rope_rows, rope_dim, 1 if neighbours else 0,
+            positions.data_ptr() if positions is not None else None, slots.data_ptr() if slots is not None else None,
+            q_out.data_ptr() if H_Q and N else None), N, H_Q, H_KV, d, q_out
 
 
 def da_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor],

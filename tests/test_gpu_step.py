@@ -313,3 +313,16 @@ def test_graphs_without_a_workspace(kind):
         for i in (1, 2) if turn == 0 else (0, 1, 2):
             check_attention(*outs[i], refs[i], f"{kind} turn {turn} call {i}")
     del graphs
+
+
+def test_empty_slices_and_an_empty_rotation_table():
+    z = lambda *s, t=torch.bfloat16: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+    qkv, cache = z(6, 12, 128), z(4, 2, 128)
+    say("empty slices")
+    q, k, v = qkv[2:2, :8], qkv[2:2, 8:10], qkv[2:2, 10:]
+    rope, none = z(9, 64, t=torch.float32), z(0, t=torch.int32)
+    out = da.da_append_kv(q, k, v, none, none, cache, cache.clone(), rope=rope)
+    torch.cuda.synchronize()
+    assert out.shape == (0, 8, 128) and not cache.any()
+    with pytest.raises(ValueError):  # not the same as no rotation
+        da.da_append_kv(qkv[:, :8], qkv[:, 8:10], qkv[:, 10:], z(6, t=torch.int32), None, cache, cache, rope=rope[:0])
