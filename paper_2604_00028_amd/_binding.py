@@ -738,7 +738,7 @@ def _one_device(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
 
 
 def da_window_keys(L_K_max: int, window: int, sinks: int = 0) -> int:
-    return int(load().da_window_keys(L_K_max, window, sinks))
+    return int(load().da_window_keys(L_K_max, min(window, INT_MAX), min(sinks, INT_MAX)))
 
 
 def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0,
@@ -759,7 +759,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
         if seq_lens is None or L_K_max is None:
             raise ValueError("seq_lens and L_K_max (the host-known longest sequence) are required with block_table")
         B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k, v, block_table, seq_lens)
-        L = int(L_K_max)
+        L = min(int(L_K_max), INT_MAX)
     _one_device(dev, k, v, cu_seqlens_k, block_table, seq_lens)
     if dev.index != _get_device():
         return _on_device(dev, da_decode_attn_window, q, k, v, window, sinks, cu_seqlens_k, block_table, seq_lens, out,
@@ -968,7 +968,8 @@ def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
 
 def da_kv4_workspace_bytes(B: int, H_Q: int, H_KV: int, L_K_max: int, pool_keys: int = 0, window: int = 0,
                            sinks: int = 0, num_splits: int = 0, num_cus: int = 0) -> int:
-    return int(load().da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, pool_keys, window, sinks, num_splits, num_cus))
+    return int(load().da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, pool_keys, min(window, INT_MAX),
+                                             min(sinks, INT_MAX), num_splits, num_cus))
 
 
 def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
@@ -996,7 +997,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
                           softmax_scale=softmax_scale, num_splits=num_splits, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
-    L = int(L_K_max)
+    L = min(int(L_K_max), INT_MAX)
     ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
         rc = load().da_decode_attn_kv4(q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),

@@ -256,3 +256,10 @@ def test_oracle_tables_give_every_page_once():
         used = [int(p) for b in range(B) for p in table[b, :-(-lens[b] // page)]]
         assert len(used) == len(set(used)) == taken and set(used) == set(free[:taken].tolist())
     assert taken > 190  # the list ran out on the way
+
+
+def test_windows_past_an_int_are_windows_over_everything():
+    assert da.da_window_keys(1000, 2 ** 40) == da.da_window_keys(1000, 2 ** 31 - 1) == 1000
+    assert da.da_window_keys(1000, 5, 2 ** 40) == 1000
+    sizes = [da.da_kv4_workspace_bytes(4, 64, 8, 4000, 0, w, s, 8, 256) for w, s in ((0, 0), (2 ** 40, 0), (5, 2 ** 33))]
+    assert sizes[0] > 0 and sizes[0] == sizes[1] == sizes[2]

@@ -326,3 +326,15 @@ def test_empty_slices_and_an_empty_rotation_table():
     assert out.shape == (0, 8, 128) and not cache.any()
     with pytest.raises(ValueError):  # not the same as no rotation
         da.da_append_kv(qkv[:, :8], qkv[:, 8:10], qkv[:, 10:], z(6, t=torch.int32), None, cache, cache, rope=rope[:0])
+
+
+def test_bounds_past_an_int_are_refused():
+    z = lambda *s, t=torch.bfloat16: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+    q, table, lens = z(1, 8, 128), z(1, 1, t=torch.int32), z(1, t=torch.int32)
+    say("bounds past an int")
+    for call in (lambda: da.da_decode_attn_kv4(q, z(1, 2, 1, 4352, t=torch.uint8), table, lens, 2 ** 32),
+                 lambda: da.da_decode_attn_window(q, z(1, 32, 2, 128), z(1, 32, 2, 128), 9, 0, None, table, lens,
+                                                  L_K_max=2 ** 32)):
+        with pytest.raises(bnd.DecodeAttnError) as e:
+            call()
+        assert e.value.code == bnd.DA_ERR_SHAPE
