@@ -21,6 +21,7 @@ HEAD_DIM = 128
 MAX_SPLITS = 64
 KV4_TILE_BYTES = 4352  # 32 keys of one KV head in the 4-bit cache
 MAX_REQUESTS = 4096    # of one da_extend_tables call
+MAX_NEW_TOKENS = 1 << 28  # rows of one
 ARRIVAL_BYTES = 1 << 20  # counters at the end of a workspace
 INT_MAX = 2 ** 31 - 1
 DEALT_MIN_KEYS = 2561  # da_prefers_dealt never holds for shorter batches: no need to ask
@@ -221,41 +222,48 @@ def da_device_info() -> Tuple[int, bool]:
 def da_choose_splits(B: int, H_Q: int, H_KV: int, L_K_max: int, d: int = HEAD_DIM, num_cus: int = 0,
                      cu_margin: int = 0, policy: int = POLICY_MI355X) -> DaPlan:
     plan = DaPlan()
-    _check(load().da_choose_splits(B, H_Q, H_KV, L_K_max, d, num_cus, cu_margin, policy, ctypes.byref(plan)))
+    _check(load().da_choose_splits(*map(_int, (B, H_Q, H_KV, L_K_max, d, num_cus, cu_margin, policy)),
+                                   ctypes.byref(plan)))
     return plan
 
 
 def da_model_time(policy: int, B: int, H_Q: int, H_KV: int, L_K: int, heads_per_tile: int, num_splits: int,
                   v_slices: int = 1, combine: int = 0, num_cus: int = 256) -> float:
     """The planner's modelled microseconds per call (-1 for no launch)."""
-    return float(load().da_model_time(policy, B, H_Q, H_KV, L_K, heads_per_tile, num_splits, v_slices, combine,
-                                      num_cus))
+    return float(load().da_model_time(*map(_int, (policy, B, H_Q, H_KV, L_K, heads_per_tile, num_splits, v_slices,
+                                                  combine, num_cus))))
 
 
 def da_make_plan(B: int, H_Q: int, H_KV: int, L_K_max: int, d: int = HEAD_DIM, num_splits: int = 0,
                  pack_gqa: int = -1, num_cus: int = 0, cu_margin: int = 0, policy: int = POLICY_MI355X) -> DaPlan:
     plan = DaPlan()
-    _check(load().da_make_plan(B, H_Q, H_KV, L_K_max, d, num_splits, pack_gqa, num_cus, cu_margin, policy,
+    _check(load().da_make_plan(*map(_int, (B, H_Q, H_KV, L_K_max, d, num_splits, pack_gqa, num_cus, cu_margin, policy)),
                                ctypes.byref(plan)))
     return plan
 
 
 def da_workspace_bytes(B: int, H_Q: int, d: int, num_splits: int) -> int:
-    return int(load().da_workspace_bytes(B, H_Q, d, num_splits))
+    return int(load().da_workspace_bytes(_int(B), _int(H_Q), _int(d), _int(num_splits)))
 
 
 def da_dealt_workspace_bytes(B: int, H_Q: int, H_KV: int, num_cus: int = 0) -> int:
-    return int(load().da_dealt_workspace_bytes(B, H_Q, H_KV, num_cus))
+    return int(load().da_dealt_workspace_bytes(_int(B), _int(H_Q), _int(H_KV), _int(num_cus)))
 
 
 def da_prefers_dealt(B: int, H_Q: int, H_KV: int, L_K_max: int, keys: int = 0, num_cus: int = 0) -> bool:
-    return bool(load().da_prefers_dealt(B, H_Q, H_KV, L_K_max, keys, num_cus))
+    return bool(load().da_prefers_dealt(_int(B), _int(H_Q), _int(H_KV), _int(L_K_max), keys, _int(num_cus)))
 
 
 def da_split_bounds(L: int, num_splits: int) -> List[int]:
-    cuts = (ctypes.c_int32 * (num_splits + 1))() if num_splits >= 0 else None
-    _check(load().da_split_bounds(L, num_splits, cuts))
+    cuts = (ctypes.c_int32 * (min(num_splits, MAX_SPLITS) + 1))() if num_splits >= 0 else None
+    _check(load().da_split_bounds(_int(L), _int(num_splits), cuts))
     return list(cuts)
+
+
+def _int(x: int) -> int:
+    """x as a C int: ctypes would wrap a number past it around to some other one,
+    where the largest is refused, or bounds as much."""
+    return x if -INT_MAX <= x <= INT_MAX else INT_MAX if x > 0 else -INT_MAX
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -324,7 +332,7 @@ def _shapes(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Optional[torc
         H_KV = k.shape[1]
         if L_K_max is None:
             raise ValueError("L_K_max (the host-known longest sequence) is required with cu_seqlens_k")
-    return B, H_Q, H_KV, int(L_K_max), d
+    return B, H_Q, H_KV, _int(int(L_K_max)), d
 
 
 _workspaces: Dict[Tuple[int, int], torch.Tensor] = {}
@@ -411,7 +419,7 @@ def da_decode_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens
     ws = _offered(workspace, dev, s_handle)
     while True:
         rc = load().da_decode_attn(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(out), _ptr(lse_out),
-                                   B, H_Q, H_KV, L, d, float(softmax_scale), int(num_splits), int(pack_gqa),
+                                   B, H_Q, H_KV, L, d, float(softmax_scale), _int(int(num_splits)), _int(int(pack_gqa)),
                                    _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
@@ -457,7 +465,8 @@ def da_decode_attn_noalloc(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     if out is None:
         out = _new_out(q)
     _check(load().da_decode_attn_noalloc(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(out), _ptr(lse_out),
-                                         B, H_Q, H_KV, L, d, float(softmax_scale), int(num_splits), int(pack_gqa),
+                                         B, H_Q, H_KV, L, d, float(softmax_scale), _int(int(num_splits)),
+                                         _int(int(pack_gqa)),
                                          _stream(q.device, stream)))
     return out
 
@@ -474,7 +483,7 @@ def _paged_args(q, k_cache, v_cache, block_table, seq_lens):
     num_pages, page_size, H_KV, dk = k_cache.shape
     if dk != d or block_table.dim() != 2 or block_table.shape[0] != B or seq_lens.numel() != B:
         raise ValueError("block_table must be [B, max_pages], seq_lens [B], and the head dims must agree")
-    return B, H_Q, H_KV, d, page_size, block_table.shape[1], num_pages
+    return B, H_Q, H_KV, d, page_size, _int(block_table.shape[1]), num_pages
 
 
 def da_decode_attn_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
@@ -488,19 +497,19 @@ def da_decode_attn_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     that pays, outside graph capture."""
     B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k_cache, v_cache, block_table, seq_lens)
     if (workspace is None and num_splits <= 0 and pack_gqa == -1 and L_K_max >= DEALT_MIN_KEYS and d == HEAD_DIM
-            and _deals(B, H_Q, H_KV, int(L_K_max), num_pages * page_size, q.device, stream)):
-        return da_decode_attn_dealt(q, k_cache, v_cache, int(L_K_max), None, block_table, seq_lens, out, lse_out,
+            and _deals(B, H_Q, H_KV, _int(int(L_K_max)), num_pages * page_size, q.device, stream)):
+        return da_decode_attn_dealt(q, k_cache, v_cache, L_K_max, None, block_table, seq_lens, out, lse_out,
                                     softmax_scale=softmax_scale, stream=stream)
     dev = q.device
     if out is None:
         out = _new_out(q)
     s_handle = _stream(dev, stream)
-    L = int(L_K_max)
+    L = _int(int(L_K_max))
     ws = _offered(workspace, dev, s_handle)
     while True:
         rc = load().da_decode_attn_paged(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
                                          _ptr(out), _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L,
-                                         d, float(softmax_scale), int(num_splits), int(pack_gqa), _ptr(ws),
+                                         d, float(softmax_scale), _int(int(num_splits)), _int(int(pack_gqa)), _ptr(ws),
                                          _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
@@ -528,13 +537,13 @@ def da_decode_attn_paged_planned(q: torch.Tensor, k_cache: torch.Tensor, v_cache
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().da_decode_attn_paged_planned(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
                                                _ptr(seq_lens), _ptr(out), _ptr(lse_out), B, H_Q, H_KV, page_size,
-                                               max_pages, num_pages, int(L_K_max), d, float(softmax_scale),
+                                               max_pages, num_pages, _int(int(L_K_max)), d, float(softmax_scale),
                                                ctypes.byref(plan), _ptr(workspace), ws_bytes, s_handle))
     return out
 
 
 def da_schedule_max_bytes(B: int, H_Q: int, H_KV: int, pack_gqa: int = -1) -> int:
-    return int(load().da_schedule_max_bytes(B, H_Q, H_KV, pack_gqa))
+    return int(load().da_schedule_max_bytes(_int(B), _int(H_Q), _int(H_KV), _int(pack_gqa)))
 
 
 def da_make_schedule(seq_lens: Sequence[int], H_Q: int, H_KV: int, L_K_max: Optional[int] = None,
@@ -550,9 +559,10 @@ def da_make_schedule(seq_lens: Sequence[int], H_Q: int, H_KV: int, L_K_max: Opti
     cap = da_schedule_max_bytes(B, H_Q, H_KV, pack_gqa)
     meta = torch.zeros(max(cap, 16), dtype=torch.uint8)
     sched = DaSchedule()
-    _check(load().da_make_schedule(lens.data_ptr() if B else None, B, H_Q, H_KV, int(L_K_max), d, pack_gqa,
-                                   num_cus, cu_margin, chunk_tiles, meta.data_ptr(), meta.numel(),
-                                   ctypes.byref(sched)))
+    _check(load().da_make_schedule(lens.data_ptr() if B else None,
+                                   *map(_int, (B, H_Q, H_KV, int(L_K_max), d, pack_gqa, num_cus, cu_margin,
+                                               chunk_tiles)),
+                                   meta.data_ptr(), meta.numel(), ctypes.byref(sched)))
     return sched, meta[: sched.meta_bytes].clone()
 
 
@@ -616,7 +626,7 @@ def da_decode_attn_dealt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, L_K_
         keys = k.shape[0]
     else:
         B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k, v, block_table, seq_lens)
-        L = int(L_K_max)
+        L = _int(int(L_K_max))
     dev = q.device
     if out is None:
         out = _new_out(q)
@@ -646,8 +656,8 @@ def da_split_partials(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     if l_part is None:
         l_part = torch.empty((num_splits, B, H_Q), dtype=torch.float32, device=dev)
     _check(load().da_split_partials(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(o_part), _ptr(m_part),
-                                    _ptr(l_part), B, H_Q, H_KV, L, d, float(softmax_scale), int(num_splits),
-                                    int(pack_gqa), _stream(dev, stream)))
+                                    _ptr(l_part), B, H_Q, H_KV, L, d, float(softmax_scale), _int(int(num_splits)),
+                                    _int(int(pack_gqa)), _stream(dev, stream)))
     return o_part, m_part, l_part
 
 
@@ -738,7 +748,7 @@ def _one_device(dev: torch.device, *tensors: Optional[torch.Tensor]) -> None:
 
 
 def da_window_keys(L_K_max: int, window: int, sinks: int = 0) -> int:
-    return int(load().da_window_keys(L_K_max, min(window, INT_MAX), min(sinks, INT_MAX)))
+    return int(load().da_window_keys(_int(L_K_max), _int(window), _int(sinks)))
 
 
 def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0,
@@ -751,7 +761,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
     its first `sinks` keys; returns `out`.  K and V as for da_decode_attn (fixed,
     or packed with cu_seqlens_k), or with block_table and seq_lens paged."""
     dev = q.device
-    window, sinks = min(window, INT_MAX), min(sinks, INT_MAX)
+    window, sinks, num_splits, pack_gqa = _int(window), _int(sinks), _int(num_splits), _int(pack_gqa)
     page_size = max_pages = num_pages = 0
     if block_table is None:
         B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
@@ -759,7 +769,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
         if seq_lens is None or L_K_max is None:
             raise ValueError("seq_lens and L_K_max (the host-known longest sequence) are required with block_table")
         B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k, v, block_table, seq_lens)
-        L = min(int(L_K_max), INT_MAX)
+        L = _int(int(L_K_max))
     _one_device(dev, k, v, cu_seqlens_k, block_table, seq_lens)
     if dev.index != _get_device():
         return _on_device(dev, da_decode_attn_window, q, k, v, window, sinks, cu_seqlens_k, block_table, seq_lens, out,
@@ -794,9 +804,10 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
     entries of new pages are written; slots and positions [max_tokens].
     lens_out may be lens and taken_out may be taken."""
     dev = lens.device
-    if lens.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2 or max_tokens < 0 or not lens.is_cuda:
+    if (lens.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2 or not 0 <= max_tokens <= MAX_NEW_TOKENS
+            or not lens.is_cuda):
         raise ValueError("lens and free_pages must have one dimension, block_table two, on the GPU, and max_tokens "
-                         "must not be negative")
+                         f"must be in [0, {MAX_NEW_TOKENS}]")
     B = lens.shape[0]
     num_free = free_pages.shape[0]
     max_pages = block_table.shape[1]
@@ -823,8 +834,8 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
         given = tuple(torch.empty(n, dtype=_I32, device=dev) if t is None else t for t, n in zip(given, sizes))
         ptrs = tuple(_ptr(t) for t in given)
     rc = load().da_extend_tables(lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(), taken.data_ptr(),
-                                 block_table.data_ptr(), *ptrs, B, page_size, max_pages, num_pages, num_free,
-                                 max_tokens, _stream(dev, stream))
+                                 block_table.data_ptr(), *ptrs, B, _int(page_size), _int(max_pages), _int(num_pages),
+                                 _int(num_free), max_tokens, _stream(dev, stream))
     if rc:
         _check(rc)
     return given if new is None else new.split_with_sizes(sizes)
@@ -968,8 +979,9 @@ def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
 
 def da_kv4_workspace_bytes(B: int, H_Q: int, H_KV: int, L_K_max: int, pool_keys: int = 0, window: int = 0,
                            sinks: int = 0, num_splits: int = 0, num_cus: int = 0) -> int:
-    return int(load().da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, pool_keys, min(window, INT_MAX),
-                                             min(sinks, INT_MAX), num_splits, num_cus))
+    return int(load().da_kv4_workspace_bytes(_int(B), _int(H_Q), _int(H_KV), _int(L_K_max),
+                                             max(0, min(pool_keys, 2 ** 63 - 1)), _int(window), _int(sinks),
+                                             _int(num_splits), _int(num_cus)))
 
 
 def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
@@ -985,11 +997,12 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
         raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")
     num_pages, H_KV, page_size = _kv4_cache(cache)
     B, H_Q, d = q.shape
-    window, sinks = min(window, INT_MAX), min(sinks, INT_MAX)
+    window, sinks, num_splits = _int(window), _int(sinks), _int(num_splits)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages]")
     max_pages = block_table.shape[1]
     _need("block_table", block_table, _I32, (B, max_pages), dev)
+    max_pages = _int(max_pages)
     _need("seq_lens", seq_lens, _I32, (B,), dev)
     _one_device(dev, cache)
     if dev.index != _get_device():
@@ -997,7 +1010,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
                           softmax_scale=softmax_scale, num_splits=num_splits, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out)
     s_handle = _stream(dev, stream)
-    L = min(int(L_K_max), INT_MAX)
+    L = _int(int(L_K_max))
     ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
         rc = load().da_decode_attn_kv4(q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),

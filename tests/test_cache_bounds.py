@@ -1,0 +1,47 @@
+"""Whole numbers past a 32-bit int in the calls of the cache operators, without a GPU: what a C int cannot
+hold is refused or counts as the largest int, and does not wrap around to some other number."""
+
+import pytest
+
+import paper_2604_00028_amd as da
+
+PAST = 2 ** 32  # wraps around to 0
+
+
+def test_window_keys():
+    assert da.da_window_keys(PAST, 5) == da.da_window_keys(2 ** 31 - 1, 5) == 64
+    assert da.da_window_keys(PAST + 5, 100) == 160
+    assert da.da_window_keys(-PAST + 5, 100) == -1
+    assert da.da_window_keys(100, -PAST + 5) == da.da_window_keys(100, 5, -PAST + 5) == -1
+
+
+def test_workspace_sizes():
+    size = lambda *a, **k: da.da_kv4_workspace_bytes(*a, num_cus=256, **k)  # noqa: E731
+    assert size(1, 64, 8, 2048, num_splits=4) > 0
+    assert size(1, 64, 8, PAST + 2048, num_splits=4) == 0    # no such length
+    assert size(1, 64, 8, 2048, num_splits=PAST + 4) == 0
+    assert size(1, 64, 8, 2048, window=-PAST + 2000, num_splits=4) == 0
+    assert size(1, 64, 8, 2048, sinks=-PAST, num_splits=4) == 0
+    assert size(PAST + 1, 64, 8, 2048, num_splits=4) == size(1, 64, PAST + 8, 2048, num_splits=4) == 0
+    # keys of a pool beyond 64 bits bound nothing
+    assert size(1, 64, 8, 30000, 2 ** 64 + 5) == size(1, 64, 8, 30000, 2 ** 63 - 1)
+    assert da.da_workspace_bytes(1, 64, 128, PAST + 4) == da.da_workspace_bytes(1, 64, 128, 2 ** 31 - 1)
+    assert da.da_dealt_workspace_bytes(PAST + 1, 64, 8, 256) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(L_K_max=PAST + 100), dict(num_splits=PAST + 1), dict(pack_gqa=PAST),
+                                dict(B=PAST + 1), dict(policy=PAST)])
+def test_plans(kw):
+    args = dict(B=1, H_Q=64, H_KV=8, L_K_max=512, num_cus=256)
+    da.da_make_plan(**args)
+    with pytest.raises(da.DecodeAttnError):
+        da.da_make_plan(**{**args, **kw})
+
+
+def test_schedules():
+    da.da_make_schedule([100, 200], 64, 8, 1000, num_cus=256)
+    for kw in (dict(L_K_max=PAST + 200), dict(pack_gqa=PAST), dict(cu_margin=PAST + 1)):
+        with pytest.raises(da.DecodeAttnError):
+            da.da_make_schedule([100, 200], 64, 8, **{"L_K_max": 1000, "num_cus": 256, **kw})
+    made = lambda c: da.da_make_schedule([100, 200], 64, 8, 1000, num_cus=256, chunk_tiles=c)[1].tolist()  # noqa: E731
+    assert made(-PAST + 1) == made(0) != made(1)  # no more than zero: chosen
