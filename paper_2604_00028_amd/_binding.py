@@ -295,8 +295,18 @@ def _capturing(dev: torch.device, stream) -> bool:
         return torch.cuda.is_current_stream_capturing()
 
 
-def _new_out(q: torch.Tensor) -> torch.Tensor:
-    return torch.empty_like(q, memory_format=torch.contiguous_format)
+def _fresh(dev: torch.device, stream, make):
+    """make(): new tensors for a call on `stream` (None: the current one) to write.
+    Of that stream's memory: a block of the current one's may be waiting for work
+    queued there, and would go to another tensor there while the call still runs."""
+    if stream is None or _stream(dev, stream) == _stream(dev, None):
+        return make()
+    with torch.cuda.stream(_on(dev, _stream(dev, stream))):
+        return make()
+
+
+def _new_out(q: torch.Tensor, stream) -> torch.Tensor:
+    return _fresh(q.device, stream, lambda: torch.empty_like(q, memory_format=torch.contiguous_format))
 
 
 def _bf16_cuda(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, names=("q", "k", "v")) -> None:
@@ -414,7 +424,7 @@ def da_decode_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens
                                     stream=stream)
     dev = q.device
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     s_handle = _stream(dev, stream)
     ws = _offered(workspace, dev, s_handle)
     while True:
@@ -439,7 +449,7 @@ def da_decode_attn_planned(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pl
     B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
     dev = q.device
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     s_handle = _stream(dev, stream)
     if workspace is None:
         nbytes = da_workspace_bytes(B, H_Q, d, plan.num_splits)
@@ -463,7 +473,7 @@ def da_decode_attn_noalloc(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     nothing at all."""
     B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     _check(load().da_decode_attn_noalloc(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(out), _ptr(lse_out),
                                          B, H_Q, H_KV, L, d, float(softmax_scale), _int(int(num_splits)),
                                          _int(int(pack_gqa)),
@@ -502,7 +512,7 @@ def da_decode_attn_paged(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
                                     softmax_scale=softmax_scale, stream=stream)
     dev = q.device
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     s_handle = _stream(dev, stream)
     L = _int(int(L_K_max))
     ws = _offered(workspace, dev, s_handle)
@@ -528,7 +538,7 @@ def da_decode_attn_paged_planned(q: torch.Tensor, k_cache: torch.Tensor, v_cache
     B, H_Q, H_KV, d, page_size, max_pages, num_pages = _paged_args(q, k_cache, v_cache, block_table, seq_lens)
     dev = q.device
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     s_handle = _stream(dev, stream)
     if workspace is None:
         nbytes = da_workspace_bytes(B, H_Q, d, plan.num_splits)
@@ -595,7 +605,7 @@ def da_decode_attn_scheduled(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
         max_pages = block_table.shape[1]
     dev = q.device
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     s_handle = _stream(dev, stream)
     if workspace is None:
         nbytes = da_schedule_workspace_bytes(sched)
@@ -629,7 +639,7 @@ def da_decode_attn_dealt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, L_K_
         L = _int(int(L_K_max))
     dev = q.device
     if out is None:
-        out = _new_out(q)
+        out = _new_out(q, stream)
     s_handle = _stream(dev, stream)
     if workspace is None:
         workspace = workspace_for(dev, s_handle, da_dealt_workspace_bytes(B, H_Q, H_KV))
@@ -649,12 +659,13 @@ def da_split_partials(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     """Per-chunk partial states (o_part [s,B,H_Q,d], m_part, l_part [s,B,H_Q])."""
     B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
     dev = q.device
+    new = lambda *shape: _fresh(dev, stream, lambda: torch.empty(shape, dtype=torch.float32, device=dev))  # noqa: E731
     if o_part is None:
-        o_part = torch.empty((num_splits, B, H_Q, d), dtype=torch.float32, device=dev)
+        o_part = new(num_splits, B, H_Q, d)
     if m_part is None:
-        m_part = torch.empty((num_splits, B, H_Q), dtype=torch.float32, device=dev)
+        m_part = new(num_splits, B, H_Q)
     if l_part is None:
-        l_part = torch.empty((num_splits, B, H_Q), dtype=torch.float32, device=dev)
+        l_part = new(num_splits, B, H_Q)
     _check(load().da_split_partials(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(o_part), _ptr(m_part),
                                     _ptr(l_part), B, H_Q, H_KV, L, d, float(softmax_scale), _int(int(num_splits)),
                                     _int(int(pack_gqa)), _stream(dev, stream)))
@@ -673,7 +684,7 @@ def da_combine_splits(o_part: torch.Tensor, m_part: torch.Tensor, l_part: torch.
         raise ValueError("m_part and l_part must be [s, B, H_Q]")
     dev = o_part.device
     if out is None:
-        out = torch.empty((B, H_Q, d), dtype=torch.bfloat16, device=dev)
+        out = _fresh(dev, stream, lambda: torch.empty((B, H_Q, d), dtype=torch.bfloat16, device=dev))
     _check(load().da_combine_splits(_ptr(o_part), _ptr(m_part), _ptr(l_part), _ptr(out), _ptr(lse_out), s, B, H_Q,
                                     d, _stream(dev, stream)))
     return out
@@ -730,9 +741,10 @@ def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...]
                          f"{tuple(t.shape)} on {t.device}")
 
 
-def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse_out: Optional[torch.Tensor]) -> torch.Tensor:
+def _outputs(q: torch.Tensor, out: Optional[torch.Tensor], lse_out: Optional[torch.Tensor], stream) -> torch.Tensor:
     if out is None:
-        out = torch.empty_like(q)  # q is contiguous
+        # q is contiguous
+        out = torch.empty_like(q) if stream is None else _new_out(q, stream)
     else:
         _need("out", out, _BF16, q.shape, q.device)
     if lse_out is not None:
@@ -775,7 +787,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
         return _on_device(dev, da_decode_attn_window, q, k, v, window, sinks, cu_seqlens_k, block_table, seq_lens, out,
                           lse_out, L_K_max=L_K_max, softmax_scale=softmax_scale, num_splits=num_splits,
                           pack_gqa=pack_gqa, workspace=workspace, stream=stream)
-    out = _outputs(q, out, lse_out)
+    out = _outputs(q, out, lse_out, stream)
     s_handle = _stream(dev, stream)
     ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
@@ -824,14 +836,16 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
     given = (lens_out, taken_out, cu_new, slots, positions)
     new = None
     if not any(t is not None for t in given):
-        new = torch.empty(2 * B + 2 + 2 * max_tokens, dtype=_I32, device=dev)
+        new = _fresh(dev, stream, lambda: torch.empty(2 * B + 2 + 2 * max_tokens, dtype=_I32, device=dev))
         at = new.data_ptr()
         ptrs = (at, at + 4 * B, at + 4 * B + 4, at + 8 * B + 8, at + 8 * B + 8 + 4 * max_tokens)
     else:
         for name, t, n in zip(("lens_out", "taken_out", "cu_new", "slots", "positions"), given, sizes):
             if t is not None:
                 _need(name, t, _I32, (n,), dev)
-        given = tuple(torch.empty(n, dtype=_I32, device=dev) if t is None else t for t, n in zip(given, sizes))
+        mine = given
+        given = _fresh(dev, stream, lambda: tuple(torch.empty(n, dtype=_I32, device=dev) if t is None else t
+                                                  for t, n in zip(mine, sizes)))
         ptrs = tuple(_ptr(t) for t in given)
     rc = load().da_extend_tables(lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(), taken.data_ptr(),
                                  block_table.data_ptr(), *ptrs, B, _int(page_size), _int(max_pages), _int(num_pages),
@@ -852,7 +866,7 @@ def _rows(name: str, t: torch.Tensor, dev: torch.device) -> Tuple[int, torch.Siz
     raise ValueError(f"{name} must be a bfloat16 tensor [N, heads, d] on {dev} whose heads are dense")
 
 
-def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours, q_out):
+def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours, q_out, stream):
     """Check what the append calls share; (their leading arguments, N, H_Q, H_KV, d, q_out)."""
     dev = k.device
     if not k.is_cuda:
@@ -869,7 +883,7 @@ def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neigh
         if q_shape[0] != N or q_shape[2] != d:
             raise ValueError("q must be [N, H_Q, d] with k's N and d")
         if q_out is None:
-            q_out = torch.empty(q_shape, dtype=_BF16, device=dev)
+            q_out = _fresh(dev, stream, lambda: torch.empty(q_shape, dtype=_BF16, device=dev))
         else:
             _need("q_out", q_out, _BF16, q_shape, dev)
     elif q_out is not None:
@@ -911,7 +925,7 @@ def da_append_kv(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, po
         return _on_device(dev, da_append_kv, q, k, v, positions, slots, k_cache, v_cache, rope=rope, q_weight=q_weight,
                           k_weight=k_weight, eps=eps, neighbours=neighbours, q_out=q_out, stream=stream)
     args, N, H_Q, H_KV, d, q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
-                                                q_out)
+                                                q_out, stream)
     shape = k_cache.shape
     if len(shape) < 3 or shape[-2] != H_KV or shape[-1] != d:
         raise ValueError("k_cache must be [..., H_KV, d]")
@@ -944,7 +958,7 @@ def da_append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, p
         return _on_device(dev, da_append_kv4, q, k, v, positions, slots, cache, rope=rope, q_weight=q_weight,
                           k_weight=k_weight, eps=eps, neighbours=neighbours, q_out=q_out, stream=stream)
     args, N, H_Q, H_KV, d, q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
-                                                q_out)
+                                                q_out, stream)
     num_pages, heads, page_size = _kv4_cache(cache)
     if heads != H_KV:
         raise ValueError(f"the cache has {heads} KV heads, k {H_KV}")
@@ -969,7 +983,7 @@ def da_read_kv4(cache: torch.Tensor, slots: Optional[torch.Tensor] = None, *,
         _need("slots", slots, _I32, (N,), dev)
     if dev.index != _get_device():
         return _on_device(dev, da_read_kv4, cache, slots, stream=stream)
-    k, v = torch.empty((2, N, H_KV, HEAD_DIM), dtype=_BF16, device=dev).unbind(0)
+    k, v = _fresh(dev, stream, lambda: torch.empty((2, N, H_KV, HEAD_DIM), dtype=_BF16, device=dev)).unbind(0)
     rc = load().da_read_kv4(cache.data_ptr(), _ptr(slots), k.data_ptr(), v.data_ptr(), N, H_KV, page_size, num_pages,
                             HEAD_DIM, _stream(dev, stream))
     if rc:
@@ -1008,7 +1022,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
     if dev.index != _get_device():
         return _on_device(dev, da_decode_attn_kv4, q, cache, block_table, seq_lens, L_K_max, window, sinks, out, lse_out,
                           softmax_scale=softmax_scale, num_splits=num_splits, workspace=workspace, stream=stream)
-    out = _outputs(q, out, lse_out)
+    out = _outputs(q, out, lse_out, stream)
     s_handle = _stream(dev, stream)
     L = _int(int(L_K_max))
     ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)

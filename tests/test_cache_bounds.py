@@ -1,9 +1,11 @@
-"""Whole numbers past a 32-bit int in the calls of the cache operators, without a GPU: what a C int cannot
+"""The binding without a GPU.  Whole numbers past a 32-bit int: what a C int cannot
 hold is refused or counts as the largest int, and does not wrap around to some other number."""
 
 import pytest
+import torch
 
 import paper_2604_00028_amd as da
+from paper_2604_00028_amd import _binding as bnd
 
 PAST = 2 ** 32  # wraps around to 0
 
@@ -45,3 +47,26 @@ def test_schedules():
             da.da_make_schedule([100, 200], 64, 8, **{"L_K_max": 1000, "num_cus": 256, **kw})
     made = lambda c: da.da_make_schedule([100, 200], 64, 8, 1000, num_cus=256, chunk_tiles=c)[1].tolist()  # noqa: E731
     assert made(-PAST + 1) == made(0) != made(1)  # no more than zero: chosen
+
+
+def test_new_outputs_come_from_the_memory_of_the_calls_stream(monkeypatch):
+    """A block of the current stream's memory may be waiting for work that is queued there."""
+    entered = []
+
+    class On:
+        def __init__(self, handle):
+            self.handle = handle
+
+        def __enter__(self):
+            entered.append(self.handle)
+
+        def __exit__(self, *exc):
+            entered.append(None)
+
+    monkeypatch.setattr(bnd, "_stream", lambda dev, stream: 5 if stream is None else stream)
+    monkeypatch.setattr(bnd, "_on", lambda dev, handle: handle)
+    monkeypatch.setattr(bnd.torch.cuda, "stream", On)
+    q = torch.ones(2, 3)
+    for stream, want in ((None, []), (5, []), (7, [7, None]), (0, [0, None])):
+        entered.clear()
+        assert bnd._new_out(q, stream).shape == (2, 3) and entered == want

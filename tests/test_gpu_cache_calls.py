@@ -7,7 +7,7 @@ import torch
 
 import paper_2604_00028_amd as da
 from paper_2604_00028_amd import _binding as bnd
-from tests.cache_helpers import Batch
+from tests.cache_helpers import Batch, normal_bits
 from tests.gpu_helpers import say, to_dev
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +63,68 @@ def test_tables_past_an_int():
     for rows in (PAST + 8, 2 ** 28 + 1, -1):
         with pytest.raises(ValueError):
             tables(16, 9, rows)
+
+
+def calls_with_outputs():
+    """name -> call(stream): entry points that make their own outputs, over inputs that stay."""
+    rng = np.random.default_rng(3)
+    packed, paged, four = (Batch([3000, 200, 1], 8, 2, layout, seed=3) for layout in ("packed", "paged", "kv4"))
+    q, k, v, cu = to_dev(packed.q), to_dev(packed.k), to_dev(packed.v), torch.from_numpy(packed.cu).cuda()
+    pk, pv, table, lens = to_dev(paged.k), to_dev(paged.v), torch.from_numpy(paged.table).cuda(), paged.seq_lens()
+    cache, table4 = torch.from_numpy(four.cache).cuda(), torch.from_numpy(four.table).cuda()
+    x = to_dev(normal_bits(rng, (40, 12, 128)))
+    parts = x[:, :8], x[:, 8:10], x[:, 10:]
+    rows = torch.zeros(2, 64, 2, 128, dtype=torch.bfloat16, device="cuda")
+    spare = torch.zeros(2, 2, 1, 4352, dtype=torch.uint8, device="cuda")
+    tables = [torch.tensor(t, dtype=torch.int32, device="cuda") for t in ([5, 9], [30, 2], [3, 1, 0, 2], [0])]
+    entries, cu_new = ints(2, 4), ints(3)
+    L = 3000
+    states = lambda s: da.da_split_partials(q, k, v, cu, num_splits=4, pack_gqa=1, L_K_max=L, stream=s)  # noqa: E731
+    held = states(None)
+    plan = da.da_make_plan(3, 8, 2, L, num_splits=4)
+    sched, meta = da.da_make_schedule(packed.lengths, 8, 2)
+    meta = meta.cuda()
+    return {
+        "tables": lambda s: da.da_extend_tables(*tables, entries, 16, 9, 40, stream=s),
+        "tables, some given": lambda s: da.da_extend_tables(*tables, entries, 16, 9, 40, cu_new=cu_new, stream=s),
+        "append": lambda s: da.da_append_kv(*parts, None, None, *rows, stream=s),
+        "append4": lambda s: da.da_append_kv4(*parts, None, None, spare, stream=s),
+        "read4": lambda s: da.da_read_kv4(cache, stream=s),
+        "window": lambda s: da.da_decode_attn_window(q, pk, pv, 500, 4, None, table, lens, L_K_max=L, stream=s),
+        "kv4": lambda s: da.da_decode_attn_kv4(q, cache, table4, lens, L, stream=s),
+        "plain": lambda s: da.da_decode_attn(q, k, v, cu, L_K_max=L, num_splits=4, stream=s),
+        "planned": lambda s: da.da_decode_attn_planned(q, k, v, plan, cu, L_K_max=L, stream=s),
+        "noalloc": lambda s: da.da_decode_attn_noalloc(q, k, v, cu, L_K_max=L, stream=s),
+        "paged": lambda s: da.da_decode_attn_paged(q, pk, pv, table, lens, L, num_splits=4, stream=s),
+        "paged planned": lambda s: da.da_decode_attn_paged_planned(q, pk, pv, table, lens, L, plan, stream=s),
+        "dealt": lambda s: da.da_decode_attn_dealt(q, k, v, L, cu, stream=s),
+        "scheduled": lambda s: da.da_decode_attn_scheduled(q, k, v, sched, meta, cu, stream=s),
+        "partials": states,
+        "merge": lambda s: da.da_combine_splits(*held, stream=s),
+    }
+
+
+def test_outputs_of_calls_on_another_stream():
+    """Memory that the current stream has freed, but whose last work it still has to do, is none for the
+    outputs of a call on another stream."""
+    side = torch.cuda.Stream()
+    a = torch.randn(8192, 8192, device="cuda").bfloat16()
+    product = torch.empty_like(a)
+    for name, call in calls_with_outputs().items():
+        say(f"own outputs on another stream: {name}")
+        listed = lambda out: list(out) if isinstance(out, (tuple, list)) else [out]  # noqa: E731
+        torch.mm(a, a, out=product)
+        call(side)  # its workspace, which waits for the current stream where it is new
+        torch.cuda.synchronize()
+        want = [t.clone() for t in listed(call(None))]
+        freed = [torch.empty_like(t) for t in want]
+        torch.cuda.synchronize()
+        for _ in range(20):  # some 15 ms
+            torch.mm(a, a, out=product)
+        for t in freed:
+            t.fill_(7)
+        del freed, t
+        got = listed(call(side))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g, w), name
