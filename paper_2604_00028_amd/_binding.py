@@ -394,7 +394,14 @@ def _offered(workspace: Optional[torch.Tensor], dev: torch.device, s_handle: int
     caller's, or the one cached for this stream as it is.  Only where the plan
     needs a larger one, which the entry point finds before it launches
     anything, is the plan made here too and the cached one grown."""
-    return workspace if workspace is not None else _workspaces.get((dev.index, s_handle))
+    return _usable(workspace, dev) if workspace is not None else _workspaces.get((dev.index, s_handle))
+
+
+def _usable(workspace: torch.Tensor, dev: torch.device) -> torch.Tensor:
+    """A caller's workspace, whose bytes a kernel on `dev` may write from its address on."""
+    if workspace.get_device() != dev.index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {dev}, got one on {workspace.device}")
+    return workspace
 
 
 def _nbytes(t: Optional[torch.Tensor]) -> int:
@@ -455,6 +462,8 @@ def da_decode_attn_planned(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pl
         nbytes = da_workspace_bytes(B, H_Q, d, plan.num_splits)
         if nbytes:
             workspace = workspace_for(dev, s_handle, nbytes)
+    else:
+        _usable(workspace, dev)
     ws_ptr = _ptr(workspace)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().da_decode_attn_planned(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(out), _ptr(lse_out),
@@ -544,6 +553,8 @@ def da_decode_attn_paged_planned(q: torch.Tensor, k_cache: torch.Tensor, v_cache
         nbytes = da_workspace_bytes(B, H_Q, d, plan.num_splits)
         if nbytes:
             workspace = workspace_for(dev, s_handle, nbytes)
+    else:
+        _usable(workspace, dev)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().da_decode_attn_paged_planned(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
                                                _ptr(seq_lens), _ptr(out), _ptr(lse_out), B, H_Q, H_KV, page_size,
@@ -611,6 +622,8 @@ def da_decode_attn_scheduled(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
         nbytes = da_schedule_workspace_bytes(sched)
         if nbytes:
             workspace = workspace_for(dev, s_handle, nbytes)
+    else:
+        _usable(workspace, dev)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(load().da_decode_attn_scheduled(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(block_table),
                                            _ptr(seq_lens), page_size, max_pages, num_pages, _ptr(out),
@@ -643,6 +656,8 @@ def da_decode_attn_dealt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, L_K_
     s_handle = _stream(dev, stream)
     if workspace is None:
         workspace = workspace_for(dev, s_handle, da_dealt_workspace_bytes(B, H_Q, H_KV))
+    else:
+        _usable(workspace, dev)
     ws_bytes = workspace.numel() * workspace.element_size()
     _check(load().da_decode_attn_dealt(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens_k), _ptr(block_table),
                                        _ptr(seq_lens), page_size, max_pages, num_pages, _ptr(out), _ptr(lse_out),
@@ -789,7 +804,7 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
                           pack_gqa=pack_gqa, workspace=workspace, stream=stream)
     out = _outputs(q, out, lse_out, stream)
     s_handle = _stream(dev, stream)
-    ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
+    ws, capture = (_usable(workspace, dev), 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
         rc = load().da_decode_attn_window(
             q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(cu_seqlens_k), _ptr(block_table), _ptr(seq_lens), page_size,
@@ -1025,7 +1040,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
     out = _outputs(q, out, lse_out, stream)
     s_handle = _stream(dev, stream)
     L = _int(int(L_K_max))
-    ws, capture = (workspace, 0) if workspace is not None else _offered_now(dev, stream, s_handle)
+    ws, capture = (_usable(workspace, dev), 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
         rc = load().da_decode_attn_kv4(q.data_ptr(), cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
                                        out.data_ptr(), _ptr(lse_out), B, H_Q, H_KV, page_size, max_pages, num_pages, L, d,

@@ -1,6 +1,8 @@
 """The binding without a GPU.  Whole numbers past a 32-bit int: what a C int cannot
 hold is refused or counts as the largest int, and does not wrap around to some other number."""
 
+from types import SimpleNamespace
+
 import pytest
 import torch
 
@@ -70,3 +72,15 @@ def test_new_outputs_come_from_the_memory_of_the_calls_stream(monkeypatch):
     for stream, want in ((None, []), (5, []), (7, [7, None]), (0, [0, None])):
         entered.clear()
         assert bnd._new_out(q, stream).shape == (2, 3) and entered == want
+
+
+def test_a_workspace_is_checked_before_its_address_is_taken():
+    """Memory the GPU cannot reach, or bytes that do not lie side by side, are no workspace."""
+    dev = torch.device("cuda", 0)
+    on = lambda device, contiguous=True: SimpleNamespace(  # noqa: E731
+        device=device, get_device=lambda: -1 if device.index is None else device.index,
+        is_contiguous=lambda: contiguous)
+    bnd._usable(on(dev), dev)
+    for ws in (torch.zeros(64, dtype=torch.uint8), on(torch.device("cuda", 1)), on(dev, contiguous=False)):
+        with pytest.raises(ValueError):
+            bnd._usable(ws, dev)

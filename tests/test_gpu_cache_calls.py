@@ -128,3 +128,18 @@ def test_outputs_of_calls_on_another_stream():
         torch.cuda.synchronize()
         for g, w in zip(got, want):
             assert torch.equal(g, w), name
+
+
+def test_a_workspace_the_gpu_cannot_write_is_refused():
+    batch, four = Batch([3000, 200], 8, 2, "packed", seed=4), Batch([3000, 200], 8, 2, "kv4", seed=4)
+    q, k, v, cu = to_dev(batch.q), to_dev(batch.k), to_dev(batch.v), torch.from_numpy(batch.cu).cuda()
+    plan = da.da_make_plan(2, 8, 2, 3000, num_splits=4)
+    for ws in (torch.zeros(8 << 20, dtype=torch.uint8), torch.zeros(16 << 20, dtype=torch.uint8, device="cuda")[::2]):
+        say(f"workspace on {ws.device}, contiguous {ws.is_contiguous()}")
+        for call in (lambda: batch.call_window(da, 2000, 4, num_splits=4, workspace=ws),
+                     lambda: four.call_kv4(da, num_splits=4, workspace=ws),
+                     lambda: da.da_decode_attn(q, k, v, cu, L_K_max=3000, num_splits=4, workspace=ws),
+                     lambda: da.da_decode_attn_planned(q, k, v, plan, cu, L_K_max=3000, workspace=ws),
+                     lambda: da.da_decode_attn_dealt(q, k, v, 3000, cu, workspace=ws)):
+            with pytest.raises(ValueError):
+                call()
