@@ -790,6 +790,8 @@ def da_decode_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, win
     dev = q.device
     window, sinks, num_splits, pack_gqa = _int(window), _int(sinks), _int(num_splits), _int(pack_gqa)
     page_size = max_pages = num_pages = 0
+    if (cu_seqlens_k if block_table is not None else seq_lens) is not None:
+        raise ValueError("seq_lens are the lengths of a paged batch (block_table), cu_seqlens_k those of a packed one")
     if block_table is None:
         B, H_Q, H_KV, L, d = _shapes(q, k, v, cu_seqlens_k, L_K_max)
     else:

@@ -143,3 +143,17 @@ def test_a_workspace_the_gpu_cannot_write_is_refused():
                      lambda: da.da_decode_attn_dealt(q, k, v, 3000, cu, workspace=ws)):
             with pytest.raises(ValueError):
                 call()
+
+
+def test_lengths_of_another_layout_are_refused():
+    """A padded dense batch with seq_lens would be attended to its full length, a paged one with
+    cu_seqlens_k by its seq_lens."""
+    dense, paged = Batch([64, 64], 8, 2, "dense", seed=5), Batch([64, 30], 8, 2, "paged", seed=5)
+    cu = torch.tensor([0, 64, 94], dtype=torch.int32, device="cuda")
+    say("lengths of another layout")
+    dense.call_window(da, 50, 4)
+    paged.call_window(da, 50, 4)
+    with pytest.raises(ValueError):
+        dense.call_window(da, 50, 4, seq_lens=paged.seq_lens())
+    with pytest.raises(ValueError):
+        paged.call_window(da, 50, 4, cu_seqlens_k=cu)
