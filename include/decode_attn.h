@@ -615,7 +615,8 @@ int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_ou
  * lengths of the whole batch.  A NaN among the visible keys, or an infinity or a
  * NaN in a query, makes the output and lse of the heads that read it NaN.
  * Other arguments and errors as for da_decode_attn_paged, and DA_ERR_SHAPE for
- * pages of 4 GiB or 2^24 head tiles and more. */
+ * pages of 4 GiB, 2^24 head tiles and more, or L_K_max above 2^30; no other limit
+ * on a sequence's length (its keys are addressed by page). */
 int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* seq_lens,
                        void* out, float* lse_out, int B, int H_Q, int H_KV, int page_size, int max_pages,
                        int num_pages, int L_K_max, int d, float softmax_scale, int window, int sinks,

@@ -579,6 +579,18 @@ Kv4Plan kv4_plan(int B, int H_Q, int H_KV, int keys, int64_t pool, int num_split
   return pl;
 }
 
+// Shape checks (no HIP calls).  Heads as for the bf16 layouts; their limit on a
+// sequence's bytes is one of 32-bit offsets into it, and this cache is addressed
+// by page: positions of a few thousand keys past a sequence have to fit an int.
+constexpr int kMostKeys = 1 << 30;
+
+int check_kv4_shape(int B, int H_Q, int H_KV, int L_K_max, int d) {
+  const int rc = da::check_shape(B, H_Q, H_KV, std::min(L_K_max, 0), d);
+  if (rc) return rc;
+  if (L_K_max > kMostKeys) return da::fail(DA_ERR_SHAPE, "L_K_max=%d exceeds %d keys", L_K_max, kMostKeys);
+  return DA_OK;
+}
+
 int kv4_keys(int L_K_max, int window, int sinks) {
   return window > 0 ? da::window_keys(L_K_max, window, sinks) : L_K_max;
 }
@@ -589,7 +601,7 @@ extern "C" {
 
 size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t pool_keys, int window, int sinks,
                               int num_splits, int num_cus) {
-  if (da::check_shape(B, H_Q, H_KV, L_K_max, D) || window < 0 || sinks < 0 || num_splits > DA_MAX_SPLITS) return 0;
+  if (check_kv4_shape(B, H_Q, H_KV, L_K_max, D) || window < 0 || sinks < 0 || num_splits > DA_MAX_SPLITS) return 0;
   if (num_cus <= 0 && ensure_gfx950(&num_cus)) return 0;
   const Kv4Plan pl = kv4_plan(B, H_Q, H_KV, kv4_keys(L_K_max, window, sinks),
                                pool_keys > 0 ? pool_keys : 1, num_splits, num_cus);
@@ -601,7 +613,7 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
                        int L_K_max, int d, float softmax_scale, int window, int sinks, int num_splits, void* workspace,
                        size_t workspace_bytes, void* stream) {
   da::clear_error();
-  int rc = da::check_shape(B, H_Q, H_KV, L_K_max, d);
+  int rc = check_kv4_shape(B, H_Q, H_KV, L_K_max, d);
   if (!q) return da::fail(DA_ERR_NULL, "q must be non-NULL");
   if (!block_table || !seq_lens) return da::fail(DA_ERR_NULL, "block_table and seq_lens must be non-NULL");
   if (!cache && !(rc == DA_OK && L_K_max == 0)) return da::fail(DA_ERR_NULL, "cache must be non-NULL");

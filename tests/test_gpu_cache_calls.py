@@ -6,8 +6,10 @@ import pytest
 import torch
 
 import paper_2604_00028_amd as da
+from oracle import bf16_bits_to_f64
+from oracle.cache import kv4_unpack
 from paper_2604_00028_amd import _binding as bnd
-from tests.cache_helpers import Batch, normal_bits
+from tests.cache_helpers import Batch, check_attention, normal_bits
 from tests.gpu_helpers import say, to_dev
 
 pytestmark = pytest.mark.gpu
@@ -157,3 +159,33 @@ def test_lengths_of_another_layout_are_refused():
         dense.call_window(da, 50, 4, seq_lens=paged.seq_lens())
     with pytest.raises(ValueError):
         paged.call_window(da, 50, 4, cu_seqlens_k=cu)
+
+
+@pytest.mark.parametrize("H_Q,H_KV,L", [(16, 8, (1 << 20) + 77), (16, 16, (1 << 19) + 1), (8, 1, (1 << 23) + 40)])
+def test_four_bit_sequences_of_two_gib_of_bf16_keys_and_more(H_Q, H_KV, L):
+    """The 4-bit cache is addressed by page, so no product of length and heads bounds it.  The sequence is one page
+    of distinct keys again and again: each counts as often as it comes, in the sums and in the log-sum-exp.
+
+    At most 1024 steps of 64 keys a wave, whose sums take one rounding of 2^-24 a step (2^-14 of l) and the outputs
+    two (2^-13 of the weighted mean of |v|): within what check_attention allows (2^-13 of lse, 2^-12)."""
+    page = 512
+    batch = Batch([page], H_Q, H_KV, "kv4", page=page, seed=H_KV, max_pages=1)
+    k, v = (x[batch.rows[0]] for x in kv4_unpack(batch.cache))
+    pages = -(-L // page)
+    table = torch.full((1, pages), int(batch.table[0, 0]), dtype=torch.int32, device="cuda")
+    lens = torch.tensor([L], dtype=torch.int32, device="cuda")
+    q, cache = to_dev(batch.q), torch.from_numpy(batch.cache).cuda()
+    times = np.where(np.arange(page) < L % page, L // page + 1, L // page).astype(np.float64)
+    s = np.einsum("hd,khd->hk", bf16_bits_to_f64(batch.q)[0], k.repeat(H_Q // H_KV, 1)) / np.sqrt(128.0)
+    top = s.max(1, keepdims=True)
+    p = np.exp(s - top) * times
+    lse = (top[:, 0] + np.log(p.sum(1)))[None]
+    p /= p.sum(1, keepdims=True)
+    v = v.repeat(H_Q // H_KV, 1)
+    ref = np.einsum("hk,khd->hd", p, v)[None], lse, np.einsum("hk,khd->hd", p, np.abs(v))[None]
+    for splits in (0, 64):
+        got = torch.empty(1, H_Q, dtype=torch.float32, device="cuda")
+        say(f"long 4-bit sequence {H_Q}/{H_KV} L={L} splits={splits}")
+        out = da.da_decode_attn_kv4(q, cache, table, lens, L, lse_out=got, num_splits=splits)
+        torch.cuda.synchronize()
+        check_attention(out, got, ref, f"{H_Q}/{H_KV} L={L}")
