@@ -520,12 +520,17 @@ int da_window_keys(int L_K_max, int window, int sinks);
  *   positions      NULL or int32 [max_tokens]: the token's position in its
  *                  sequence; 0 past the last token
  * A request is not extended (as a whole) where its table row could not hold
- * the keys, its rows would pass max_tokens, or the list does not hold the
- * pages that it and the extended requests before it need; later ones that need
- * no page are extended all the same.  lens_out may be lens and taken_out may
- * be taken (a state advanced in place by a captured step); no other output may
- * overlap an input.  Lengths and their sums count as 2^30 beyond that.  One
- * launch; two where outputs take their inputs' place and max_tokens > 2048.
+ * the keys, its rows would pass max_tokens, or pages run out: they are given in
+ * request order, and from the first request on for which the list does not hold
+ * the pages it needs, no request gets one, also not one that needs fewer.
+ * Requests that need no page are extended all the same, and one that does
+ * not fit its row or max_tokens takes none.  (A caller that would rather serve the
+ * requests behind a large one puts it last, or leaves it for another call.)
+ * lens_out may be lens and taken_out may be taken (a state advanced in place by
+ * a captured step); no other output may overlap an input.  Lengths and their
+ * sums count as 2^30 beyond that.  One launch; two where outputs take their
+ * inputs' place and max_tokens > 2048.  page_size up to 2^20, num_pages *
+ * page_size below 2^31, num_free below 2^30, max_tokens up to 2^28.
  * Errors: DA_ERR_SHAPE, DA_ERR_NULL, DA_ERR_ALIGN, before any HIP call. */
 int da_extend_tables(const int32_t* lens, const int32_t* new_lens, const int32_t* free_pages,
                      const int32_t* taken, int32_t* block_table, int32_t* lens_out, int32_t* taken_out,

@@ -831,7 +831,8 @@ def da_extend_tables(lens: torch.Tensor, new_lens: torch.Tensor, free_pages: tor
     passed.  All int32 on one device: lens and new_lens [B]; free_pages: page
     ids, of which `taken` [1] are in use; block_table [B, max_pages], whose
     entries of new pages are written; slots and positions [max_tokens].
-    lens_out may be lens and taken_out may be taken."""
+    lens_out may be lens and taken_out may be taken.  After the first request
+    that the list cannot serve no later one gets a page."""
     dev = lens.device
     if (lens.dim() != 1 or free_pages.dim() != 1 or block_table.dim() != 2 or not 0 <= max_tokens <= MAX_NEW_TOKENS
             or not lens.is_cuda):

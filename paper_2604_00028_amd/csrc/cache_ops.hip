@@ -92,7 +92,9 @@ __device__ __forceinline__ int last_at_most(const uint32_t* at, int n, uint32_t 
 
 // Request b holds l_b keys in ceil(l_b / P) pages of P rows and gets n_b more:
 // its rows start at the exclusive sum of n, its pages at `taken` plus the
-// exclusive sum of the pages needed.  Every workgroup takes both sums over all
+// exclusive sum of the pages needed, also of those by requests that the list
+// could not serve: past it once, the sum stays past it, so none of the later
+// ones gets a page (and places that are given have no gaps).  Every workgroup takes both sums over all
 // requests for itself (PER of them a thread), so one launch needs no hand-over;
 // then the workgroups share the rows, each thread looking its row's request up
 // in LDS.  Bound by latency: two dependent loads, two scans, log2 B LDS reads a

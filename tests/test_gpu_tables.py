@@ -162,3 +162,21 @@ def test_two_streams_at_once():
         assert np.array_equal(tab.cpu().numpy(), want[0])
         for g, w in zip(out, (want[1], [want[2]], want[3], want[4], want[5])):
             assert np.array_equal(g.cpu().numpy(), w)
+
+
+@pytest.mark.parametrize("B,extra", [(2, 0), (300, 0), (300, 3000)])
+def test_a_list_too_short_for_one_request_serves_no_later_one(B, extra):
+    """Pages go out in request order: after the first request that the list cannot serve none gets a page, also one
+    that it could; requests that need none are extended before and after."""
+    page = 16
+    lens, new = np.full(B, 20), np.ones(B, int)          # a page and a part of one: room for the next key
+    at = B // 2 - 1
+    lens[at], new[at] = 0, 40 + extra                    # needs three pages (and more), the list holds one
+    lens[B - 1], new[B - 1] = 0, 5                       # needs the one there is
+    lens, new, free, taken, table, num = state(lens, new, page, taken=2, seed=10)
+    free = free[:taken + 1]
+    _, lens_out, taken_out, _, slots, _ = extend_tables(lens, new, free, taken, table, page, num, 4000)
+    assert lens_out[at] == 0 and lens_out[B - 1] == 0 and taken_out == taken
+    assert all(lens_out[b] == 21 for b in range(B - 1) if b != at)
+    for in_place in (False, True):
+        check(lens, new, free, taken, table, num, page, 4000, f"one page for {B} requests", in_place)
