@@ -90,8 +90,11 @@ def test_four_bit_lengths_are_not_bounded_by_the_bytes_of_bf16_keys():
     size = lambda L, **k: da.da_kv4_workspace_bytes(1, 64, 8, L, num_splits=4, num_cus=256, **k)  # noqa: E731
     assert size(1 << 20) == size((1 << 20) - 1) == size(1 << 30) == da.da_workspace_bytes(1, 64, 128, 4)
     assert size((1 << 30) + 1) == 0
-    call = lambda L: bnd.load().da_decode_attn_kv4(*[0x100000] * 5, None, 1, 64, 8, 1 << 14, 1 << 17, 1, L, 128, 0.0,  # noqa: E731
-                                                   0, 0, 4, 0x100000, 1000, None)
+
+    def call(L):
+        return bnd.load().da_decode_attn_kv4(*[0x100000] * 5, None, 1, 64, 8, 1 << 14, 1 << 17, 1, L, 128, 0.0, 0, 0, 4,
+                                             0x100000, 1000, None)
+
     assert call((1 << 30) + 1) == bnd.DA_ERR_SHAPE
     # nothing refused before the workspace (too small), or the device (none here)
     assert call(1 << 20) == call(1 << 30) in (bnd.DA_ERR_WORKSPACE, bnd.DA_ERR_HIP, bnd.DA_ERR_UNSUPPORTED)

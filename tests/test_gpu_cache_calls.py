@@ -56,8 +56,10 @@ def test_numbers_past_an_int_without_a_window():
 
 def test_tables_past_an_int():
     say("tables past an int")
-    tables = lambda page, pages, rows=8: da.da_extend_tables(ints(2), ints(2), ints(4), ints(1), ints(2, 4),  # noqa: E731
-                                                             page, pages, rows)
+
+    def tables(page, pages, rows=8):
+        return da.da_extend_tables(ints(2), ints(2), ints(4), ints(1), ints(2, 4), page, pages, rows)
+
     tables(16, 9)
     refused(lambda: tables(PAST + 16, 9), bnd.DA_ERR_SHAPE)
     refused(lambda: tables(-PAST + 16, 9), bnd.DA_ERR_SHAPE)
