@@ -578,7 +578,11 @@ int da_append_kv(const void* q, int64_t q_stride, const void* k, int64_t k_strid
  *              + 1 as e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6; the high bit negative);
  *              block g of 32 dims of key r has its K scale at 4 (4 (r % 16) + g)
  *              + r / 16 and its V scale two bytes further on.  A value is its
- *              code times 2^(scale - 127), exact in bf16; scale 255 is NaN
+ *              code times 2^(scale - 127), exact in bf16, for scales from 2 to
+ *              252; scale 255 is NaN.  The appends write no others, and a cache
+ *              filled by other means must not hold them: 0, 1, 253 and 254 have
+ *              values beyond bf16's normal range, and what K and V then read as
+ *              is unspecified
  * A block's scale is the least power of two that leaves its largest magnitude
  * at most 7 (within [2^-125, 2^125]), codes are rounded to the nearest, ties to
  * even.  Keys are rounded to bf16 first, so the cache holds what a quantised

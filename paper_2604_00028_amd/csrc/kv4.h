@@ -3,7 +3,7 @@
 // A tile is 32 keys of one KV head, DA_KV4_TILE_BYTES bytes: K codes 32 x 64
 // bytes, V codes 32 x 64 bytes, then 256 scale bytes.  A row's byte i holds
 // dims 2i (low half) and 2i + 1.  A value is code x 2^(scale byte - 127), one
-// scale for 32 dims: the FP4 (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+// scale byte, 2 to 252 (255: NaN), for 32 dims: the FP4 (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
 // negatives) and power-of-two scale formats that gfx950 converts in one
 // instruction, exactly into bf16.
 //
@@ -28,8 +28,6 @@ __device__ __forceinline__ int kv4_scale_at(int key, int block, int isv) {
 }
 
 __device__ __forceinline__ float kv4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Eight codes times the scale as bf16.
 __device__ __forceinline__ void dequantise(uint32_t codes, float scale, u32x4& y) {

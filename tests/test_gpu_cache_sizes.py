@@ -195,3 +195,20 @@ def test_four_bit_steps_hold_the_quantised_rows_of_the_bf16_steps():
             graph.replay()
         torch.cuda.synchronize()
         compare(buffers, before, f"replay {step}")
+
+
+def test_scale_bytes_of_every_bf16_value():
+    """Appends write scale bytes from 2 to 252, and 255 where a block holds an infinity or a NaN, whatever the values."""
+    x = np.arange(1 << 16).astype(np.uint16)
+    rng = np.random.default_rng(22)
+    x = np.concatenate([x, rng.permutation(x), np.sort(x & 0x7FFF), x & 0x80FF]).reshape(-1, 1, 128)
+    cache = torch.zeros(x.shape[0] // 32, 1, 1, 4352, dtype=torch.uint8, device="cuda")
+    say("scale bytes of every bf16 value")
+    da.da_append_kv4(None, to_dev(x), to_dev(x), None, None, cache)
+    torch.cuda.synchronize()
+    got, want = cache_rows(cache.cpu().numpy()), row_bytes(x)
+    scales = got[..., 64:68]
+    assert np.array_equal(scales, want[..., 64:]) and np.array_equal(got[..., 68:], got[..., :68])
+    assert {2, 252, 255} <= set(np.unique(scales).tolist()) <= set(range(2, 253)) | {255}
+    finite = (scales != 255).repeat(16, axis=-1)
+    assert np.array_equal(got[..., :64][finite], want[..., :64][finite])
