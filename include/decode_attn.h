@@ -476,7 +476,9 @@ int da_prefers_dealt(int B, int H_Q, int H_KV, int L_K_max, int64_t keys, int nu
 /* Decode attention with a sliding window and sinks: the last `window` keys of
  * each sequence (the query's own key among them) and its first `sinks` keys are
  * visible, key j of L where j < sinks or j >= L - window; the softmax of
- * da_decode_attn over those.  Invisible keys are not read and do not reach the
+ * da_decode_attn over those, its probabilities rounded to bf16 for the product
+ * with V as there (by up to 2^-8 each; lse takes them in 32 bits, and
+ * da_decode_attn_dealt keeps two bf16 parts of each).  Invisible keys are not read and do not reach the
  * result, whatever they hold; a NaN in a visible one reaches the output and lse
  * of the heads that read it.
  *   block_table == NULL: k, v fixed (cu_seqlens_k NULL) or packed, as for
@@ -560,8 +562,9 @@ int da_extend_tables(const int32_t* lens, const int32_t* new_lens, const int32_t
  *   q_out      bf16 [N, H_Q, d] dense; may be q where q_stride is H_Q * d
  *   k_cache, v_cache  bf16 [num_rows, H_KV, d]: page pools (row = page *
  *              page_size + offset), or contiguous sequences
- * Computed in 32 bits and rounded to bf16 once; v is copied.  One launch; no
- * row without a token is touched.  Errors: DA_ERR_NULL, DA_ERR_SHAPE,
+ * Computed in 32 bits, the mean of squares too (right for elements below 2^60),
+ * and rounded to bf16 once; v is copied.  One launch; no row without a token is
+ * touched.  N up to 2^24, H_Q and H_KV up to 2^20.  Errors: DA_ERR_NULL, DA_ERR_SHAPE,
  * DA_ERR_ALIGN (16 bytes for bf16 and rope), DA_ERR_UNSUPPORTED (d, rope_dim),
  * DA_ERR_ARG (eps, neighbours). */
 int da_append_kv(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
@@ -595,7 +598,7 @@ int da_append_kv4(const void* q, int64_t q_stride, const void* k, int64_t k_stri
 
 /* Rows of a 4-bit cache as bf16 (exact): k_out, v_out [N, H_KV, d] of cache rows
  * slots[0 .. N), or rows 0 .. N - 1 where slots is NULL; zeros for a row outside
- * the cache.  Errors as for da_append_kv4. */
+ * the cache.  N H_KV up to 2^26.  Errors as for da_append_kv4. */
 int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_out, int N, int H_KV,
                 int page_size, int num_pages, int d, void* stream);
 
@@ -607,21 +610,27 @@ int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_ou
  *              or outside the window do not reach the result
  *   window     0: all keys (sinks is then ignored); otherwise as for
  *              da_decode_attn_window
- *   num_splits 1..64: chunks that a sequence of L_K_max keys is cut into (fewer
- *              where chunk states would reach 2 GiB, or for more than
- *              DA_ARRIVAL_BYTES / DA_ARRIVAL_STRIDE head tiles); <= 0: a chunk
- *              length chosen by the batch's lengths on the device, or for one
- *              sequence, short ones and more than 1024 by L_K_max and the pool's
- *              size.  Every sequence is cut into
- *              chunks of the same length, a multiple of 64 keys, so a shorter one
- *              has fewer, and one that fits a chunk writes its output directly
+ *   num_splits 1..64: chunks that a sequence of L_K_max keys (with a window, of
+ *              da_window_keys) is cut into; <= 0: a chunk length chosen on the
+ *              device by the batch's lengths, where it has 2 to 1024 sequences,
+ *              more than 2048 such keys, B H_Q < 65536 and B times the keys at
+ *              most 2^35; else on the host by those keys and the pool's size (for
+ *              one sequence, L_K_max well above its length then costs chunks that
+ *              it would have been cut into).
+ *              Either way fewer where chunk states would reach 2 GiB, and one
+ *              where the batch has more than DA_ARRIVAL_BYTES / DA_ARRIVAL_STRIDE
+ *              = 4096 head tiles (B H_KV times the tiles of at most 32 heads that
+ *              a KV head's query heads take).  Every sequence is cut into chunks
+ *              of the same length, a multiple of 64 keys, so a shorter one has
+ *              fewer, and one that fits a chunk writes its output directly
  *   workspace  >= da_kv4_workspace_bytes(B, H_Q, H_KV, L_K_max, num_pages *
  *              page_size, window, sinks, num_splits, 0); 0 bytes for one chunk.
  *              Counters in its last DA_ARRIVAL_BYTES zero before the first call,
  *              as for da_decode_attn
  * One launch; replays of a captured call follow the lengths the device then
  * holds.  Results are bit-identical across runs for the same arguments and
- * lengths of the whole batch.  A NaN among the visible keys, or an infinity or a
+ * lengths of the whole batch.  Probabilities are rounded to bf16 for the product
+ * with V, as in da_decode_attn; lse takes them in 32 bits.  A NaN among the visible keys, or an infinity or a
  * NaN in a query, makes the output and lse of the heads that read it NaN.
  * Other arguments and errors as for da_decode_attn_paged, and DA_ERR_SHAPE for
  * pages of 4 GiB, 2^24 head tiles and more, or L_K_max above 2^30; no other limit

@@ -725,10 +725,13 @@ _graph_workspaces: Dict[Tuple[int, int], Tuple[int, torch.Tensor]] = {}
 def _offered_now(dev: torch.device, stream, handle: int) -> Tuple[Optional[torch.Tensor], int]:
     """The workspace to offer a call on the current device that passes none, and
     the number of the capture it is part of, or 0.  Outside graph capture it is
-    the one cached for the stream.  A captured call takes one that its graph
-    owns, shared by the calls captured on that stream and cleared by each replay,
-    so that graphs can be replayed in any order, beside each other and beside the
-    stream's own calls."""
+    the one cached for the stream.  A captured call takes one out of its graph's
+    memory (torch.cuda.graph's; a capture made by other means passes its own),
+    shared by the calls captured on that stream and cleared by each replay, so that
+    graphs with pools of their own can be replayed in any order, beside each other
+    and beside the stream's own calls.  Graphs that share a pool are replayed one
+    after the other, as torch asks of them.  The last one of a stream is held until
+    another graph is captured there, and its pool with it."""
     if not (_captures() if stream is None else _capturing(dev, stream)):
         return _workspaces.get((dev.index, handle)), 0
     status, number = ctypes.c_int(), ctypes.c_ulonglong()

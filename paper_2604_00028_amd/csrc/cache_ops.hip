@@ -264,12 +264,14 @@ __device__ __forceinline__ float bf16_high(uint32_t two) { return __uint_as_floa
 // lanes apart, so the bf16 words change lanes, four a pass.
 //
 // Bound by HBM (each head row read and written once: 8192 tokens of 64/8 heads,
-// 340 MB, 66.9 us, 5.1 TB/s, where a copy of 2 GiB reaches 4.9).  STREAM 1: rows
-// are written with the streaming hint (more than L2 holds: 42 MB 11.4 -> 10.5 us);
-// 2: read with it too (more than half the last-level cache: 340 MB 70.5 -> 66.9 us,
-// but 85 MB, which a projection may just have left there, 16.7 -> 20.9).  KV4: keys are rounded
-// to bf16 as the bf16 cache would hold them and then to 4 bits, values at once
-// (quantise in kv4.h).
+// 340 MB, 62.5 us a call among others, 5.4 TB/s, where a copy of 2 GiB reaches
+// 4.9).  STREAM 1: rows are written with the streaming hint (more than L2 holds:
+// 42 MB 11.4 -> 10.5 us in a graph); 2: read with it too (more than half the
+// last-level cache: 340 MB 70.5 -> 66.9 us in a graph, but 85 MB, which a
+// projection may just have left there, 16.7 -> 20.9).  KV4: keys are rounded to
+// bf16 as the bf16 cache would hold them and then to 4 bits, values at once
+// (quantise in kv4.h); stores of 4 bytes of codes and single bytes of scales, one
+// token a wave: 3001 tokens of 8 heads 7 us, where their 16 MB would take 3.
 template <bool KV4, int STREAM>
 __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams p) {
   const int lane = threadIdx.x & 63;

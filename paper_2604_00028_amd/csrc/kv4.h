@@ -3,9 +3,9 @@
 // A tile is 32 keys of one KV head, DA_KV4_TILE_BYTES bytes: K codes 32 x 64
 // bytes, V codes 32 x 64 bytes, then 256 scale bytes.  A row's byte i holds
 // dims 2i (low half) and 2i + 1.  A value is code x 2^(scale byte - 127), one
-// scale byte, 2 to 252 (255: NaN), for 32 dims: the FP4 (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
-// negatives) and power-of-two scale formats that gfx950 converts in one
-// instruction, exactly into bf16.
+// scale byte, 2 to 252 (255: NaN), for 32 dims: the FP4 (e2m1: 0, 0.5, 1, 1.5, 2,
+// 3, 4, 6 and their negatives) and power-of-two scale formats that gfx950
+// converts in one instruction, exactly into bf16.
 //
 // The order inside a tile is what the attention loads: lane (key % 16, block of
 // 32 dims) of a wave reads 16 bytes of codes of each of two keys, 1 KiB

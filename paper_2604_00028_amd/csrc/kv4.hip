@@ -109,7 +109,10 @@ __device__ __forceinline__ Query split_query(const u32x4 (&x)[4]) {
 
 // Softmax of a pair of tiles (64 keys) per head column, as TileReducer::softmax
 // does it for one: sc holds the raw scores, then the probabilities as bf16
-// operands of the two tiles.
+// operands of the two tiles.  Each is rounded once for that, by 2^-8 of itself at
+// most; their sum is taken in 32 bits before, so the output is off by at most
+// 2^-8 of the weighted mean of |v|, the size of its own rounding to bf16, and lse
+// not at all.
 template <int NT>
 __device__ __forceinline__ void softmax_pair(TileReducer<NT, 8>& red, f32x4 (&sc)[NT][4], bf16x8 (&pb)[2][1][NT]) {
 #pragma unroll
