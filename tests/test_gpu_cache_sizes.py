@@ -206,7 +206,8 @@ def test_scale_bytes_of_every_bf16_value():
     say("scale bytes of every bf16 value")
     da.da_append_kv4(None, to_dev(x), to_dev(x), None, None, cache)
     torch.cuda.synchronize()
-    got, want = cache_rows(cache.cpu().numpy()), row_bytes(x)
+    with np.errstate(invalid="ignore"):  # signalling NaNs
+        got, want = cache_rows(cache.cpu().numpy()), row_bytes(x)
     scales = got[..., 64:68]
     assert np.array_equal(scales, want[..., 64:]) and np.array_equal(got[..., 68:], got[..., :68])
     assert {2, 252, 255} <= set(np.unique(scales).tolist()) <= set(range(2, 253)) | {255}
