@@ -59,6 +59,8 @@ extern "C" {
 #define DA_KV4_TILE_BYTES 4352
 /* Requests one da_extend_tables call takes. */
 #define DA_MAX_REQUESTS 4096
+/* Position axes of da_append_kv_axes. */
+#define DA_MAX_AXES 4
 
 typedef enum da_status {
   DA_OK = 0,
@@ -595,6 +597,33 @@ int da_append_kv4(const void* q, int64_t q_stride, const void* k, int64_t k_stri
                   int rope_rows, int rope_dim, int neighbours, const int32_t* positions, const int32_t* slots,
                   void* q_out, void* cache, int page_size, int num_pages, int N, int H_Q, int H_KV, int d,
                   void* stream);
+
+/* da_append_kv and da_append_kv4 for tokens with positions on several axes (time,
+ * height and width of an image or a video): pair i of the rotation turns by the
+ * angle of the token's position on axis axes[i],
+ *   (a, b) -> (a cos - b sin, b cos + a sin), cos = rope[positions[axes[i]][n]][i],
+ *   sin = rope[positions[axes[i]][n]][rope_dim / 2 + i].
+ *   rope       required; column i of the table holds pair i's angles, whatever
+ *              frequencies the axes have
+ *   axes       HOST memory, uint8 [rope_dim / 2], each below num_axes; read
+ *              before the call returns
+ *   num_axes   1 to DA_MAX_AXES
+ *   positions  int32 [num_axes, N]; one outside [0, rope_rows) counts as a row of
+ *              zeros for the pairs of its axis
+ * A text token has the same position on every axis, and gets what da_append_kv
+ * gives it, bit for bit.  Other arguments and errors as there, and DA_ERR_NULL
+ * for rope or axes, DA_ERR_ARG for num_axes or an axis out of range. */
+int da_append_kv_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                      int64_t v_stride, const void* q_weight, const void* k_weight, float eps, const float* rope,
+                      int rope_rows, int rope_dim, int neighbours, const uint8_t* axes, int num_axes,
+                      const int32_t* positions, const int32_t* slots, void* q_out, void* k_cache, void* v_cache,
+                      int64_t num_rows, int N, int H_Q, int H_KV, int d, void* stream);
+
+int da_append_kv4_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const void* q_weight, const void* k_weight, float eps, const float* rope,
+                       int rope_rows, int rope_dim, int neighbours, const uint8_t* axes, int num_axes,
+                       const int32_t* positions, const int32_t* slots, void* q_out, void* cache, int page_size,
+                       int num_pages, int N, int H_Q, int H_KV, int d, void* stream);
 
 /* Rows of a 4-bit cache as bf16 (exact): k_out, v_out [N, H_KV, d] of cache rows
  * slots[0 .. N), or rows 0 .. N - 1 where slots is NULL; zeros for a row outside

@@ -70,6 +70,23 @@ def norm_rotate(x: np.ndarray, weight: Optional[np.ndarray], eps: float, rope: O
     return y, size
 
 
+def norm_rotate_axes(x: np.ndarray, weight: Optional[np.ndarray], eps: float, rope: np.ndarray, positions: np.ndarray,
+                     axes, neighbours: bool) -> Tuple[np.ndarray, np.ndarray]:
+    """norm_rotate with pair i turned by positions[axes[i]]; positions [A, N]."""
+    y, size = norm_rotate(x, weight, eps, None, None, neighbours)
+    half = rope.shape[1] // 2
+    for i in range(half):
+        at = positions[axes[i]]
+        inside = (at >= 0) & (at < rope.shape[0])
+        turn = np.where(inside[:, None], rope[np.where(inside, at, 0)][:, [i, half + i]].astype(np.float64), 0.0)
+        c, s = turn[:, :1], turn[:, 1:]
+        a, b = (2 * i, 2 * i + 1) if neighbours else (i, i + half)
+        ya, yb = y[:, :, a].copy(), y[:, :, b].copy()
+        y[:, :, a], y[:, :, b] = ya * c - yb * s, yb * c + ya * s
+        size[:, :, a], size[:, :, b] = np.abs(ya * c) + np.abs(yb * s), np.abs(yb * c) + np.abs(ya * s)
+    return y, size
+
+
 def kv4_codes(rows: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
     """bf16 bits [..., 128]: codes uint8 [..., 128] and scale bytes uint8 [..., 4]."""
     x = bf16_bits_to_f64(rows).reshape(rows.shape[:-1] + (4, 32))

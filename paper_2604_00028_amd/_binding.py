@@ -21,6 +21,7 @@ HEAD_DIM = 128
 MAX_SPLITS = 64
 KV4_TILE_BYTES = 4352  # 32 keys of one KV head in the 4-bit cache
 MAX_REQUESTS = 4096    # of one da_extend_tables call
+MAX_AXES = 4           # of da_append_kv_axes
 MAX_NEW_TOKENS = 1 << 28  # rows of one
 ARRIVAL_BYTES = 1 << 20  # counters at the end of a workspace
 INT_MAX = 2 ** 31 - 1
@@ -50,7 +51,7 @@ EXPORTS = (
     "da_make_schedule", "da_schedule_workspace_bytes",
     "da_decode_attn_scheduled", "da_decode_attn_dealt", "da_dealt_workspace_bytes", "da_prefers_dealt",
     "da_decode_attn_window", "da_window_keys", "da_extend_tables", "da_append_kv", "da_append_kv4", "da_read_kv4",
-    "da_decode_attn_kv4", "da_kv4_workspace_bytes",
+    "da_append_kv_axes", "da_append_kv4_axes", "da_decode_attn_kv4", "da_kv4_workspace_bytes",
     "da_split_partials", "da_combine_splits", "da_device_info", "da_strerror",
     "da_last_error",
 )
@@ -177,6 +178,12 @@ def load() -> ctypes.CDLL:
     lib.da_append_kv4.argtypes = [_P, _L, _P, _L, _P, _L, _P, _P, _F, _P, _I, _I, _I, _P, _P, _P, _P, _I, _I, _I, _I,
                                   _I, _I, _P]
     lib.da_append_kv4.restype = _I
+    lib.da_append_kv_axes.argtypes = [_P, _L, _P, _L, _P, _L, _P, _P, _F, _P, _I, _I, _I, ctypes.c_char_p, _I, _P, _P, _P,
+                                      _P, _P, _L, _I, _I, _I, _I, _P]
+    lib.da_append_kv_axes.restype = _I
+    lib.da_append_kv4_axes.argtypes = [_P, _L, _P, _L, _P, _L, _P, _P, _F, _P, _I, _I, _I, ctypes.c_char_p, _I, _P, _P,
+                                       _P, _P, _I, _I, _I, _I, _I, _I, _P]
+    lib.da_append_kv4_axes.restype = _I
     lib.da_read_kv4.argtypes = [_P, _P, _P, _P, _I, _I, _I, _I, _I, _P]
     lib.da_read_kv4.restype = _I
     lib.da_decode_attn_kv4.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _I, _F, _I, _I, _I, _P, _Z,
@@ -887,7 +894,7 @@ def _rows(name: str, t: torch.Tensor, dev: torch.device) -> Tuple[int, torch.Siz
     raise ValueError(f"{name} must be a bfloat16 tensor [N, heads, d] on {dev} whose heads are dense")
 
 
-def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours, q_out, stream):
+def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours, q_out, stream, axes=None):
     """Check what the append calls share; (their leading arguments, N, H_Q, H_KV, d, q_out)."""
     dev = k.device
     if not k.is_cuda:
@@ -920,13 +927,20 @@ def _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neigh
             raise ValueError("rope must be [positions, rope_dim], not empty, and needs positions")
         rope_rows, rope_dim = rope.shape
         _need("rope", rope, _F32, rope.shape, dev)
-        _need("positions", positions, _I32, (N,), dev)
+        if axes is None:
+            _need("positions", positions, _I32, (N,), dev)
+        else:
+            if positions.dim() != 2 or not 1 <= positions.shape[0] <= MAX_AXES or len(axes) != rope_dim // 2:
+                raise ValueError(f"positions must be [1 to {MAX_AXES} axes, N], and axes name one for each of the "
+                                 "rope_dim / 2 pairs")
+            _need("positions", positions, _I32, (positions.shape[0], N), dev)
     if slots is not None:
         _need("slots", slots, _I32, (N,), dev)
     return (q.data_ptr() if H_Q and N else None, q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
             q_weight.data_ptr() if q_weight is not None else None,
             k_weight.data_ptr() if k_weight is not None else None, eps,
             rope.data_ptr() if rope is not None else None, rope_rows, rope_dim, 1 if neighbours else 0,
+            *(() if axes is None else (axes, positions.shape[0])),
             positions.data_ptr() if positions is not None else None, slots.data_ptr() if slots is not None else None,
             q_out.data_ptr() if H_Q and N else None), N, H_Q, H_KV, d, q_out
 
@@ -985,6 +999,63 @@ def da_append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, p
         raise ValueError(f"the cache has {heads} KV heads, k {H_KV}")
     _one_device(dev, cache)
     rc = load().da_append_kv4(*args, cache.data_ptr(), page_size, num_pages, N, H_Q, H_KV, d, _stream(dev, stream))
+    if rc:
+        _check(rc)
+    return q_out
+
+
+def _axis_bytes(axes, rope) -> bytes:
+    if rope is None:
+        raise ValueError("rope is required")
+    return axes if isinstance(axes, bytes) else bytes(axes)
+
+
+def da_append_kv_axes(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+                      slots: Optional[torch.Tensor], k_cache: torch.Tensor, v_cache: torch.Tensor, *,
+                      rope: torch.Tensor, axes: Sequence[int], q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, neighbours: bool = False,
+                      q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """da_append_kv for positions [A, N] on up to four axes: pair i of the
+    rotation turns by the position on axis axes[i] (rope_dim / 2 whole numbers
+    below A; bytes save the conversion); returns q_out."""
+    dev = k.device
+    if k.is_cuda and dev.index != _get_device():
+        return _on_device(dev, da_append_kv_axes, q, k, v, positions, slots, k_cache, v_cache, rope=rope, axes=axes,
+                          q_weight=q_weight, k_weight=k_weight, eps=eps, neighbours=neighbours, q_out=q_out,
+                          stream=stream)
+    args, N, H_Q, H_KV, d, q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
+                                                q_out, stream, _axis_bytes(axes, rope))
+    shape = k_cache.shape
+    if len(shape) < 3 or shape[-2] != H_KV or shape[-1] != d:
+        raise ValueError("k_cache must be [..., H_KV, d]")
+    _need("k_cache", k_cache, _BF16, shape, dev)
+    _need("v_cache", v_cache, _BF16, shape, dev)
+    rc = load().da_append_kv_axes(*args, k_cache.data_ptr(), v_cache.data_ptr(),
+                                  k_cache.numel() // (H_KV * d) if H_KV * d else 0, N, H_Q, H_KV, d,
+                                  _stream(dev, stream))
+    if rc:
+        _check(rc)
+    return q_out
+
+
+def da_append_kv4_axes(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+                       slots: Optional[torch.Tensor], cache: torch.Tensor, *, rope: torch.Tensor, axes: Sequence[int],
+                       q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                       eps: float = 1e-6, neighbours: bool = False, q_out: Optional[torch.Tensor] = None,
+                       stream=None) -> Optional[torch.Tensor]:
+    """da_append_kv_axes into a 4-bit cache (da_append_kv4); returns q_out."""
+    dev = k.device
+    if k.is_cuda and dev.index != _get_device():
+        return _on_device(dev, da_append_kv4_axes, q, k, v, positions, slots, cache, rope=rope, axes=axes,
+                          q_weight=q_weight, k_weight=k_weight, eps=eps, neighbours=neighbours, q_out=q_out,
+                          stream=stream)
+    args, N, H_Q, H_KV, d, q_out = _append_args(q, k, v, positions, slots, rope, q_weight, k_weight, eps, neighbours,
+                                                q_out, stream, _axis_bytes(axes, rope))
+    num_pages, heads, page_size = _kv4_cache(cache)
+    if heads != H_KV:
+        raise ValueError(f"the cache has {heads} KV heads, k {H_KV}")
+    _one_device(dev, cache)
+    rc = load().da_append_kv4_axes(*args, cache.data_ptr(), page_size, num_pages, N, H_Q, H_KV, d, _stream(dev, stream))
     if rc:
         _check(rc)
     return q_out

@@ -210,6 +210,8 @@ __global__ void __launch_bounds__(kTableThreads) extend_kernel(TableParams p) {
 // ---------------------------------------------------------------- append
 
 constexpr int kAppendWaves = 4;
+constexpr int kMaxAxes = DA_MAX_AXES;
+static_assert(kMaxAxes == 4 && D / 2 <= 64, "the axis of a pair has two bits, the axes of all pairs four words");
 
 struct AppendParams {
   const uint16_t* q;  // nullable
@@ -221,7 +223,9 @@ struct AppendParams {
   float eps;
   const float* rope;                     // nullable: no rotation
   int rope_rows, rope_dim, neighbours;
-  const int32_t* positions;
+  const int32_t* positions;              // [num_axes, N]
+  int num_axes;
+  uint32_t axes[4];                      // axis of pair i: bits 2 (i mod 16) of word i / 16
   const int32_t* slots;
   uint16_t* q_out;
   uint16_t* k_cache;                     // bf16 rows [num_rows, H_KV, D]
@@ -272,7 +276,13 @@ __device__ __forceinline__ float bf16_high(uint32_t two) { return __uint_as_floa
 // bf16 as the bf16 cache would hold them and then to 4 bits, values at once
 // (quantise in kv4.h); stores of 4 bytes of codes and single bytes of scales, one
 // token a wave: 3001 tokens of 8 heads 7 us, where their 16 MB would take 3.
-template <bool KV4, int STREAM>
+//
+// AXES: pair i of the rotation turns by the token's position on axis a(i) of up
+// to four, so its coefficients come from row positions[a(i)] of the table.  A
+// lane reads its eight dims' cosines and sines of every axis that one of its
+// pairs has (the others are out of the range of its loads and cost nothing) and
+// picks by pair.
+template <bool KV4, int STREAM, bool AXES>
 __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams p) {
   const int lane = threadIdx.x & 63;
   const int unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x * kAppendWaves + (int)(threadIdx.x >> 6));
@@ -292,7 +302,48 @@ __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams 
     c[e] = 1.f;
     s[e] = 0.f;
   }
-  if (p.rope) {
+  if constexpr (AXES) {
+    const bool second = !p.neighbours && l >= half;  // the pairs' second dims
+    const int pair0 = p.neighbours ? 4 * l : 8 * (second ? l - half : l);  // the lane's first pair
+    const int word = (pair0 >> 4) & 3;
+    const uint32_t mine =
+        (word == 0 ? p.axes[0] : word == 1 ? p.axes[1] : word == 2 ? p.axes[2] : p.axes[3]) >> (2 * (pair0 & 15));
+    const int pairs = p.neighbours ? 4 : 8;
+    f32x4 cc[kMaxAxes][2], ss[kMaxAxes][2];
+#pragma unroll
+    for (int a = 0; a < kMaxAxes; ++a) {
+      if (a >= p.num_axes) break;  // uniform
+      const int pos = __builtin_amdgcn_readfirstlane(p.positions[(int64_t)a * p.N + n]);
+      const bool in = pos >= 0 && pos < p.rope_rows;  // a position outside the table: zeros
+      const __amdgpu_buffer_rsrc_t rr =
+          make_rsrc(p.rope + (int64_t)(in ? pos : 0) * p.rope_dim, in ? (uint32_t)p.rope_dim * 4u : 0u);
+      bool has = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) has |= e < pairs && ((mine >> (2 * e)) & 3u) == (uint32_t)a;
+      const uint32_t at = has && l < lanes ? 4u * (uint32_t)pair0 : 0x80000000u;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        // four pairs a lane need the first halves only
+        const uint32_t from = i == 0 || !p.neighbours ? at + 16u * i : 0x80000000u;
+        cc[a][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, from, 0, 0));
+        ss[a][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, from + 2u * p.rope_dim, 0, 0));
+      }
+    }
+    if (l < lanes) {
+#pragma unroll
+      for (int a = 0; a < kMaxAxes; ++a) {
+        if (a >= p.num_axes) break;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int i = p.neighbours ? e / 2 : e;
+          if (((mine >> (2 * i)) & 3u) != (uint32_t)a) continue;
+          c[e] = p.neighbours ? cc[a][0][e / 2] : cc[a][e / 4][e % 4];
+          const float turn = p.neighbours ? ss[a][0][e / 2] : ss[a][e / 4][e % 4];
+          s[e] = (p.neighbours ? e % 2 == 0 : !second) ? -turn : turn;
+        }
+      }
+    }
+  } else if (p.rope) {
     const int pos = __builtin_amdgcn_readfirstlane(p.positions[n]);
     const bool in = pos >= 0 && pos < p.rope_rows;  // a position outside the table: zeros
     const __amdgpu_buffer_rsrc_t rr =
@@ -523,7 +574,20 @@ int append_params(AppendParams& p, const void* q, int64_t q_stride, const void* 
   return DA_OK;
 }
 
-template <bool KV4>
+// The axis of each pair of the rotation, for the calls with positions on several.
+int append_axes(AppendParams& p, const uint8_t* axes, int num_axes) {
+  if (!p.rope || !axes) return da::fail(DA_ERR_NULL, "rope and axes must be non-NULL");
+  if (num_axes < 1 || num_axes > kMaxAxes)
+    return da::fail(DA_ERR_ARG, "num_axes=%d not in [1, %d]", num_axes, kMaxAxes);
+  for (int i = 0; i < p.rope_dim / 2; ++i) {
+    if (axes[i] >= num_axes) return da::fail(DA_ERR_ARG, "axes[%d]=%d of %d axes", i, axes[i], num_axes);
+    p.axes[i / 16] |= (uint32_t)axes[i] << (2 * (i % 16));
+  }
+  p.num_axes = num_axes;
+  return DA_OK;
+}
+
+template <bool KV4, bool AXES>
 int launch_append(AppendParams& p, int cus, hipStream_t stream) {
   if (p.N == 0) return DA_OK;
   // A wave keeps a token's coefficients over its passes, so it takes as many as
@@ -545,12 +609,12 @@ int launch_append(AppendParams& p, int cus, hipStream_t stream) {
   void* args[] = {&p};
   const void* fn;
   if constexpr (KV4) {
-    fn = reinterpret_cast<const void*>(&append_kernel<true, 0>);
+    fn = reinterpret_cast<const void*>(&append_kernel<true, 0, AXES>);
   } else {
     const int64_t moved = (int64_t)p.N * (p.H_Q + 2 * p.H_KV) * D * 4;
-    fn = moved > (128ll << 20)       ? reinterpret_cast<const void*>(&append_kernel<false, 2>)
-         : moved > da::kL2Bytes ? reinterpret_cast<const void*>(&append_kernel<false, 1>)
-                                : reinterpret_cast<const void*>(&append_kernel<false, 0>);
+    fn = moved > (128ll << 20)       ? reinterpret_cast<const void*>(&append_kernel<false, 2, AXES>)
+         : moved > da::kL2Bytes ? reinterpret_cast<const void*>(&append_kernel<false, 1, AXES>)
+                                : reinterpret_cast<const void*>(&append_kernel<false, 0, AXES>);
   }
   return launched(hipLaunchKernel(fn, dim3((uint32_t)((units + kAppendWaves - 1) / kAppendWaves)),
                                   dim3(64 * kAppendWaves), args, 0, stream),
@@ -566,6 +630,37 @@ int check_kv4_cache(const void* cache, int page_size, int num_pages, int H_KV) {
   if (num_pages < 0 || H_KV <= 0 || (int64_t)num_pages * page_size >= ((int64_t)1 << 31))
     return da::fail(DA_ERR_SHAPE, "num_pages=%d pages of %d rows (H_KV=%d)", num_pages, page_size, H_KV);
   return DA_OK;
+}
+
+// The rest of an append call: the cache's checks and the launch.
+template <bool AXES>
+int append_rows(AppendParams& p, void* k_cache, void* v_cache, int64_t num_rows, void* stream) {
+  if (num_rows < 0) return da::fail(DA_ERR_SHAPE, "num_rows=%lld is negative", (long long)num_rows);
+  if (num_rows > 0 && (!k_cache || !v_cache)) return da::fail(DA_ERR_NULL, "k_cache and v_cache must be non-NULL");
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16))
+    return da::fail(DA_ERR_ALIGN, "k_cache and v_cache must be 16-byte aligned");
+  int cus = 0;
+  const int rc = ensure_gfx950(&cus);
+  if (rc) return rc;
+  p.k_cache = static_cast<uint16_t*>(k_cache);
+  p.v_cache = static_cast<uint16_t*>(v_cache);
+  p.num_rows = num_rows;
+  return launch_append<false, AXES>(p, cus, static_cast<hipStream_t>(stream));
+}
+
+template <bool AXES>
+int append_rows4(AppendParams& p, void* cache, int page_size, int num_pages, void* stream) {
+  int rc = check_kv4_cache(cache, page_size, num_pages, p.H_KV);
+  if (rc) return rc;
+  int cus = 0;
+  rc = ensure_gfx950(&cus);
+  if (rc) return rc;
+  p.cache = static_cast<unsigned char*>(cache);
+  p.page_size = page_size;
+  p.blocks = page_size / kKeysPerTile;
+  p.div_page = make_div((uint32_t)page_size);
+  p.num_rows = (int64_t)num_pages * page_size;
+  return launch_append<true, AXES>(p, cus, static_cast<hipStream_t>(stream));
 }
 
 }  // namespace
@@ -629,18 +724,7 @@ int da_append_kv(const void* q, int64_t q_stride, const void* k, int64_t k_strid
   AppendParams p{};
   int rc = append_params(p, q, q_stride, k, k_stride, v, v_stride, q_weight, k_weight, eps, rope, rope_rows, rope_dim,
                          neighbours, positions, slots, q_out, N, H_Q, H_KV, d);
-  if (rc) return rc;
-  if (num_rows < 0) return da::fail(DA_ERR_SHAPE, "num_rows=%lld is negative", (long long)num_rows);
-  if (num_rows > 0 && (!k_cache || !v_cache)) return da::fail(DA_ERR_NULL, "k_cache and v_cache must be non-NULL");
-  if (!aligned(k_cache, 16) || !aligned(v_cache, 16))
-    return da::fail(DA_ERR_ALIGN, "k_cache and v_cache must be 16-byte aligned");
-  int cus = 0;
-  rc = ensure_gfx950(&cus);
-  if (rc) return rc;
-  p.k_cache = static_cast<uint16_t*>(k_cache);
-  p.v_cache = static_cast<uint16_t*>(v_cache);
-  p.num_rows = num_rows;
-  return launch_append<false>(p, cus, static_cast<hipStream_t>(stream));
+  return rc ? rc : append_rows<false>(p, k_cache, v_cache, num_rows, stream);
 }
 
 int da_append_kv4(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -651,18 +735,33 @@ int da_append_kv4(const void* q, int64_t q_stride, const void* k, int64_t k_stri
   AppendParams p{};
   int rc = append_params(p, q, q_stride, k, k_stride, v, v_stride, q_weight, k_weight, eps, rope, rope_rows, rope_dim,
                          neighbours, positions, slots, q_out, N, H_Q, H_KV, d);
-  if (rc) return rc;
-  rc = check_kv4_cache(cache, page_size, num_pages, H_KV);
-  if (rc) return rc;
-  int cus = 0;
-  rc = ensure_gfx950(&cus);
-  if (rc) return rc;
-  p.cache = static_cast<unsigned char*>(cache);
-  p.page_size = page_size;
-  p.blocks = page_size / kKeysPerTile;
-  p.div_page = make_div((uint32_t)page_size);
-  p.num_rows = (int64_t)num_pages * page_size;
-  return launch_append<true>(p, cus, static_cast<hipStream_t>(stream));
+  return rc ? rc : append_rows4<false>(p, cache, page_size, num_pages, stream);
+}
+
+int da_append_kv_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                      const void* q_weight, const void* k_weight, float eps, const float* rope, int rope_rows,
+                      int rope_dim, int neighbours, const uint8_t* axes, int num_axes, const int32_t* positions,
+                      const int32_t* slots, void* q_out, void* k_cache, void* v_cache, int64_t num_rows, int N, int H_Q,
+                      int H_KV, int d, void* stream) {
+  da::clear_error();
+  AppendParams p{};
+  int rc = append_params(p, q, q_stride, k, k_stride, v, v_stride, q_weight, k_weight, eps, rope, rope_rows, rope_dim,
+                         neighbours, positions, slots, q_out, N, H_Q, H_KV, d);
+  if (!rc) rc = append_axes(p, axes, num_axes);
+  return rc ? rc : append_rows<true>(p, k_cache, v_cache, num_rows, stream);
+}
+
+int da_append_kv4_axes(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const void* q_weight, const void* k_weight, float eps, const float* rope,
+                       int rope_rows, int rope_dim, int neighbours, const uint8_t* axes, int num_axes,
+                       const int32_t* positions, const int32_t* slots, void* q_out, void* cache, int page_size,
+                       int num_pages, int N, int H_Q, int H_KV, int d, void* stream) {
+  da::clear_error();
+  AppendParams p{};
+  int rc = append_params(p, q, q_stride, k, k_stride, v, v_stride, q_weight, k_weight, eps, rope, rope_rows, rope_dim,
+                         neighbours, positions, slots, q_out, N, H_Q, H_KV, d);
+  if (!rc) rc = append_axes(p, axes, num_axes);
+  return rc ? rc : append_rows4<true>(p, cache, page_size, num_pages, stream);
 }
 
 int da_read_kv4(const void* cache, const int32_t* slots, void* k_out, void* v_out, int N, int H_KV, int page_size,
