@@ -676,6 +676,78 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
 size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t pool_keys, int window, int sinks,
                               int num_splits, int num_cus);
 
+/* The attention weight that each key of a paged bf16 cache received in a step,
+ * summed over the query heads that share its KV head, and over steps:
+ *   weights_out[b][kvh][j] = decay weights[b][kvh][j] +
+ *                            sum over heads h of kvh of exp(scale q_h . k_j - lse[b][h])
+ * for the keys j < seq_lens[b].  Entries past the sequence are neither read nor
+ * written.  Call it with the q and the lse of any attention call that saw all
+ * keys of the sequence; what da_evict_kv goes by.
+ *   q            bf16 [B, H_Q, d], lse fp32 [B, H_Q] (lse_out of the attention);
+ *                a head whose lse is -inf adds nothing
+ *   k_cache, block_table, seq_lens, page_size, max_pages, num_pages, L_K_max,
+ *                softmax_scale  as for da_decode_attn_paged
+ *   weights, weights_out  fp32 [B, H_KV, weight_stride], weight_stride >=
+ *                L_K_max; they may be the same
+ *   decay        in [0, 1]; with 0 `weights` is not read
+ * A new key's entry has to be 0 beforehand: zero the tensor once, and
+ * da_evict_kv leaves zeros where keys were.  Scores, exponentials and sums in 32
+ * bits; results are bit-identical across runs.  One launch, no workspace.
+ * Errors as for da_decode_attn_paged (H_Q / H_KV up to 2^16), DA_ERR_SHAPE for
+ * weight_stride, DA_ERR_ARG for decay. */
+int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_table, const int32_t* seq_lens,
+                       const float* lse, const float* weights, float* weights_out, int64_t weight_stride, int B,
+                       int H_Q, int H_KV, int page_size, int max_pages, int num_pages, int L_K_max, int d,
+                       float softmax_scale, float decay, void* stream);
+
+/* Eviction from a paged bf16 cache: every sequence of more than `budget` keys
+ * keeps `budget` of them, chosen for each KV head by itself, and gives back the
+ * pages behind.  Of a head's rows stay, in this order: those of the first
+ * `sinks` and the last `recent` positions, then those of the largest weight, of
+ * equal ones the lowest rows; a NaN counts below all numbers.  Kept rows at
+ * `budget` and beyond move into the rows below it that come free, the i-th into
+ * the i-th; no other row of the pool is written.  Decode attention does not
+ * depend on the order of a sequence's keys (a window over them does), and keys
+ * carry their rotation with them.
+ *   block_table, seq_lens, page_size, max_pages, num_pages, L_K_max  as for
+ *                da_decode_attn_paged; num_pages * page_size < 2^31, B <=
+ *                DA_MAX_REQUESTS.  A sequence's rows below `sinks` stay where
+ *                they are, so sequences may share pages that hold only such
+ *                rows (a common prompt), and no others
+ *   totals       int32 [B]: tokens the sequence has had, evicted ones included:
+ *                the position of its next token
+ *   weights      fp32 [B, H_KV, weight_stride], weight_stride >= L_K_max
+ *   positions    int32 [B, H_KV, weight_stride]: the position of each row; a
+ *                negative one stands for row + totals - seq_lens, right for rows
+ *                appended after the last eviction, so a tensor filled with -1
+ *                once needs no more care
+ *   weights_out, positions_out  the same after the moves (0 and -1 in rows [budget,
+ *                seq_lens), other rows past the sequence not written); may be
+ *                weights and positions
+ *   lens_out     int32 [B]: min(seq_lens, budget); may be seq_lens
+ *   free_pages, taken, taken_out, num_free  NULL, or da_extend_tables's list of
+ *                free pages [num_free], of which *taken are in use: the pages
+ *                that hold rows at `budget` and beyond only, in order of
+ *                sequence, are written to the places that end at *taken, and
+ *                *taken_out (may be taken) is that much less.  Of more pages than
+ *                *taken the first ones find no place.  The table keeps its
+ *                entries; those behind the new length are stale
+ *   budget >= 1, sinks, recent >= 0, sinks + recent <= budget
+ *   workspace    >= da_evict_workspace_bytes(B, H_KV, L_K_max, budget); its last
+ *                DA_ARRIVAL_BYTES are not touched, so the other calls' may be
+ *                shared
+ * Two launches.  Errors as for da_decode_attn_paged, and DA_ERR_ARG for budget,
+ * sinks and recent. */
+int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* seq_lens,
+                const int32_t* totals, const float* weights, const int32_t* positions, float* weights_out,
+                int32_t* positions_out, int64_t weight_stride, int32_t* lens_out, int32_t* free_pages,
+                const int32_t* taken, int32_t* taken_out, int num_free, int B, int H_KV, int page_size, int max_pages,
+                int num_pages, int L_K_max, int d, int budget, int sinks, int recent, void* workspace,
+                size_t workspace_bytes, void* stream);
+
+/* Workspace bytes da_evict_kv needs; 0 for a shape it does not take. */
+size_t da_evict_workspace_bytes(int B, int H_KV, int L_K_max, int budget);
+
 /* The split step alone: the partial softmax state of every chunk (the
  * per-chunk max, sum and unnormalised output the paper's final reduction
  * merges; Sections 3.1, 5.3).  Same inputs as da_decode_attn; num_splits

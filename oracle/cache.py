@@ -166,3 +166,62 @@ def attend(q: np.ndarray, keys: List[np.ndarray], values: List[np.ndarray],
             out[b, h] = p @ values[b][:, h // g] / p.sum()
             size[b, h] = p @ np.abs(values[b][:, h // g]) / p.sum()
     return out, lse, size
+
+
+def key_weights(q, ks, lse, old, decay, scale=None):
+    """decay old + sum over heads of exp(scale q k - lse), and what its 32-bit steps may be off by: per sequence [H_KV, L].
+
+    q float64 [B, H_Q, D]; ks: per sequence float64 [L, H_KV, D]; lse [B, H_Q]; old: per sequence [H_KV, L]."""
+    scale = 1.0 / np.sqrt(q.shape[-1]) if scale is None else scale
+    out, tol = [], []
+    for b, k in enumerate(ks):
+        L, H_KV = k.shape[:2]
+        g = q.shape[1] // H_KV
+        w = np.zeros((H_KV, L)) if decay == 0 else decay * old[b]
+        e = 2.0 ** -23 * np.abs(w) + 2.0 ** -120
+        for h in range(q.shape[1]):
+            if lse[b, h] == -np.inf:
+                continue
+            kh = k[:, h // g]
+            s, size = scale * (kh @ q[b, h]), scale * (np.abs(kh) @ np.abs(q[b, h]))
+            p = np.exp(s - lse[b, h])
+            w[h // g] += p
+            # 128 products and sums; scale, score and lse in log2 units; their difference, the exponential, the heads' sum
+            e[h // g] += p * 2.0 ** -24 * (132 * size + 4 * np.abs(s) + 4 * abs(lse[b, h]) + 16 + g)
+        out.append(w)
+        tol.append(e)
+    return out, tol
+
+
+def evict(lens, totals, weights, positions, table, page, budget, sinks, recent, free_pages=None, taken=0):
+    """(lens, weights, positions, moves, free_pages, taken) after the step; moves: (sequence, head, target row, source
+    row) with rows counted within the sequence."""
+    weights, positions = weights.copy(), positions.copy()
+    out, moves, back = [], [], []
+    for b, L in enumerate(lens):
+        out.append(min(L, budget))
+        if L <= budget:
+            continue
+        back += [int(x) for x in table[b, -(-budget // page):-(-L // page)]]
+        for h in range(weights.shape[1]):
+            pos = [int(positions[b, h, r]) if positions[b, h, r] >= 0 else r + int(totals[b]) - L for r in range(L)]
+            w = weights[b, h]
+            def rank(r):
+                if pos[r] < sinks or pos[r] >= totals[b] - recent:
+                    return (0, 0.0, r)
+                return (2, 0.0, r) if np.isnan(w[r]) else (1, -float(w[r]), r)
+            kept = set(sorted(range(L), key=rank)[:budget])
+            holes = [r for r in range(budget) if r not in kept]
+            late = [r for r in range(budget, L) if r in kept]
+            moves += [(b, h, d, s) for d, s in zip(holes, late)]
+            new_w, new_p = w[:L].copy(), np.array(pos, dtype=np.int32)
+            new_w[holes], new_p[holes] = w[late], new_p[late]
+            new_w[budget:], new_p[budget:] = 0.0, -1
+            weights[b, h, :L], positions[b, h, :L] = new_w, new_p
+    if free_pages is not None:
+        free_pages = free_pages.copy()
+        for i, page_id in enumerate(back):
+            if taken - len(back) + i >= 0:
+                free_pages[taken - len(back) + i] = page_id
+        taken = max(0, taken - len(back))
+    return np.array(out, np.int32), weights, positions, moves, free_pages, taken

@@ -51,7 +51,7 @@ EXPORTS = (
     "da_make_schedule", "da_schedule_workspace_bytes",
     "da_decode_attn_scheduled", "da_decode_attn_dealt", "da_dealt_workspace_bytes", "da_prefers_dealt",
     "da_decode_attn_window", "da_window_keys", "da_extend_tables", "da_append_kv", "da_append_kv4", "da_read_kv4",
-    "da_append_kv_axes", "da_append_kv4_axes", "da_decode_attn_kv4", "da_kv4_workspace_bytes",
+    "da_append_kv_axes", "da_append_kv4_axes", "da_add_key_weights", "da_evict_kv", "da_evict_workspace_bytes", "da_decode_attn_kv4", "da_kv4_workspace_bytes",
     "da_split_partials", "da_combine_splits", "da_device_info", "da_strerror",
     "da_last_error",
 )
@@ -191,6 +191,12 @@ def load() -> ctypes.CDLL:
     lib.da_decode_attn_kv4.restype = _I
     lib.da_kv4_workspace_bytes.argtypes = [_I] * 4 + [_L] + [_I] * 4
     lib.da_kv4_workspace_bytes.restype = _Z
+    lib.da_add_key_weights.argtypes = [_P] * 7 + [_L] + [_I] * 8 + [_F, _F, _P]
+    lib.da_add_key_weights.restype = _I
+    lib.da_evict_kv.argtypes = [_P] * 9 + [_L] + [_P] * 4 + [_I] * 11 + [_P, _Z, _P]
+    lib.da_evict_kv.restype = _I
+    lib.da_evict_workspace_bytes.argtypes = [_I] * 4
+    lib.da_evict_workspace_bytes.restype = _Z
     lib.da_split_partials.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _F, _I, _I, _P]
     lib.da_split_partials.restype = _I
     lib.da_combine_splits.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _I, _P]
@@ -1129,3 +1135,130 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
     if rc:
         _check(rc)
     return out
+
+
+# ---------------------------------------------------------------- a shared and bounded cache
+
+
+def _paged_pool(name: str, cache: torch.Tensor, dev: torch.device) -> Tuple[int, int, int, int]:
+    """(num_pages, page_size, H_KV, d) of a bf16 page pool."""
+    shape = cache.shape
+    if len(shape) != 4:
+        raise ValueError(f"{name} must be [num_pages, page_size, H_KV, d]")
+    _need(name, cache, _BF16, shape, dev)
+    return shape
+
+
+def _table_args(block_table: torch.Tensor, seq_lens: torch.Tensor, B: int, dev: torch.device) -> int:
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
+    max_pages = block_table.shape[1]
+    _need("block_table", block_table, _I32, (B, max_pages), dev)
+    _need("seq_lens", seq_lens, _I32, (B,), dev)
+    return _int(max_pages)
+
+
+def da_add_key_weights(q: torch.Tensor, k_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                       lse: torch.Tensor, weights: torch.Tensor, L_K_max: int, decay: float = 1.0,
+                       weights_out: Optional[torch.Tensor] = None, *, softmax_scale: float = 0.0,
+                       stream=None) -> torch.Tensor:
+    """The attention weight of every key, summed over the heads that share it:
+    weights_out = decay weights + sum over heads of exp(scale q k - lse); returns
+    weights_out, which is `weights` where none is passed.  q [B, H_Q, d], lse
+    [B, H_Q] of the attention call, weights fp32 [B, H_KV, at least L_K_max]."""
+    dev = q.device
+    if q.dim() != 3 or q.dtype is not _BF16 or not q.is_contiguous() or not q.is_cuda:
+        raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")
+    B, H_Q, d = q.shape
+    num_pages, page_size, H_KV, dk = _paged_pool("k_cache", k_cache, dev)
+    if dk != d:
+        raise ValueError(f"k_cache has head dim {dk}, q {d}")
+    max_pages = _table_args(block_table, seq_lens, B, dev)
+    _need("lse", lse, _F32, (B, H_Q), dev)
+    if weights.dim() != 3:
+        raise ValueError("weights must be [B, H_KV, keys]")
+    stride = weights.shape[2]
+    _need("weights", weights, _F32, (B, H_KV, stride), dev)
+    if weights_out is None:
+        weights_out = weights
+    else:
+        _need("weights_out", weights_out, _F32, (B, H_KV, stride), dev)
+    if dev.index != _get_device():
+        return _on_device(dev, da_add_key_weights, q, k_cache, block_table, seq_lens, lse, weights, L_K_max, decay,
+                          weights_out, softmax_scale=softmax_scale, stream=stream)
+    rc = load().da_add_key_weights(_ptr(q), _ptr(k_cache), _ptr(block_table), _ptr(seq_lens), _ptr(lse),
+                                   weights.data_ptr() or None, weights_out.data_ptr() or None, stride, B, H_Q, H_KV,
+                                   _int(page_size), max_pages, _int(num_pages), _int(int(L_K_max)), d, softmax_scale,
+                                   decay, _stream(dev, stream))
+    if rc:
+        _check(rc)
+    return weights_out
+
+
+def da_evict_workspace_bytes(B: int, H_KV: int, L_K_max: int, budget: int) -> int:
+    return int(load().da_evict_workspace_bytes(_int(B), _int(H_KV), _int(L_K_max), _int(budget)))
+
+
+def da_evict_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                totals: torch.Tensor, weights: torch.Tensor, positions: torch.Tensor, budget: int, L_K_max: int, *,
+                sinks: int = 0, recent: int = 0, free_pages: Optional[torch.Tensor] = None,
+                taken: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+                weights_out: Optional[torch.Tensor] = None, positions_out: Optional[torch.Tensor] = None,
+                taken_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Sequences of more than `budget` keys keep that many, of each KV head those
+    of the first `sinks` and the last `recent` positions and the largest weights;
+    rows move within the caches; returns (lens_out, weights_out, positions_out,
+    taken_out), which are seq_lens, weights, positions and taken where none are
+    passed.  totals int32 [B]: tokens each sequence has had; weights fp32 and
+    positions int32 [B, H_KV, at least L_K_max] (-1: where no eviction has placed
+    the row); free_pages and taken: da_extend_tables's, to which pages go back."""
+    dev = k_cache.device
+    if not k_cache.is_cuda:
+        raise ValueError("k_cache must be on the GPU")
+    num_pages, page_size, H_KV, d = _paged_pool("k_cache", k_cache, dev)
+    _need("v_cache", v_cache, _BF16, k_cache.shape, dev)
+    B = seq_lens.shape[0] if seq_lens.dim() == 1 else 0
+    max_pages = _table_args(block_table, seq_lens, B, dev)
+    _need("totals", totals, _I32, (B,), dev)
+    if weights.dim() != 3:
+        raise ValueError("weights must be [B, H_KV, keys]")
+    shape = (B, H_KV, weights.shape[2])
+    _need("weights", weights, _F32, shape, dev)
+    _need("positions", positions, _I32, shape, dev)
+    if (free_pages is None) != (taken is None) or (taken_out is not None and taken is None):
+        raise ValueError("free_pages and taken go together, and taken_out with them")
+    num_free = 0
+    if free_pages is not None:
+        num_free = _int(free_pages.numel())
+        _need("free_pages", free_pages, _I32, (num_free,), dev)
+        _need("taken", taken, _I32, (1,), dev)
+    outs = []
+    for name, t, own, dtype in (("lens_out", lens_out, seq_lens, _I32), ("weights_out", weights_out, weights, _F32),
+                                ("positions_out", positions_out, positions, _I32),
+                                ("taken_out", taken_out, taken, _I32)):
+        if t is None:
+            t = own
+        else:
+            _need(name, t, dtype, own.shape, dev)
+        outs.append(t)
+    if dev.index != _get_device():
+        return _on_device(dev, da_evict_kv, k_cache, v_cache, block_table, seq_lens, totals, weights, positions, budget,
+                          L_K_max, sinks=sinks, recent=recent, free_pages=free_pages, taken=taken, lens_out=outs[0],
+                          weights_out=outs[1], positions_out=outs[2], taken_out=outs[3], workspace=workspace,
+                          stream=stream)
+    budget, L = _int(int(budget)), _int(int(L_K_max))
+    s_handle = _stream(dev, stream)
+    ws, capture = (_usable(workspace, dev), 0) if workspace is not None else _offered_now(dev, stream, s_handle)
+    while True:
+        rc = load().da_evict_kv(_ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens), _ptr(totals),
+                                _ptr(weights), _ptr(positions), _ptr(outs[1]), _ptr(outs[2]), shape[2], _ptr(outs[0]),
+                                _ptr(free_pages), _ptr(taken), _ptr(outs[3]), num_free, B, H_KV, _int(page_size),
+                                max_pages, _int(num_pages), L, d, budget, _int(int(sinks)), _int(int(recent)), _ptr(ws),
+                                _nbytes(ws), s_handle)
+        if rc != DA_ERR_WORKSPACE or workspace is not None:
+            break
+        workspace = ws = _grown(dev, s_handle, capture, da_evict_workspace_bytes(B, H_KV, L, budget))
+    if rc:
+        _check(rc)
+    return tuple(outs)

@@ -1,0 +1,608 @@
+// A cache that is bounded by eviction: the attention weight each key received
+// (weights_kernel), and the choice of the rows that stay (select_kernel) with
+// their way into the places that come free (move_kernel).  Entry points at the
+// end.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "decode_attn.h"
+#include "host.h"
+#include "plan.h"
+#include "tile.h"
+
+namespace {
+
+using da::aligned;
+using da::ensure_gfx950;
+
+// ---------------------------------------------------------------- weights
+
+constexpr int kWeightWaves = 4;
+constexpr int kMostChunkTiles = 64;  // page ids of a chunk: one a lane
+
+struct WeightParams {
+  const uint16_t* q;
+  const uint16_t* k;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const float* lse;
+  const float* in;
+  float* out;
+  int64_t stride;  // floats between the rows of two heads
+  int B, H_Q, H_KV, g, L_K, page_size, max_pages, num_pages;
+  int chunk_tiles, chunks;
+  Div div_page, div_chunks, div_heads;
+  float scale_log2, decay;
+};
+
+// out_j = decay in_j + sum_h exp(scale q_h k_j - lse_h) over the g query heads
+// of a KV head.  A workgroup takes `chunk_tiles` tiles of 32 keys of one
+// (sequence, KV head), its waves one tile in four; a wave's product has the
+// heads as rows and the keys as columns (S = Q K^T, the operands of the
+// attention kernels' S^T exchanged), so that a key's sum over 16 heads is three
+// additions and two lane exchanges.  K comes straight into the operand layout,
+// the next tile's loads in flight while one is reduced.  exp(x) = 2^(raw scale
+// log2 e - lse log2 e), one fma and one exponential a score; in 32 bits
+// throughout.  Up to 16 NT heads stay in registers; more (g > 64) are read anew
+// for each tile.
+template <int NT>
+__global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(WeightParams p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const int unit = div_by((int)blockIdx.x, p.div_chunks), chunk = (int)blockIdx.x - unit * p.chunks;
+  const int b = div_by(unit, p.div_heads), kvh = unit - b * p.H_KV;
+  const int L = min(p.seq_lens[b], p.L_K);
+  const int tiles = L > 0 ? (L + kKeysPerTile - 1) / kKeysPerTile : 0;
+  const int first = chunk * p.chunk_tiles;
+  const int end = min(first + p.chunk_tiles, tiles);
+  int t = first + wave;
+  if (t >= end) return;  // waves are independent
+  const int pg0 = div_by(first * kKeysPerTile, p.div_page);
+  const int pg1 = div_by(end * kKeysPerTile - 1, p.div_page);
+  const int pages = pg0 + lane <= pg1 ? p.block_table[(int64_t)b * p.max_pages + pg0 + lane] : 0;
+
+  const uint32_t rs = (uint32_t)p.H_KV * (D * 2);
+  const int64_t row0 = (int64_t)b * p.H_Q + (int64_t)kvh * p.g;
+  const __amdgpu_buffer_rsrc_t qr = make_rsrc(p.q + row0 * D, (uint32_t)p.g * (D * 2));
+  const __amdgpu_buffer_rsrc_t lr = make_rsrc(p.lse + row0, (uint32_t)p.g * 4u);
+  bf16x8 q[NT][4];
+  float base[NT][4];  // -lse log2 e; -inf for rows past the heads, and for heads that saw nothing
+  auto load_heads = [&](int h0) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        q[nt][j] = as_bf16x8(__builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                       qr, (uint32_t)(h0 + nt * 16 + col) * (D * 2) + 64u * j + 16u * quad, 0, 0)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int h = h0 + nt * 16 + quad * 4 + e;
+        const float l = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(lr, (uint32_t)h * 4u, 0, 0));
+        base[nt][e] = h < p.g && l != -INFINITY ? -l * kLog2e : -INFINITY;
+      }
+    }
+  };
+  load_heads(0);
+
+  const float* in = p.in + ((int64_t)b * p.H_KV + kvh) * p.stride;
+  float* out = p.out + ((int64_t)b * p.H_KV + kvh) * p.stride;
+  const bool keep = p.decay != 0.f;
+  auto load = [&](u32x4 (&k)[2][4], float& old, int t) {
+    const int key = t * kKeysPerTile, j = div_by(key, p.div_page);
+    const int page = __builtin_amdgcn_readlane(pages, (j - pg0) & 63);
+    const bool in_pool = page >= 0 && page < p.num_pages;  // a page outside the cache reads as zero keys
+    const int rows = min(L - key, kKeysPerTile);
+    const int64_t prow = (in_pool ? (int64_t)page : 0) * p.page_size + (key - j * p.page_size);
+    const __amdgpu_buffer_rsrc_t kr =
+        make_rsrc(p.k + (prow * p.H_KV + kvh) * D,
+                  (uint32_t)__builtin_amdgcn_readfirstlane(in_pool ? (uint32_t)(rows - 1) * rs + D * 2u : 0u));
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        k[mt][i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (uint32_t)(16 * mt + col) * rs + 64u * i + 16u * quad, 0, 0);
+    old = keep && lane < rows ? in[key + lane] : 0.f;
+  };
+  auto reduce = [&](const u32x4 (&k)[2][4], float old, int t) {
+    float sum[2] = {0.f, 0.f};
+    for (int h0 = 0; h0 < p.g; h0 += 16 * NT) {
+      if (NT == 4 && p.g > 64) load_heads(h0);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[nt][i], as_bf16x8(k[mt][i]), s, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)  // an infinite key times a row of no head is NaN
+            sum[mt] += base[nt][e] != -INFINITY ? __builtin_amdgcn_exp2f(fmaf(s[e], p.scale_log2, base[nt][e])) : 0.f;
+        }
+    }
+    const float s0 = sum_rows(sum[0]), s1 = sum_rows(sum[1]);
+    const int key = t * kKeysPerTile + lane;
+    if (lane < kKeysPerTile && key < L) {
+      const float w = lane < 16 ? s0 : s1;
+      out[key] = keep ? fmaf(p.decay, old, w) : w;
+    }
+  };
+  u32x4 k[2][4];
+  float old;
+  load(k, old, t);
+  for (; t + kWeightWaves < end; t += kWeightWaves) {
+    u32x4 next[2][4];
+    float next_old;
+    load(next, next_old, t + kWeightWaves);
+    reduce(k, old, t);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[mt][i] = next[mt][i];
+    old = next_old;
+  }
+  reduce(k, old, t);
+}
+
+// ---------------------------------------------------------------- eviction
+
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kBins = 2048;
+constexpr int kMoveRows = 64;  // rows a workgroup of move_kernel takes at a time
+
+struct EvictParams {
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const int32_t* totals;
+  const float* w_in;
+  const int32_t* p_in;
+  float* w_out;
+  int32_t* p_out;
+  int64_t stride;
+  int32_t* moves;      // workspace: per (sequence, KV head) a count, then `most` target rows and `most` source rows
+  int64_t move_ints;   // integers of one
+  int most;
+  int B, H_KV, L_K, budget, sinks, recent, page_size, max_pages, num_pages;
+  Div div_page, div_heads;
+  // move_kernel
+  uint16_t* k;
+  uint16_t* v;
+  int32_t* lens_out;
+  int32_t* free_pages;
+  const int32_t* taken;
+  int32_t* taken_out;   // nullable: pages are not given back
+  int num_free;
+  int groups;           // workgroups a (sequence, KV head)
+  Div div_groups;
+};
+
+// Weights in the order of unsigned numbers; NaN below all, both zeros alike.
+__device__ __forceinline__ uint32_t order_of(float w) {
+  const uint32_t u = __float_as_uint(w + 0.0f);
+  return w != w ? 0u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// Sums of x and y over the threads before this one.  Two barriers; `sums` is
+// free for the next call after them.
+__device__ __forceinline__ int2 scan_before(int x, int y, int2* sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int sx = wave_scan(x), sy = wave_scan(y);
+  if (lane == 63) sums[wave] = make_int2(sx, sy);
+  __syncthreads();
+  int2 before = make_int2(sx - x, sy - y);
+  for (int w = 0; w < wave; ++w) {
+    before.x += sums[w].x;
+    before.y += sums[w].y;
+  }
+  __syncthreads();
+  return before;
+}
+
+// The rows of one (sequence, KV head) that stay.  With more than `budget` rows,
+// those of the `budget` largest keys do, where a key is the row's weight (all
+// ones for a protected row), of equal ones the lowest rows.  The budget-th
+// largest key comes from three histograms in LDS of 11, 11 and 10 bits: each
+// fixes the bits of its digit and the number still to be found among the keys
+// that share them.  A thread holds consecutive rows, so one scan over the
+// threads ranks the equal keys, and another the evicted rows below the budget
+// (holes) and the kept ones above it: the i-th of these moves into the i-th
+// hole, in place and without an order among the moves.  EACH rows of a thread
+// stay in registers, or (0) are read anew for each step.
+template <int EACH>
+__global__ void __launch_bounds__(kSelectThreads) select_kernel(EvictParams p) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ int2 sums[kSelectWaves];
+  __shared__ uint32_t found[2];
+  const int tid = threadIdx.x;
+  const int unit = blockIdx.x, b = div_by(unit, p.div_heads);
+  const int L = max(0, min(p.seq_lens[b], p.L_K)), total = p.totals[b];
+  const float* w_in = p.w_in + unit * p.stride;
+  const int32_t* p_in = p.p_in + unit * p.stride;
+  float* w_out = p.w_out + unit * p.stride;
+  int32_t* p_out = p.p_out + unit * p.stride;
+  int32_t* moves = p.moves + unit * p.move_ints;
+  if (L <= p.budget) {
+    if (tid == 0) moves[0] = 0;
+    if (w_in != w_out)
+      for (int r = tid; r < L; r += kSelectThreads) w_out[r] = w_in[r];
+    if (p_in != p_out)
+      for (int r = tid; r < L; r += kSelectThreads) p_out[r] = p_in[r];
+    return;
+  }
+  const int each = (L + kSelectThreads - 1) / kSelectThreads;
+  const int r0 = min((int64_t)tid * each, (int64_t)L), r1 = min((int64_t)r0 + each, (int64_t)L);
+  const int shift = (int)((uint32_t)total - (uint32_t)L);  // position of a row that no eviction has placed: row + shift
+  auto position = [&](int r) {
+    const int at = p_in[r];
+    return at >= 0 ? at : (int)((uint32_t)r + (uint32_t)shift);
+  };
+  auto read_key = [&](int r) {
+    const int at = position(r);
+    return at < p.sinks || (int64_t)at >= (int64_t)total - p.recent ? 0xffffffffu : order_of(w_in[r]);
+  };
+  uint32_t held[EACH > 0 ? EACH : 1];
+  if constexpr (EACH > 0) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) held[e] = r0 + e < r1 ? read_key(r0 + e) : 0u;
+  }
+  // f(row, key) for the thread's rows in order
+  auto rows = [&](auto f) {
+    if constexpr (EACH > 0) {
+#pragma unroll
+      for (int e = 0; e < EACH; ++e)
+        if (r0 + e < r1) f(r0 + e, held[e]);
+    } else {
+      for (int r = r0; r < r1; ++r) f(r, read_key(r));
+    }
+  };
+
+  uint32_t prefix = 0, mask = 0;
+  uint32_t want = (uint32_t)p.budget;  // of the keys that share the prefix, the want-th largest is the last to stay
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t bits = pass == 2 ? 1023u : 2047u;
+    hist[tid] = 0;
+    hist[tid + kSelectThreads] = 0;
+    __syncthreads();
+    rows([&](int, uint32_t key) {
+      if ((key & mask) == prefix) atomicAdd(&hist[(key >> low) & bits], 1u);
+    });
+    __syncthreads();
+    // from the largest digit down: thread t has 2047 - 2t and the one below it
+    const uint32_t a = hist[kBins - 1 - 2 * tid], c = hist[kBins - 2 - 2 * tid];
+    const uint32_t before = (uint32_t)scan_before((int)(a + c), 0, sums).x;
+    if (before < want && want <= before + a + c) {
+      const bool upper = want <= before + a;
+      found[0] = (uint32_t)(kBins - 1 - 2 * tid - (upper ? 0 : 1));
+      found[1] = want - before - (upper ? 0u : a);
+    }
+    __syncthreads();
+    prefix |= found[0] << low;
+    mask |= bits << low;
+    want = found[1];
+  }
+
+  int equal = 0;
+  rows([&](int, uint32_t key) { equal += key == prefix; });
+  int rank = scan_before(equal, 0, sums).x;
+  const int rank0 = rank;
+  int holes = 0, late = 0;
+  rows([&](int r, uint32_t key) {
+    const bool stays = key > prefix || (key == prefix && rank < (int)want);
+    rank += key == prefix;
+    holes += !stays && r < p.budget;
+    late += stays && r >= p.budget;
+  });
+  const int2 at = scan_before(holes, late, sums);
+  if (tid == kSelectThreads - 1) found[0] = (uint32_t)min(at.x + holes, p.most);
+  // a thread's rows and places of its row in the pool; the lists hold rows first
+  int32_t* to = moves + 1;
+  int32_t* from = moves + 1 + p.most;
+  rank = rank0;
+  int hole = at.x, mover = at.y;
+  rows([&](int r, uint32_t key) {
+    const bool stays = key > prefix || (key == prefix && rank < (int)want);
+    rank += key == prefix;
+    if (r < p.budget) {
+      if (!stays) {
+        if (hole < p.most) to[hole] = r;
+        ++hole;
+      } else {
+        if (w_in != w_out) w_out[r] = w_in[r];
+        p_out[r] = position(r);
+      }
+    } else if (stays) {
+      if (mover < p.most) from[mover] = r;
+      ++mover;
+    }
+  });
+  __syncthreads();
+  const int count = (int)found[0];
+  if (tid == 0) moves[0] = count;
+  auto pool_row = [&](int r) {
+    const int j = div_by(r, p.div_page);
+    const int page = p.block_table[(int64_t)b * p.max_pages + j];
+    return page >= 0 && page < p.num_pages ? page * p.page_size + (r - j * p.page_size) : -1;
+  };
+  for (int i = tid; i < count; i += kSelectThreads) {
+    const int d = to[i], s = from[i];
+    w_out[d] = w_in[s];
+    p_out[d] = position(s);
+    to[i] = pool_row(d);
+    from[i] = pool_row(s);
+  }
+  __syncthreads();
+  for (int r = p.budget + tid; r < L; r += kSelectThreads) {
+    w_out[r] = 0.f;
+    p_out[r] = -1;
+  }
+}
+
+// The rows into their places, and (block 0) the lengths and the pages that come
+// free.  A head's row of K or V is 16 lanes of 16 bytes; a wave moves four rows
+// of both at a time.  Targets lie below the budget and sources above it, so no
+// move meets another.
+__global__ void __launch_bounds__(256) move_kernel(EvictParams p) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x > 0) {
+    const int blk = (int)blockIdx.x - 1;
+    const int unit = div_by(blk, p.div_groups), part = blk - unit * p.groups;
+    const int h = unit - div_by(unit, p.div_heads) * p.H_KV;
+    const int32_t* moves = p.moves + unit * p.move_ints;
+    const int count = moves[0];
+    const int32_t* to = moves + 1;
+    const int32_t* from = moves + 1 + p.most;
+    for (int i0 = part * kMoveRows; i0 < count; i0 += p.groups * kMoveRows) {
+      u32x4 x[4][2];
+      int d[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 16 + wave * 4 + (lane >> 4);
+        d[u] = i < count ? to[i] : -1;
+        const int s = i < count ? from[i] : -1;
+        x[u][0] = x[u][1] = u32x4{0u, 0u, 0u, 0u};  // a page outside the pool reads as zeros
+        if (s >= 0) {
+          const int64_t at = ((int64_t)s * p.H_KV + h) * D + 8 * (lane & 15);
+          x[u][0] = *reinterpret_cast<const u32x4*>(p.k + at);
+          x[u][1] = *reinterpret_cast<const u32x4*>(p.v + at);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (d[u] < 0) continue;
+        const int64_t at = ((int64_t)d[u] * p.H_KV + h) * D + 8 * (lane & 15);
+        *reinterpret_cast<u32x4*>(p.k + at) = x[u][0];
+        *reinterpret_cast<u32x4*>(p.v + at) = x[u][1];
+      }
+    }
+    return;
+  }
+  // Sequences in order, 256 at a time: their pages past the budget by one scan,
+  // then a page a thread, its sequence by bisection.
+  __shared__ int32_t wave_sum[4];
+  __shared__ int32_t starts[256];
+  const int first_page = (p.budget + p.page_size - 1) / p.page_size;
+  auto length = [&](int b) { return b < p.B ? max(0, min(p.seq_lens[b], p.L_K)) : 0; };
+  auto pages_gone = [&](int L) { return L > p.budget ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
+  int all = 0;
+  if (p.taken_out) {
+    for (int b = tid; b < p.B; b += 256) all += pages_gone(length(b));
+    all = __builtin_amdgcn_readlane(wave_scan(all), 63);
+    if (lane == 0) wave_sum[wave] = all;
+    __syncthreads();
+    all = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+    __syncthreads();
+  }
+  const int taken = p.taken_out ? max(0, min(*p.taken, p.num_free)) : 0;
+  int at0 = taken - all;  // the place of the first page; the list has none for those below 0
+  for (int b0 = 0; b0 < p.B; b0 += 256) {
+    const int L = length(b0 + tid);
+    if (p.taken_out) {
+      const int n = pages_gone(L), upto = wave_scan(n);
+      if (lane == 63) wave_sum[wave] = upto;
+      __syncthreads();
+      int before = upto - n;
+      for (int w = 0; w < wave; ++w) before += wave_sum[w];
+      starts[tid] = before;
+      const int sum = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+      __syncthreads();
+      for (int e = tid; e < sum; e += 256) {
+        int lo = 0, hi = 256;  // the last sequence that starts at or before e
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (starts[mid] <= e)
+            lo = mid;
+          else
+            hi = mid;
+        }
+        if (at0 + e >= 0)
+          p.free_pages[at0 + e] = p.block_table[(int64_t)(b0 + lo) * p.max_pages + first_page + (e - starts[lo])];
+      }
+      at0 += sum;
+      __syncthreads();
+    }
+    if (b0 + tid < p.B) p.lens_out[b0 + tid] = min(L, p.budget);
+  }
+  if (p.taken_out && tid == 0) *p.taken_out = max(0, taken - all);
+}
+
+// ---------------------------------------------------------------- host side
+
+int launched(hipError_t e, const char* what) {
+  return e == hipSuccess ? (int)DA_OK : da::fail(DA_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
+}
+
+int most_moves(int L_K_max, int budget) { return std::max(0, std::min(budget, L_K_max - budget)); }
+
+// Workspace bytes of an eviction, without the counters at its end.
+int64_t move_bytes(int B, int H_KV, int L_K_max, int budget) {
+  return 4ll * B * H_KV * (1 + 2ll * most_moves(L_K_max, budget));
+}
+
+}  // namespace
+
+extern "C" {
+
+int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_table, const int32_t* seq_lens,
+                       const float* lse, const float* weights, float* weights_out, int64_t weight_stride, int B,
+                       int H_Q, int H_KV, int page_size, int max_pages, int num_pages, int L_K_max, int d,
+                       float softmax_scale, float decay, void* stream) {
+  da::clear_error();
+  int rc = da::check_shape(B, H_Q, H_KV, L_K_max, d);
+  if (!q || !block_table || !seq_lens || !lse || !weights || !weights_out)
+    return da::fail(DA_ERR_NULL, "q, block_table, seq_lens, lse, weights and weights_out must be non-NULL");
+  if (!k_cache && !(rc == DA_OK && L_K_max == 0)) return da::fail(DA_ERR_NULL, "k_cache must be non-NULL");
+  if (rc) return rc;
+  rc = da::check_page_table(B, page_size, max_pages, num_pages, L_K_max);
+  if (rc) return rc;
+  if (H_Q / H_KV > (1 << 16)) return da::fail(DA_ERR_SHAPE, "%d query heads a KV head", H_Q / H_KV);
+  if (weight_stride < L_K_max)
+    return da::fail(DA_ERR_SHAPE, "weight_stride=%lld is less than L_K_max=%d", (long long)weight_stride, L_K_max);
+  if (!(decay >= 0.f && decay <= 1.f)) return da::fail(DA_ERR_ARG, "decay must be in [0, 1]");
+  if (!aligned(q, 16) || !aligned(k_cache, 16))
+    return da::fail(DA_ERR_ALIGN, "q and k_cache must be 16-byte aligned");
+  if (!aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(lse, 4) || !aligned(weights, 4) ||
+      !aligned(weights_out, 4))
+    return da::fail(DA_ERR_ALIGN, "block_table, seq_lens, lse and weights must be 4-byte aligned");
+  int cus = 0;
+  rc = ensure_gfx950(&cus);
+  if (rc || L_K_max == 0) return rc;
+  WeightParams p{};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k_cache);
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.lse = lse;
+  p.in = weights;
+  p.out = weights_out;
+  p.stride = weight_stride;
+  p.B = B;
+  p.H_Q = H_Q;
+  p.H_KV = H_KV;
+  p.g = H_Q / H_KV;
+  p.L_K = L_K_max;
+  p.page_size = page_size;
+  p.max_pages = max_pages;
+  p.num_pages = num_pages;
+  p.div_page = make_div((uint32_t)page_size);
+  p.div_heads = make_div((uint32_t)H_KV);
+  // four workgroups a CU, of one tile a wave at least
+  const int64_t tiles = (L_K_max + kKeysPerTile - 1) / kKeysPerTile, units = (int64_t)B * H_KV;
+  int64_t each = (tiles * units + 4 * cus - 1) / (4 * cus);
+  each = std::min<int64_t>(std::max<int64_t>(4, (each + 3) / 4 * 4), kMostChunkTiles);
+  p.chunk_tiles = (int)each;
+  p.chunks = (int)((tiles + each - 1) / each);
+  p.div_chunks = make_div((uint32_t)p.chunks);
+  if (units * p.chunks >= ((int64_t)1 << 31))
+    return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many workgroups", B, H_KV, L_K_max);
+  p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * kLog2e;
+  p.decay = decay;
+  const void* fn = p.g <= 16   ? reinterpret_cast<const void*>(&weights_kernel<1>)
+                   : p.g <= 32 ? reinterpret_cast<const void*>(&weights_kernel<2>)
+                               : reinterpret_cast<const void*>(&weights_kernel<4>);
+  void* args[] = {&p};
+  return launched(hipLaunchKernel(fn, dim3((uint32_t)(units * p.chunks)), dim3(64 * kWeightWaves), args, 0,
+                                  static_cast<hipStream_t>(stream)),
+                  "key weight");
+}
+
+size_t da_evict_workspace_bytes(int B, int H_KV, int L_K_max, int budget) {
+  if (B <= 0 || B > DA_MAX_REQUESTS || H_KV <= 0 || L_K_max < 0 || budget < 1 || (int64_t)B * H_KV > (1 << 24)) return 0;
+  const int64_t bytes = move_bytes(B, H_KV, L_K_max, budget);
+  return (size_t)((bytes + 255) / 256 * 256) + DA_ARRIVAL_BYTES;
+}
+
+int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* seq_lens,
+                const int32_t* totals, const float* weights, const int32_t* positions, float* weights_out,
+                int32_t* positions_out, int64_t weight_stride, int32_t* lens_out, int32_t* free_pages,
+                const int32_t* taken, int32_t* taken_out, int num_free, int B, int H_KV, int page_size, int max_pages,
+                int num_pages, int L_K_max, int d, int budget, int sinks, int recent, void* workspace,
+                size_t workspace_bytes, void* stream) {
+  da::clear_error();
+  int rc = da::check_shape(B, H_KV, H_KV, L_K_max, d);
+  if (!block_table || !seq_lens || !totals || !weights || !positions || !weights_out || !positions_out || !lens_out)
+    return da::fail(DA_ERR_NULL, "tables, lengths, totals, weights and positions must be non-NULL");
+  if ((!k_cache || !v_cache) && !(rc == DA_OK && L_K_max == 0))
+    return da::fail(DA_ERR_NULL, "k_cache and v_cache must be non-NULL");
+  if ((free_pages || taken_out) && (!taken || !taken_out || (!free_pages && num_free > 0)))
+    return da::fail(DA_ERR_NULL, "free_pages, taken and taken_out go together");
+  if (rc) return rc;
+  rc = da::check_page_table(B, page_size, max_pages, num_pages, L_K_max);
+  if (rc) return rc;
+  if (B > DA_MAX_REQUESTS) return da::fail(DA_ERR_SHAPE, "B=%d exceeds %d", B, DA_MAX_REQUESTS);
+  if ((int64_t)num_pages * page_size >= ((int64_t)1 << 31))
+    return da::fail(DA_ERR_SHAPE, "num_pages=%d pages of %d rows: rows have 32 bits", num_pages, page_size);
+  if (weight_stride < L_K_max)
+    return da::fail(DA_ERR_SHAPE, "weight_stride=%lld is less than L_K_max=%d", (long long)weight_stride, L_K_max);
+  if (num_free < 0) return da::fail(DA_ERR_SHAPE, "num_free=%d is negative", num_free);
+  if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
+    return da::fail(DA_ERR_ARG, "budget=%d must be positive and hold sinks=%d and recent=%d", budget, sinks, recent);
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16))
+    return da::fail(DA_ERR_ALIGN, "k_cache and v_cache must be 16-byte aligned");
+  for (const void* x : {(const void*)block_table, (const void*)seq_lens, (const void*)totals, (const void*)weights,
+                        (const void*)positions, (const void*)weights_out, (const void*)positions_out,
+                        (const void*)lens_out, (const void*)free_pages, (const void*)taken, (const void*)taken_out})
+    if (!aligned(x, 4)) return da::fail(DA_ERR_ALIGN, "tables, lengths, weights and positions must be 4-byte aligned");
+  if (workspace && !aligned(workspace, 16)) return da::fail(DA_ERR_ALIGN, "workspace must be 16-byte aligned");
+  if (move_bytes(B, H_KV, L_K_max, budget) >= ((int64_t)1 << 40))
+    return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many rows", B, H_KV, L_K_max);
+  const size_t need = da_evict_workspace_bytes(B, H_KV, L_K_max, budget);
+  if (!workspace || workspace_bytes < need)
+    return da::fail(DA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
+  int cus = 0;
+  rc = ensure_gfx950(&cus);
+  if (rc) return rc;
+  EvictParams p{};
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.totals = totals;
+  p.w_in = weights;
+  p.p_in = positions;
+  p.w_out = weights_out;
+  p.p_out = positions_out;
+  p.stride = weight_stride;
+  p.moves = static_cast<int32_t*>(workspace);
+  p.most = most_moves(L_K_max, budget);
+  p.move_ints = 1 + 2ll * p.most;
+  p.B = B;
+  p.H_KV = H_KV;
+  p.L_K = L_K_max;
+  p.budget = budget;
+  p.sinks = sinks;
+  p.recent = recent;
+  p.page_size = page_size;
+  p.max_pages = max_pages;
+  p.num_pages = num_pages;
+  p.div_page = make_div((uint32_t)page_size);
+  p.div_heads = make_div((uint32_t)H_KV);
+  p.k = static_cast<uint16_t*>(k_cache);
+  p.v = static_cast<uint16_t*>(v_cache);
+  p.lens_out = lens_out;
+  p.free_pages = free_pages;
+  p.taken = taken;
+  p.taken_out = taken_out;
+  p.num_free = num_free;
+  const int64_t units = (int64_t)B * H_KV;
+  void* args[] = {&p};
+  const void* fn = L_K_max <= 4 * kSelectThreads    ? reinterpret_cast<const void*>(&select_kernel<4>)
+                   : L_K_max <= 8 * kSelectThreads  ? reinterpret_cast<const void*>(&select_kernel<8>)
+                   : L_K_max <= 16 * kSelectThreads ? reinterpret_cast<const void*>(&select_kernel<16>)
+                                                    : reinterpret_cast<const void*>(&select_kernel<0>);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  rc = launched(hipLaunchKernel(fn, dim3((uint32_t)units), dim3(kSelectThreads), args, 0, s), "select");
+  if (rc) return rc;
+  // eight workgroups a CU at most; a workgroup that finds nothing to move ends at once
+  const int64_t parts = (p.most + kMoveRows - 1) / kMoveRows;
+  p.groups = (int)std::max<int64_t>(1, std::min<int64_t>(parts, (8ll * cus + units - 1) / units));
+  p.div_groups = make_div((uint32_t)p.groups);
+  const int64_t grid = 1 + (p.most ? units * p.groups : 0);
+  return launched(hipLaunchKernel(reinterpret_cast<const void*>(&move_kernel), dim3((uint32_t)grid), dim3(256), args, 0, s),
+                  "move");
+}
+
+}  // extern "C"

@@ -56,3 +56,73 @@ def test_oracle_of_one_axis(neighbours):
     c = norm_rotate_axes(x, w, 1e-5, rope, np.stack([1 - pos, pos]), [1] * 31 + [0], neighbours)[0]
     keep = [i for i in range(128) if i not in ((62, 63) if neighbours else (31, 63))]
     assert np.array_equal(a[0][..., keep], c[..., keep]) and not np.array_equal(a[0], c)
+
+
+def weights_call(lib, q=FAKE, k=FAKE, table=FAKE, lens=FAKE, lse=FAKE, w=FAKE, out=FAKE, stride=2048, B=2, H_Q=8, H_KV=1,
+                 page=64, max_pages=32, pages=64, L=2048, d=128, decay=1.0):
+    return lib.da_add_key_weights(q, k, table, lens, lse, w, out, stride, B, H_Q, H_KV, page, max_pages, pages, L, d, 0.0,
+                                  decay, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(table=None), NULL), (dict(lens=None), NULL), (dict(lse=None), NULL),
+    (dict(w=None), NULL), (dict(out=None), NULL), (dict(B=0), SHAPE), (dict(H_Q=9, H_KV=2), SHAPE), (dict(L=-1), SHAPE),
+    (dict(max_pages=31), SHAPE), (dict(stride=2047), SHAPE), (dict(stride=-1), SHAPE), (dict(H_Q=1 << 17, B=1), SHAPE),
+    (dict(d=64), UNSUP), (dict(page=48), UNSUP), (dict(decay=-0.5), ARG), (dict(decay=1.5), ARG),
+    (dict(decay=float("nan")), ARG), (dict(q=FAKE + 8), ALIGN), (dict(k=FAKE + 2), ALIGN), (dict(lse=FAKE + 2), ALIGN),
+    (dict(w=FAKE + 1), ALIGN), (dict(out=FAKE + 2), ALIGN), (dict(table=FAKE + 2), ALIGN), (dict(lens=FAKE + 1), ALIGN),
+])
+def test_weight_refusals(lib, kw, code):
+    refused(weights_call(lib, **kw), code)
+
+
+def evict_call(lib, k=FAKE, v=FAKE, table=FAKE, lens=FAKE, totals=FAKE, w=FAKE, p=FAKE, wo=FAKE, po=FAKE, stride=2048,
+               lo=FAKE, free=FAKE, taken=FAKE, to=FAKE, num_free=10, B=2, H_KV=2, page=64, max_pages=32, pages=64, L=2048,
+               d=128, budget=100, sinks=4, recent=8, ws=FAKE, ws_bytes=1 << 30):
+    return lib.da_evict_kv(k, v, table, lens, totals, w, p, wo, po, stride, lo, free, taken, to, num_free, B, H_KV, page,
+                           max_pages, pages, L, d, budget, sinks, recent, ws, ws_bytes, None)
+
+
+WS = -6
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(k=None), NULL), (dict(v=None), NULL), (dict(table=None), NULL), (dict(lens=None), NULL),
+    (dict(totals=None), NULL), (dict(w=None), NULL), (dict(p=None), NULL), (dict(wo=None), NULL), (dict(po=None), NULL),
+    (dict(lo=None), NULL), (dict(taken=None), NULL), (dict(to=None), NULL), (dict(free=None), NULL),
+    (dict(B=0), SHAPE), (dict(B=4097), SHAPE), (dict(H_KV=0), SHAPE), (dict(L=-1), SHAPE), (dict(max_pages=31), SHAPE),
+    (dict(stride=2047), SHAPE), (dict(num_free=-1), SHAPE), (dict(pages=1 << 25), SHAPE), (dict(d=64), UNSUP),
+    (dict(page=16), UNSUP), (dict(budget=0), ARG), (dict(budget=-3), ARG), (dict(sinks=-1), ARG), (dict(recent=-1), ARG),
+    (dict(sinks=60, recent=41), ARG), (dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1), ARG), (dict(k=FAKE + 8), ALIGN),
+    (dict(v=FAKE + 2), ALIGN), (dict(table=FAKE + 2), ALIGN), (dict(w=FAKE + 1), ALIGN), (dict(po=FAKE + 2), ALIGN),
+    (dict(free=FAKE + 2), ALIGN), (dict(ws=FAKE + 8), ALIGN), (dict(ws=None), WS), (dict(ws_bytes=1 << 20), WS),
+])
+def test_evict_refusals(lib, kw, code):
+    refused(evict_call(lib, **kw), code)
+
+
+def test_evict_workspace_bytes():
+    # a count and two lists of the rows that may move, a sequence and head; counters of other calls behind
+    assert da.da_evict_workspace_bytes(1, 1, 100, 60) == 512 + (1 << 20)      # 4 (1 + 80) bytes
+    assert da.da_evict_workspace_bytes(2, 8, 4097, 4096) == 256 + (1 << 20)
+    assert da.da_evict_workspace_bytes(2, 8, 100, 200) == 256 + (1 << 20)     # nothing ever moves
+    for bad in ((0, 1, 10, 5), (4097, 1, 10, 5), (1, 0, 10, 5), (1, 1, -1, 5), (1, 1, 10, 0)):
+        assert da.da_evict_workspace_bytes(*bad) == 0
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls would run")
+def test_calls_that_pass_the_checks_reach_the_device_check(lib):
+    for rc in (axes_call(lib), axes_call(lib, True), weights_call(lib), evict_call(lib),
+               evict_call(lib, free=None, taken=None, to=None, num_free=0)):
+        assert rc in (-7, UNSUP)
+
+
+def test_python_refuses_tensors_of_the_cpu():
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError):
+        da.da_add_key_weights(bf(1, 8, 128), bf(2, 32, 1, 128), ints(1, 2), ints(1), torch.zeros(1, 8), torch.zeros(1, 1, 64),
+                              64)
+    with pytest.raises(ValueError):
+        da.da_evict_kv(bf(2, 32, 1, 128), bf(2, 32, 1, 128), ints(1, 2), ints(1), ints(1), torch.zeros(1, 1, 64),
+                       ints(1, 1, 64), 32, 64)
