@@ -676,6 +676,49 @@ int da_decode_attn_kv4(const void* q, const void* cache, const int32_t* block_ta
 size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t pool_keys, int window, int sinks,
                               int num_splits, int num_cus);
 
+/* Decode attention of a batch in which groups of sequences begin with the same
+ * keys (a system prompt, a document, the samples of one request): the result of
+ * da_decode_attn_paged, but a group's shared keys are read once for all its
+ * query rows, as one matrix product with them.
+ *   cu_groups    device int32 [G + 1], 0 <= cu_groups[0] <= ... <= cu_groups[G]
+ *                <= B: group i is the sequences [cu_groups[i], cu_groups[i + 1]).
+ *                Sequences outside all groups share nothing; nor do any where
+ *                the entries decrease
+ *   prefix_lens  device int32 [G]: the first prefix_lens[i] keys of every sequence
+ *                of group i are the same (where a sequence is shorter, all its
+ *                keys); G may be 0
+ *   block_table, seq_lens  as for da_decode_attn_paged, whole sequences, prefix
+ *                included: the table rows of a group repeat the pages of its
+ *                prefix, or hold copies.  Shared keys are read through the row of
+ *                the group's first sequence that has keys, up to the last whole
+ *                32 keys that all of its sequences with keys have; what follows,
+ *                through each sequence's own
+ *   chunk_keys   <= 0: the length of chunks that the work is cut into is chosen on
+ *                the device by the batch's lengths and groups; else that many
+ *                keys, in whole tiles of 32 (at most 64 chunks of a prefix or of
+ *                a sequence's own keys, and longer ones where the workspace
+ *                holds no more)
+ *   workspace    >= da_prefix_workspace_bytes(B, G, H_Q, H_KV, 0); its last
+ *                DA_ARRIVAL_BYTES are not touched, so the other calls' may be
+ *                shared
+ * Three launches; replays of a captured call follow the lengths and groups the
+ * device then holds.  Results are bit-identical across runs for the same
+ * arguments, lengths and groups of the whole batch.  Probabilities are rounded to
+ * bf16 for the product with V, as in da_decode_attn; lse takes them in 32 bits.
+ * A NaN among a sequence's keys or in a query reaches the output and lse of the
+ * heads that read it.  Other arguments and errors as for da_decode_attn_paged,
+ * and DA_ERR_SHAPE for B above DA_MAX_REQUESTS, G above B, H_KV above 2^16 or B
+ * H_Q above 2^22. */
+int da_decode_attn_prefix(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_table,
+                          const int32_t* seq_lens, const int32_t* cu_groups, const int32_t* prefix_lens, void* out,
+                          float* lse_out, int B, int G, int H_Q, int H_KV, int page_size, int max_pages, int num_pages,
+                          int L_K_max, int d, float softmax_scale, int chunk_keys, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Workspace bytes da_decode_attn_prefix needs (num_cus 0: query the current
+ * device); 0 for a shape it does not take. */
+size_t da_prefix_workspace_bytes(int B, int G, int H_Q, int H_KV, int num_cus);
+
 /* The attention weight that each key of a paged bf16 cache received in a step,
  * summed over the query heads that share its KV head, and over steps:
  *   weights_out[b][kvh][j] = decay weights[b][kvh][j] +

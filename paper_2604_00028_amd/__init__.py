@@ -11,7 +11,8 @@ from ._binding import (DA_OK, EXPORTS, POLICY_EVOLVED, POLICY_MI355X, POLICY_PAP
                        da_device_info, da_last_error, da_make_plan, da_model_time, da_make_schedule, da_prefers_dealt, da_schedule_max_bytes, da_schedule_workspace_bytes, da_split_bounds, da_split_partials,
                        da_strerror, da_workspace_bytes, load, KV4_TILE_BYTES, MAX_REQUESTS,
                        da_append_kv, da_append_kv4, da_append_kv4_axes, da_append_kv_axes,
-                       da_add_key_weights, da_evict_kv, da_evict_workspace_bytes,
+                       da_add_key_weights, da_decode_attn_prefix, da_evict_kv, da_evict_workspace_bytes,
+                       da_prefix_workspace_bytes,
                        da_decode_attn_kv4, da_decode_attn_window, da_extend_tables,
                        da_kv4_workspace_bytes, da_read_kv4, da_window_keys)
 
@@ -24,6 +25,6 @@ __all__ = [
     "da_schedule_max_bytes", "da_schedule_workspace_bytes", "da_split_bounds", "da_split_partials", "da_strerror",
     "da_workspace_bytes", "load", "KV4_TILE_BYTES", "MAX_REQUESTS",
     "da_append_kv", "da_append_kv4", "da_append_kv4_axes", "da_append_kv_axes", "da_decode_attn_kv4",
-    "da_add_key_weights", "da_evict_kv", "da_evict_workspace_bytes", "da_decode_attn_window", "da_extend_tables",
+    "da_add_key_weights", "da_decode_attn_prefix", "da_evict_kv", "da_evict_workspace_bytes", "da_prefix_workspace_bytes", "da_decode_attn_window", "da_extend_tables",
     "da_kv4_workspace_bytes", "da_read_kv4", "da_window_keys",
 ]

@@ -51,7 +51,8 @@ EXPORTS = (
     "da_make_schedule", "da_schedule_workspace_bytes",
     "da_decode_attn_scheduled", "da_decode_attn_dealt", "da_dealt_workspace_bytes", "da_prefers_dealt",
     "da_decode_attn_window", "da_window_keys", "da_extend_tables", "da_append_kv", "da_append_kv4", "da_read_kv4",
-    "da_append_kv_axes", "da_append_kv4_axes", "da_add_key_weights", "da_evict_kv", "da_evict_workspace_bytes", "da_decode_attn_kv4", "da_kv4_workspace_bytes",
+    "da_append_kv_axes", "da_append_kv4_axes", "da_add_key_weights", "da_evict_kv", "da_evict_workspace_bytes",
+    "da_decode_attn_prefix", "da_prefix_workspace_bytes", "da_decode_attn_kv4", "da_kv4_workspace_bytes",
     "da_split_partials", "da_combine_splits", "da_device_info", "da_strerror",
     "da_last_error",
 )
@@ -191,6 +192,10 @@ def load() -> ctypes.CDLL:
     lib.da_decode_attn_kv4.restype = _I
     lib.da_kv4_workspace_bytes.argtypes = [_I] * 4 + [_L] + [_I] * 4
     lib.da_kv4_workspace_bytes.restype = _Z
+    lib.da_decode_attn_prefix.argtypes = [_P] * 9 + [_I] * 9 + [_F, _I, _P, _Z, _P]
+    lib.da_decode_attn_prefix.restype = _I
+    lib.da_prefix_workspace_bytes.argtypes = [_I] * 5
+    lib.da_prefix_workspace_bytes.restype = _Z
     lib.da_add_key_weights.argtypes = [_P] * 7 + [_L] + [_I] * 8 + [_F, _F, _P]
     lib.da_add_key_weights.restype = _I
     lib.da_evict_kv.argtypes = [_P] * 9 + [_L] + [_P] * 4 + [_I] * 11 + [_P, _Z, _P]
@@ -1156,6 +1161,55 @@ def _table_args(block_table: torch.Tensor, seq_lens: torch.Tensor, B: int, dev: 
     _need("block_table", block_table, _I32, (B, max_pages), dev)
     _need("seq_lens", seq_lens, _I32, (B,), dev)
     return _int(max_pages)
+
+
+def da_prefix_workspace_bytes(B: int, G: int, H_Q: int, H_KV: int, num_cus: int = 0) -> int:
+    return int(load().da_prefix_workspace_bytes(_int(B), _int(G), _int(H_Q), _int(H_KV), _int(num_cus)))
+
+
+def da_decode_attn_prefix(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                          seq_lens: torch.Tensor, cu_groups: torch.Tensor, prefix_lens: torch.Tensor, L_K_max: int,
+                          out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, *,
+                          softmax_scale: float = 0.0, chunk_keys: int = 0, workspace: Optional[torch.Tensor] = None,
+                          stream=None) -> torch.Tensor:
+    """Decode attention over a paged cache in which groups of sequences begin with
+    the same keys, which are read once a group; returns `out`.  Group i is the
+    sequences [cu_groups[i], cu_groups[i + 1]), whose first prefix_lens[i] keys are
+    the same; block_table and seq_lens hold whole sequences, as for
+    da_decode_attn_paged."""
+    dev = q.device
+    if q.dim() != 3 or q.dtype is not _BF16 or not q.is_contiguous() or not q.is_cuda:
+        raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")
+    B, H_Q, d = q.shape
+    num_pages, page_size, H_KV, dk = _paged_pool("k_cache", k_cache, dev)
+    if dk != d:
+        raise ValueError(f"k_cache has head dim {dk}, q {d}")
+    _need("v_cache", v_cache, _BF16, k_cache.shape, dev)
+    max_pages = _table_args(block_table, seq_lens, B, dev)
+    if prefix_lens.dim() != 1:
+        raise ValueError("prefix_lens must have one dimension")
+    G = prefix_lens.shape[0]
+    _need("prefix_lens", prefix_lens, _I32, (G,), dev)
+    _need("cu_groups", cu_groups, _I32, (G + 1,), dev)
+    if dev.index != _get_device():
+        return _on_device(dev, da_decode_attn_prefix, q, k_cache, v_cache, block_table, seq_lens, cu_groups, prefix_lens,
+                          L_K_max, out, lse_out, softmax_scale=softmax_scale, chunk_keys=chunk_keys,
+                          workspace=workspace, stream=stream)
+    out = _outputs(q, out, lse_out, stream)
+    s_handle = _stream(dev, stream)
+    L, chunk_keys = _int(int(L_K_max)), _int(int(chunk_keys))
+    ws, capture = (_usable(workspace, dev), 0) if workspace is not None else _offered_now(dev, stream, s_handle)
+    while True:
+        rc = load().da_decode_attn_prefix(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
+                                          _ptr(cu_groups), _ptr(prefix_lens), _ptr(out), _ptr(lse_out), B, G, H_Q, H_KV,
+                                          _int(page_size), max_pages, _int(num_pages), L, d, softmax_scale, chunk_keys,
+                                          _ptr(ws), _nbytes(ws), s_handle)
+        if rc != DA_ERR_WORKSPACE or workspace is not None:
+            break
+        workspace = ws = _grown(dev, s_handle, capture, da_prefix_workspace_bytes(B, G, H_Q, H_KV))
+    if rc:
+        _check(rc)
+    return out
 
 
 def da_add_key_weights(q: torch.Tensor, k_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,

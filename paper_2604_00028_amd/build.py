@@ -26,7 +26,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libdecode_attn.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
-SOURCES = [os.path.join(CSRC, f) for f in ("decode_attn.hip", "kv4.hip", "cache_ops.hip", "evict.hip", "plan.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("decode_attn.hip", "kv4.hip", "cache_ops.hip", "evict.hip", "prefix.hip", "plan.cpp")]
 PROBE_NAME = "libhbm_probe.so"
 PROBE_PATH = os.path.join(HERE, PROBE_NAME)
 PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]

@@ -1,8 +1,6 @@
 """The operators of a shared and bounded cache on the CPU: refusals (every call
 below returns before any HIP call), host-side sizing, and their oracle."""
 
-import ctypes
-
 import numpy as np
 import pytest
 import torch
@@ -110,9 +108,35 @@ def test_evict_workspace_bytes():
         assert da.da_evict_workspace_bytes(*bad) == 0
 
 
+def prefix_call(lib, q=FAKE, k=FAKE, v=FAKE, table=FAKE, lens=FAKE, cu=FAKE, pre=FAKE, out=FAKE, lse=None, B=4, G=2, H_Q=8,
+                H_KV=1, page=64, max_pages=32, pages=64, L=2048, d=128, chunk=0, ws=FAKE, ws_bytes=1 << 40):
+    return lib.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, out, lse, B, G, H_Q, H_KV, page, max_pages, pages, L, d,
+                                     0.0, chunk, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(table=None), NULL), (dict(lens=None), NULL),
+    (dict(cu=None), NULL), (dict(pre=None), NULL), (dict(out=None), NULL), (dict(B=0), SHAPE), (dict(B=4097), SHAPE),
+    (dict(G=5), SHAPE), (dict(G=-1), SHAPE), (dict(H_Q=9, H_KV=2), SHAPE), (dict(L=-1), SHAPE), (dict(max_pages=31), SHAPE),
+    (dict(H_Q=1 << 17, H_KV=1 << 17, L=1, B=1, G=1), SHAPE), (dict(B=4096, H_Q=2048), SHAPE), (dict(d=64), UNSUP),
+    (dict(page=48), UNSUP), (dict(q=FAKE + 8), ALIGN), (dict(k=FAKE + 2), ALIGN), (dict(out=FAKE + 4), ALIGN),
+    (dict(cu=FAKE + 2), ALIGN), (dict(pre=FAKE + 1), ALIGN), (dict(lse=FAKE + 2), ALIGN), (dict(lens=FAKE + 2), ALIGN),
+    (dict(ws=FAKE + 4), ALIGN),
+])
+def test_prefix_refusals(lib, kw, code):
+    refused(prefix_call(lib, **kw), code)
+
+
+def test_prefix_workspace_bytes():
+    assert da.da_prefix_workspace_bytes(32, 1, 64, 8, 256) > 128 * 512 * 130 * 4 + (1 << 20)
+    for bad in ((0, 0, 8, 1), (4097, 1, 8, 1), (4, 5, 8, 1), (4, -1, 8, 1), (4, 1, 9, 2), (4096, 1, 2048, 1)):
+        assert da.da_prefix_workspace_bytes(*bad, 256) == 0
+
+
 @pytest.mark.skipif(torch.cuda.is_available(), reason="the calls would run")
 def test_calls_that_pass_the_checks_reach_the_device_check(lib):
-    for rc in (axes_call(lib), axes_call(lib, True), weights_call(lib), evict_call(lib),
+    for rc in (axes_call(lib), axes_call(lib, True), weights_call(lib), evict_call(lib), prefix_call(lib),
+               prefix_call(lib, G=0, cu=None, pre=None),
                evict_call(lib, free=None, taken=None, to=None, num_free=0)):
         assert rc in (-7, UNSUP)
 
