@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "decode_attn.h"
 #include "host.h"
@@ -42,17 +43,24 @@ struct WeightParams {
 // (sequence, KV head), its waves one tile in four; a wave's product has the
 // heads as rows and the keys as columns (S = Q K^T, the operands of the
 // attention kernels' S^T exchanged), so that a key's sum over 16 heads is three
-// additions and two lane exchanges.  K comes straight into the operand layout,
-// the next tile's loads in flight while one is reduced.  exp(x) = 2^(raw scale
-// log2 e - lse log2 e), one fma and one exponential a score; in 32 bits
-// throughout.  Up to 16 NT heads stay in registers; more (g > 64) are read anew
-// for each tile.
-template <int NT>
+// additions and two lane exchanges.  K is loaded row by row and takes its operand
+// layout by way of LDS, the next tile's loads in flight while one is reduced.
+// exp(x) = 2^(raw scale log2 e - lse log2 e), one fma and one exponential a
+// score; in 32 bits throughout.  Up to 16 NT heads stay in registers; more (g >
+// 64) are read anew for each tile.  AUX: the loads' cache policy (2: streaming).
+//
+// Bound by HBM: 32 sequences of 8192 keys of 8 heads (516 MB of K, 34 of
+// weights) 95 us, 5.8 TB/s; K straight into the operand layout 112.
+template <int NT, int AUX>
 __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(WeightParams p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
-  const int unit = div_by((int)blockIdx.x, p.div_chunks), chunk = (int)blockIdx.x - unit * p.chunks;
-  const int b = div_by(unit, p.div_heads), kvh = unit - b * p.H_KV;
+  // the heads of a chunk side by side, and each sequence's chunks turned by one: chunks that only long sequences have
+  // would else be the work of a few XCDs
+  const int item = div_by((int)blockIdx.x, p.div_heads), kvh = (int)blockIdx.x - item * p.H_KV;
+  const int b = div_by(item, p.div_chunks);
+  const int turned = item - b * p.chunks + (b - div_by(b, p.div_chunks) * p.chunks);
+  const int chunk = turned < p.chunks ? turned : turned - p.chunks;
   const int L = min(p.seq_lens[b], p.L_K);
   const int tiles = L > 0 ? (L + kKeysPerTile - 1) / kKeysPerTile : 0;
   const int first = chunk * p.chunk_tiles;
@@ -90,6 +98,8 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(WeightParams
   const float* in = p.in + ((int64_t)b * p.H_KV + kvh) * p.stride;
   float* out = p.out + ((int64_t)b * p.H_KV + kvh) * p.stride;
   const bool keep = p.decay != 0.f;
+  __shared__ __attribute__((aligned(16))) unsigned char stages[kWeightWaves][kKeysPerTile * kKPitch];
+  unsigned char* const stage = stages[wave];
   auto load = [&](u32x4 (&k)[2][4], float& old, int t) {
     const int key = t * kKeysPerTile, j = div_by(key, p.div_page);
     const int page = __builtin_amdgcn_readlane(pages, (j - pg0) & 63);
@@ -103,10 +113,26 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(WeightParams
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        k[mt][i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (uint32_t)(16 * mt + col) * rs + 64u * i + 16u * quad, 0, 0);
+        k[mt][i] = __builtin_amdgcn_raw_buffer_load_b128(kr, (uint32_t)(16 * mt + 4 * i + quad) * rs + 16u * col, 0, AUX);
     old = keep && lane < rows ? in[key + lane] : 0.f;
   };
-  auto reduce = [&](const u32x4 (&k)[2][4], float old, int t) {
+  // rows of the tile to LDS, and back as operands: lane (col, quad) of (mt, i) holds dims [32 i + 8 quad, + 8) of key 16 mt + col
+  auto put = [&](const u32x4 (&k)[2][4]) {
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<u32x4*>(stage + (16 * mt + 4 * i + quad) * kKPitch + 16 * col) = k[mt][i];
+    __builtin_amdgcn_wave_barrier();
+  };
+  auto reduce = [&](float old, int t) {
+    u32x4 k[2][4];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        k[mt][i] = *reinterpret_cast<const u32x4*>(stage + (16 * mt + col) * kKPitch + 16 * (4 * i + quad));
+    __builtin_amdgcn_wave_barrier();
     float sum[2] = {0.f, 0.f};
     for (int h0 = 0; h0 < p.g; h0 += 16 * NT) {
       if (NT == 4 && p.g > 64) load_heads(h0);
@@ -134,24 +160,21 @@ __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(WeightParams
   float old;
   load(k, old, t);
   for (; t + kWeightWaves < end; t += kWeightWaves) {
-    u32x4 next[2][4];
-    float next_old;
-    load(next, next_old, t + kWeightWaves);
-    reduce(k, old, t);
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) k[mt][i] = next[mt][i];
-    old = next_old;
+    put(k);
+    const float was = old;
+    load(k, old, t + kWeightWaves);
+    reduce(was, t);
   }
-  reduce(k, old, t);
+  put(k);
+  reduce(old, t);
 }
 
 // ---------------------------------------------------------------- eviction
 
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWaves = kSelectThreads / 64;
-constexpr int kBins = 2048;
+constexpr int kBins = 4096;       // of the second and third digit; of the first 256, in kCopies
+constexpr int kCopies = 16;
+constexpr int kListed = kBins / 2;  // moves whose rows are listed in LDS, in the histogram's place
+constexpr int kMostKeys = 32768;    // keys that stay in LDS
 constexpr int kMoveRows = 64;  // rows a workgroup of move_kernel takes at a time
 
 struct EvictParams {
@@ -186,38 +209,57 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return w != w ? 0u : (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Sums of x and y over the threads before this one.  Two barriers; `sums` is
-// free for the next call after them.
-__device__ __forceinline__ int2 scan_before(int x, int y, int2* sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Sum over lanes 0 to 15's values before lane `n` (n <= 16, uniform).
+__device__ __forceinline__ int row_sum_before(int x, int n) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  const int upto = __builtin_amdgcn_readlane(x, (n + 15) & 15);
+  return n > 0 ? upto : 0;
+}
+
+// Sums of x and y over the threads before this one; *total: over all.  One
+// barrier: `sums` is this call's own.
+template <int WAVES>
+__device__ __forceinline__ int2 scan_before(int x, int y, int2* sums, int2* total) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int sx = wave_scan(x), sy = wave_scan(y);
   if (lane == 63) sums[wave] = make_int2(sx, sy);
   __syncthreads();
-  int2 before = make_int2(sx - x, sy - y);
-  for (int w = 0; w < wave; ++w) {
-    before.x += sums[w].x;
-    before.y += sums[w].y;
-  }
-  __syncthreads();
-  return before;
+  const int2 s = lane < WAVES ? sums[lane] : make_int2(0, 0);
+  *total = make_int2(row_sum_before(s.x, 16), row_sum_before(s.y, 16));
+  return make_int2(sx - x + row_sum_before(s.x, wave), sy - y + row_sum_before(s.y, wave));
 }
 
 // The rows of one (sequence, KV head) that stay.  With more than `budget` rows,
 // those of the `budget` largest keys do, where a key is the row's weight (all
 // ones for a protected row), of equal ones the lowest rows.  The budget-th
-// largest key comes from three histograms in LDS of 11, 11 and 10 bits: each
+// largest key comes from three histograms in LDS of 8, 12 and 12 bits: each
 // fixes the bits of its digit and the number still to be found among the keys
-// that share them.  A thread holds consecutive rows, so one scan over the
-// threads ranks the equal keys, and another the evicted rows below the budget
+// that share them.  Weights agree in their first bits, and additions to one
+// address go one after the other, so the first histogram has a copy for each of
+// 16 lanes.  A thread then ranks `each` consecutive rows: one scan over the
+// threads numbers the equal keys, and another the evicted rows below the budget
 // (holes) and the kept ones above it: the i-th of these moves into the i-th
-// hole, in place and without an order among the moves.  EACH rows of a thread
-// stay in registers, or (0) are read anew for each step.
-template <int EACH>
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(EvictParams p) {
-  __shared__ uint32_t hist[kBins];
-  __shared__ int2 sums[kSelectWaves];
-  __shared__ uint32_t found[2];
-  const int tid = threadIdx.x;
+// hole, in place and without an order among the moves.
+//
+// Bound by latency: one pass over weights and positions, coalesced, whose keys
+// stay in LDS (KEEP; longer sequences read both anew for each step), about ten
+// barriers, two lookups a move (32 sequences of 8 heads one key past 4096: 12.1
+// us; with the rows in registers, loaded and stored `each` apart, and one copy of
+// the first histogram 18.0, a third of it for the stores; eight of 16000 rows
+// 36.6, a third for that histogram).
+template <int THREADS, bool KEEP>
+__global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
+  constexpr int WAVES = THREADS / 64;
+  static_assert(WAVES <= 16 && THREADS >= 256, "the waves' sums are scanned by 16 lanes; 256 threads have a first digit each");
+  extern __shared__ uint32_t keys[];  // KEEP: [L_K]
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
+  __shared__ int2 sums[5][WAVES];
+  __shared__ uint32_t found[3][2];
+  __shared__ int ties;  // not all keys equal to the last that stays do
+  const int tid = threadIdx.x, lane = tid & 63;
   const int unit = blockIdx.x, b = div_by(unit, p.div_heads);
   const int L = max(0, min(p.seq_lens[b], p.L_K)), total = p.totals[b];
   const float* w_in = p.w_in + unit * p.stride;
@@ -228,116 +270,171 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(EvictParams p) {
   if (L <= p.budget) {
     if (tid == 0) moves[0] = 0;
     if (w_in != w_out)
-      for (int r = tid; r < L; r += kSelectThreads) w_out[r] = w_in[r];
+      for (int r = tid; r < L; r += THREADS) w_out[r] = w_in[r];
     if (p_in != p_out)
-      for (int r = tid; r < L; r += kSelectThreads) p_out[r] = p_in[r];
+      for (int r = tid; r < L; r += THREADS) p_out[r] = p_in[r];
     return;
   }
-  const int each = (L + kSelectThreads - 1) / kSelectThreads;
-  const int r0 = min((int64_t)tid * each, (int64_t)L), r1 = min((int64_t)r0 + each, (int64_t)L);
   const int shift = (int)((uint32_t)total - (uint32_t)L);  // position of a row that no eviction has placed: row + shift
-  auto position = [&](int r) {
-    const int at = p_in[r];
-    return at >= 0 ? at : (int)((uint32_t)r + (uint32_t)shift);
+  auto placed = [&](int r, int at) { return at >= 0 ? at : (int)((uint32_t)r + (uint32_t)shift); };
+  const int64_t newest = (int64_t)total - p.recent;
+  auto key_of = [&](int at, float w) { return at < p.sinks || (int64_t)at >= newest ? 0xffffffffu : order_of(w); };
+  auto key = [&](int r) {
+    if constexpr (KEEP)
+      return keys[r];
+    else
+      return key_of(placed(r, p_in[r]), w_in[r]);
   };
-  auto read_key = [&](int r) {
-    const int at = position(r);
-    return at < p.sinks || (int64_t)at >= (int64_t)total - p.recent ? 0xffffffffu : order_of(w_in[r]);
-  };
-  uint32_t held[EACH > 0 ? EACH : 1];
-  if constexpr (EACH > 0) {
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) held[e] = r0 + e < r1 ? read_key(r0 + e) : 0u;
-  }
-  // f(row, key) for the thread's rows in order
-  auto rows = [&](auto f) {
-    if constexpr (EACH > 0) {
-#pragma unroll
-      for (int e = 0; e < EACH; ++e)
-        if (r0 + e < r1) f(r0 + e, held[e]);
-    } else {
-      for (int r = r0; r < r1; ++r) f(r, read_key(r));
-    }
-  };
+  for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
+  __syncthreads();
 
   uint32_t prefix = 0, mask = 0;
   uint32_t want = (uint32_t)p.budget;  // of the keys that share the prefix, the want-th largest is the last to stay
+  int2 all;
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
-    const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const uint32_t bits = pass == 2 ? 1023u : 2047u;
-    hist[tid] = 0;
-    hist[tid + kSelectThreads] = 0;
-    __syncthreads();
-    rows([&](int, uint32_t key) {
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> low) & bits], 1u);
-    });
-    __syncthreads();
-    // from the largest digit down: thread t has 2047 - 2t and the one below it
-    const uint32_t a = hist[kBins - 1 - 2 * tid], c = hist[kBins - 2 - 2 * tid];
-    const uint32_t before = (uint32_t)scan_before((int)(a + c), 0, sums).x;
-    if (before < want && want <= before + a + c) {
-      const bool upper = want <= before + a;
-      found[0] = (uint32_t)(kBins - 1 - 2 * tid - (upper ? 0 : 1));
-      found[1] = want - before - (upper ? 0u : a);
+    const int low = pass == 0 ? 24 : pass == 1 ? 12 : 0;
+    if (pass == 0) {
+      // rows below the budget are written as if they stayed; what moves into the others follows
+      for (int r8 = tid; r8 < L; r8 += 8 * THREADS) {
+        float w[8];
+        int at[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = min(r8 + i * THREADS, L - 1);
+          w[i] = w_in[r];
+          at[i] = p_in[r];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = r8 + i * THREADS;
+          if (r >= L) break;
+          const int pos = placed(r, at[i]);
+          const uint32_t k = key_of(pos, w[i]);
+          if constexpr (KEEP) keys[r] = k;
+          atomicAdd(&hist[(k >> 24) * kCopies + (lane & (kCopies - 1))], 1u);
+          if (r < p.budget) {
+            if (w_in != w_out) w_out[r] = w[i];
+            if (at[i] < 0 || p_in != p_out) p_out[r] = pos;
+          }
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int r = tid; r < L; r += THREADS) {
+        const uint32_t k = key(r);
+        if ((k & mask) == prefix) atomicAdd(&hist[(k >> low) & (kBins - 1)], 1u);
+      }
     }
     __syncthreads();
-    prefix |= found[0] << low;
-    mask |= bits << low;
-    want = found[1];
+    // from the largest digit down: the first digit one a thread, the others kBins / THREADS
+    constexpr int PER = kBins / THREADS;
+    uint32_t c[PER], sum = 0;
+    if (pass == 0) {
+      if (tid < 256)
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+          const int at = (255 - tid) * kCopies + ((tid + i) & (kCopies - 1));
+          sum += hist[at];
+          hist[at] = 0;
+        }
+    } else {
+      u32x4* const mine = reinterpret_cast<u32x4*>(hist + kBins - PER * (tid + 1));
+#pragma unroll
+      for (int i = 0; i < PER / 4; ++i) {
+        const u32x4 x = mine[PER / 4 - 1 - i];
+        mine[PER / 4 - 1 - i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          c[4 * i + e] = x[3 - e];
+          sum += x[3 - e];
+        }
+      }
+    }
+    uint32_t before = (uint32_t)scan_before<WAVES>((int)sum, 0, sums[pass], &all).x;
+    if (before < want && want <= before + sum) {
+      int digit = 255 - tid;
+      if (pass > 0) {
+        digit = kBins - 1 - PER * tid;
+        sum = c[0];
+#pragma unroll
+        for (int i = 0; i < PER - 1; ++i)
+          if (kBins - 1 - PER * tid - i == digit && want > before + c[i]) {
+            before += c[i];
+            sum = c[i + 1];
+            --digit;
+          }
+      }
+      found[pass][0] = (uint32_t)digit;
+      found[pass][1] = want - before;
+      if (pass == 2) ties = sum != want - before;
+    }
+    __syncthreads();
+    prefix |= found[pass][0] << low;
+    mask |= (pass == 0 ? 255u : kBins - 1u) << low;
+    want = found[pass][1];
   }
 
-  int equal = 0;
-  rows([&](int, uint32_t key) { equal += key == prefix; });
-  int rank = scan_before(equal, 0, sums).x;
-  const int rank0 = rank;
-  int holes = 0, late = 0;
-  rows([&](int r, uint32_t key) {
-    const bool stays = key > prefix || (key == prefix && rank < (int)want);
-    rank += key == prefix;
+  // the thread's rows: an odd number of them, so that the threads' keys lie in different banks
+  const int each = ((L + THREADS - 1) / THREADS) | 1;
+  const int r0 = (int)min((int64_t)tid * each, (int64_t)L), r1 = (int)min((int64_t)r0 + each, (int64_t)L);
+  int rank0 = 0;
+  if (ties) {
+    int equal = 0;
+#pragma unroll 4
+    for (int r = r0; r < r1; ++r) equal += key(r) == prefix;
+    rank0 = scan_before<WAVES>(equal, 0, sums[3], &all).x;
+  } else {
+    want = (uint32_t)L;  // a thread's rows are fewer
+  }
+  int rank = rank0, holes = 0, late = 0;
+#pragma unroll 4
+  for (int r = r0; r < r1; ++r) {
+    const uint32_t k = key(r);
+    const bool stays = k > prefix || (k == prefix && rank < (int)want);
+    rank += k == prefix;
     holes += !stays && r < p.budget;
     late += stays && r >= p.budget;
-  });
-  const int2 at = scan_before(holes, late, sums);
-  if (tid == kSelectThreads - 1) found[0] = (uint32_t)min(at.x + holes, p.most);
-  // a thread's rows and places of its row in the pool; the lists hold rows first
-  int32_t* to = moves + 1;
-  int32_t* from = moves + 1 + p.most;
-  rank = rank0;
-  int hole = at.x, mover = at.y;
-  rows([&](int r, uint32_t key) {
-    const bool stays = key > prefix || (key == prefix && rank < (int)want);
-    rank += key == prefix;
-    if (r < p.budget) {
-      if (!stays) {
-        if (hole < p.most) to[hole] = r;
+  }
+  const int2 first = scan_before<WAVES>(holes, late, sums[4], &all);
+  const int count = min(all.x, p.most);
+  // rows that move, listed within the sequence first
+  const bool in_lds = count <= kListed;
+  int32_t* to = in_lds ? reinterpret_cast<int32_t*>(hist) : moves + 1;
+  int32_t* from = in_lds ? to + kListed : moves + 1 + p.most;
+  if (holes + late > 0) {
+    rank = rank0;
+    int hole = first.x, mover = first.y;
+    for (int r = r0; r < r1; ++r) {
+      const uint32_t k = key(r);
+      const bool stays = k > prefix || (k == prefix && rank < (int)want);
+      rank += k == prefix;
+      if (r < p.budget && !stays) {
+        if (hole < count) to[hole] = r;
         ++hole;
-      } else {
-        if (w_in != w_out) w_out[r] = w_in[r];
-        p_out[r] = position(r);
       }
-    } else if (stays) {
-      if (mover < p.most) from[mover] = r;
-      ++mover;
+      if (r >= p.budget && stays) {
+        if (mover < count) from[mover] = r;
+        ++mover;
+      }
     }
-  });
+  }
   __syncthreads();
-  const int count = (int)found[0];
   if (tid == 0) moves[0] = count;
   auto pool_row = [&](int r) {
     const int j = div_by(r, p.div_page);
     const int page = p.block_table[(int64_t)b * p.max_pages + j];
     return page >= 0 && page < p.num_pages ? page * p.page_size + (r - j * p.page_size) : -1;
   };
-  for (int i = tid; i < count; i += kSelectThreads) {
+  for (int i = tid; i < count; i += THREADS) {
     const int d = to[i], s = from[i];
     w_out[d] = w_in[s];
-    p_out[d] = position(s);
-    to[i] = pool_row(d);
-    from[i] = pool_row(s);
+    p_out[d] = placed(s, p_in[s]);
+    moves[1 + i] = pool_row(d);
+    moves[1 + p.most + i] = pool_row(s);
   }
   __syncthreads();
-  for (int r = p.budget + tid; r < L; r += kSelectThreads) {
+  for (int r = p.budget + tid; r < L; r += THREADS) {
     w_out[r] = 0.f;
     p_out[r] = -1;
   }
@@ -491,22 +588,31 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
   p.num_pages = num_pages;
   p.div_page = make_div((uint32_t)page_size);
   p.div_heads = make_div((uint32_t)H_KV);
-  // four workgroups a CU, of one tile a wave at least
+  // sixteen workgroups a CU, of one tile a wave at least: they start as others end, so lengths even out
   const int64_t tiles = (L_K_max + kKeysPerTile - 1) / kKeysPerTile, units = (int64_t)B * H_KV;
-  int64_t each = (tiles * units + 4 * cus - 1) / (4 * cus);
+  int64_t each = (tiles * units + 16 * cus - 1) / (16 * cus);
   each = std::min<int64_t>(std::max<int64_t>(4, (each + 3) / 4 * 4), kMostChunkTiles);
   p.chunk_tiles = (int)each;
-  p.chunks = (int)((tiles + each - 1) / each);
-  p.div_chunks = make_div((uint32_t)p.chunks);
-  if (units * p.chunks >= ((int64_t)1 << 31))
+  const int64_t chunks = (tiles + each - 1) / each;
+  p.chunks = (int)chunks;
+  p.div_chunks = make_div((uint32_t)chunks);
+  if (units * chunks >= ((int64_t)1 << 31))
     return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many workgroups", B, H_KV, L_K_max);
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * kLog2e;
   p.decay = decay;
-  const void* fn = p.g <= 16   ? reinterpret_cast<const void*>(&weights_kernel<1>)
-                   : p.g <= 32 ? reinterpret_cast<const void*>(&weights_kernel<2>)
-                               : reinterpret_cast<const void*>(&weights_kernel<4>);
+  // keys that the caches cannot hold until the next call take the streaming hint (552 MB of keys and weights 104 ->
+  // 91 us; 270 MB 40 -> 43, so not below)
+  const int64_t keys = std::min((int64_t)num_pages * page_size, (int64_t)B * L_K_max);
+  const bool stream_hint = (uint64_t)keys * H_KV * D * 2 > DA_RESIDENT_BYTES;
+  auto pick = [&](auto hint) {
+    constexpr int AUX = decltype(hint)::value;
+    return p.g <= 16   ? reinterpret_cast<const void*>(&weights_kernel<1, AUX>)
+           : p.g <= 32 ? reinterpret_cast<const void*>(&weights_kernel<2, AUX>)
+                       : reinterpret_cast<const void*>(&weights_kernel<4, AUX>);
+  };
+  const void* fn = stream_hint ? pick(std::integral_constant<int, 2>{}) : pick(std::integral_constant<int, 0>{});
   void* args[] = {&p};
-  return launched(hipLaunchKernel(fn, dim3((uint32_t)(units * p.chunks)), dim3(64 * kWeightWaves), args, 0,
+  return launched(hipLaunchKernel(fn, dim3((uint32_t)(units * chunks)), dim3(64 * kWeightWaves), args, 0,
                                   static_cast<hipStream_t>(stream)),
                   "key weight");
 }
@@ -589,12 +695,14 @@ int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const 
   p.num_free = num_free;
   const int64_t units = (int64_t)B * H_KV;
   void* args[] = {&p};
-  const void* fn = L_K_max <= 4 * kSelectThreads    ? reinterpret_cast<const void*>(&select_kernel<4>)
-                   : L_K_max <= 8 * kSelectThreads  ? reinterpret_cast<const void*>(&select_kernel<8>)
-                   : L_K_max <= 16 * kSelectThreads ? reinterpret_cast<const void*>(&select_kernel<16>)
-                                                    : reinterpret_cast<const void*>(&select_kernel<0>);
+  const int threads = L_K_max <= 512 ? 256 : L_K_max <= 1024 ? 512 : 1024;
+  const void* fn = threads == 256         ? reinterpret_cast<const void*>(&select_kernel<256, true>)
+                   : threads == 512       ? reinterpret_cast<const void*>(&select_kernel<512, true>)
+                   : L_K_max <= kMostKeys ? reinterpret_cast<const void*>(&select_kernel<1024, true>)
+                                          : reinterpret_cast<const void*>(&select_kernel<1024, false>);
+  const int smem = L_K_max <= kMostKeys ? 4 * L_K_max : 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  rc = launched(hipLaunchKernel(fn, dim3((uint32_t)units), dim3(kSelectThreads), args, 0, s), "select");
+  rc = launched(hipLaunchKernel(fn, dim3((uint32_t)units), dim3(threads), args, smem, s), "select");
   if (rc) return rc;
   // eight workgroups a CU at most; a workgroup that finds nothing to move ends at once
   const int64_t parts = (p.most + kMoveRows - 1) / kMoveRows;
