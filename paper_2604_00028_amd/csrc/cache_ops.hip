@@ -225,6 +225,7 @@ struct AppendParams {
   int rope_rows, rope_dim, neighbours;
   const int32_t* positions;              // [num_axes, N]
   int num_axes;
+  int by_four;                           // pairs 4 i to 4 i + 3 have one axis
   uint32_t axes[4];                      // axis of pair i: bits 2 (i mod 16) of word i / 16
   const int32_t* slots;
   uint16_t* q_out;
@@ -278,10 +279,10 @@ __device__ __forceinline__ float bf16_high(uint32_t two) { return __uint_as_floa
 // token a wave: 3001 tokens of 8 heads 7 us, where their 16 MB would take 3.
 //
 // AXES: pair i of the rotation turns by the token's position on axis a(i) of up
-// to four, so its coefficients come from row positions[a(i)] of the table.  A
-// lane reads its eight dims' cosines and sines of every axis that one of its
-// pairs has (the others are out of the range of its loads and cost nothing) and
-// picks by pair.
+// to four, so its coefficients come from row positions[a(i)] of the table: four
+// pairs a load where four have one axis each (8192 tokens with three axes 65 us, as with one;
+// a wide load for each axis and a choice by pair, which takes 20 more registers,
+// 79), else one by one.
 template <bool KV4, int STREAM, bool AXES>
 __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams p) {
   const int lane = threadIdx.x & 63;
@@ -309,39 +310,53 @@ __global__ void __launch_bounds__(64 * kAppendWaves) append_kernel(AppendParams 
     const uint32_t mine =
         (word == 0 ? p.axes[0] : word == 1 ? p.axes[1] : word == 2 ? p.axes[2] : p.axes[3]) >> (2 * (pair0 & 15));
     const int pairs = p.neighbours ? 4 : 8;
-    f32x4 cc[kMaxAxes][2], ss[kMaxAxes][2];
-#pragma unroll
-    for (int a = 0; a < kMaxAxes; ++a) {
-      if (a >= p.num_axes) break;  // uniform
-      const int pos = __builtin_amdgcn_readfirstlane(p.positions[(int64_t)a * p.N + n]);
-      const bool in = pos >= 0 && pos < p.rope_rows;  // a position outside the table: zeros
-      const __amdgpu_buffer_rsrc_t rr =
-          make_rsrc(p.rope + (int64_t)(in ? pos : 0) * p.rope_dim, in ? (uint32_t)p.rope_dim * 4u : 0u);
-      bool has = false;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) has |= e < pairs && ((mine >> (2 * e)) & 3u) == (uint32_t)a;
-      const uint32_t at = has && l < lanes ? 4u * (uint32_t)pair0 : 0x80000000u;
+    // the token's positions: one load for all axes, then the lane's pairs' rows of the table
+    const int at = p.positions[(int64_t)min(lane & 3, p.num_axes - 1) * p.N + n];
+    const int pos[kMaxAxes] = {__builtin_amdgcn_readlane(at, 0), __builtin_amdgcn_readlane(at, 1),
+                               __builtin_amdgcn_readlane(at, 2), __builtin_amdgcn_readlane(at, 3)};
+    auto row_of = [&](int i, bool& in) {  // of the lane's pair i; outside the table: row 0, and zeros in the end
+      const uint32_t a = (mine >> (2 * i)) & 3u;
+      const int r = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
+      in = r >= 0 && r < p.rope_rows;
+      return p.rope + (int64_t)(in ? r : 0) * p.rope_dim + pair0 + i;
+    };
+    auto set = [&](int i, float cosine, float sine) {
+      if (p.neighbours) {
+        if (i >= 4) return;
+        c[2 * i] = c[2 * i + 1] = cosine;
+        s[2 * i] = -sine;
+        s[2 * i + 1] = sine;
+      } else {
+        c[i] = cosine;
+        s[i] = second ? sine : -sine;
+      }
+    };
+    if (l < lanes && p.by_four) {
+      f32x4 cosine[2], sine[2];
+      bool in[2] = {false, false};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        // four pairs a lane need the first halves only
-        const uint32_t from = i == 0 || !p.neighbours ? at + 16u * i : 0x80000000u;
-        cc[a][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, from, 0, 0));
-        ss[a][i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, from + 2u * p.rope_dim, 0, 0));
+        if (i == 1 && p.neighbours) break;
+        const float* row = row_of(4 * i, in[i]);
+        cosine[i] = *reinterpret_cast<const f32x4*>(row);
+        sine[i] = *reinterpret_cast<const f32x4*>(row + p.rope_dim / 2);
       }
-    }
-    if (l < lanes) {
 #pragma unroll
-      for (int a = 0; a < kMaxAxes; ++a) {
-        if (a >= p.num_axes) break;
+      for (int i = 0; i < 8; ++i)
+        if (i < pairs) set(i, in[i / 4] ? cosine[i / 4][i % 4] : 0.f, in[i / 4] ? sine[i / 4][i % 4] : 0.f);
+    } else if (l < lanes) {
+      float cosine[8], sine[8];
+      bool in[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int i = p.neighbours ? e / 2 : e;
-          if (((mine >> (2 * i)) & 3u) != (uint32_t)a) continue;
-          c[e] = p.neighbours ? cc[a][0][e / 2] : cc[a][e / 4][e % 4];
-          const float turn = p.neighbours ? ss[a][0][e / 2] : ss[a][e / 4][e % 4];
-          s[e] = (p.neighbours ? e % 2 == 0 : !second) ? -turn : turn;
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (i == 4 && p.neighbours) break;
+        const float* row = row_of(i, in[i]);
+        cosine[i] = row[0];
+        sine[i] = row[p.rope_dim / 2];
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < pairs) set(i, in[i] ? cosine[i] : 0.f, in[i] ? sine[i] : 0.f);
     }
   } else if (p.rope) {
     const int pos = __builtin_amdgcn_readfirstlane(p.positions[n]);
@@ -584,6 +599,8 @@ int append_axes(AppendParams& p, const uint8_t* axes, int num_axes) {
     p.axes[i / 16] |= (uint32_t)axes[i] << (2 * (i % 16));
   }
   p.num_axes = num_axes;
+  p.by_four = 1;
+  for (int i = 0; i < p.rope_dim / 2; ++i) p.by_four &= axes[i] == axes[i & ~3];
   return DA_OK;
 }
 
