@@ -166,10 +166,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     for (int b = lane; b < p.B; b += 64) work_b += min(tiles[b], 1 << 16);
     work_g = min(wave_total(work_g), (1 << 30) / p.H_KV) * p.H_KV;
     work_b = min(wave_total(work_b), (1 << 30) / (p.H_KV * own_tiles)) * (p.H_KV * own_tiles);
-    // About a unit a CU of shared keys (of 64 tiles at most: more are dealt as they run out), as many of a
-    // sequence's own by a workgroup each, or several for each wave where there are more.
+    // About a unit a CU of shared keys (128 tiles at most: more are dealt as they run out).  Shorter ones write more
+    // states, whose merge costs as much: 32 sequences over 8192 keys in 256 units of 16 tiles 38.8 us, in 512 of 8 47.8;
+    // 128 over 16384, with own parts, in units of 128 tiles 150 us, of 64 161 (without own parts 119 and 112).
+    // Half as many of a sequence's own keys by a workgroup each, or long ones for a wave each where there are many.
     waves = work_b >= 24 * p.slots;
-    length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 64);
+    length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 128);
     length_b = p.chunk_tiles > 0 ? p.chunk_tiles : waves ? 64 : min(max(work_b / (p.slots / 4), 4), 64);
     auto longer = [&](int length, int w) { return (int)min((int64_t)length << w, (int64_t)kWhole); };
     int w = 0;
@@ -703,18 +705,15 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     }
     bf16x8 kop[2][4];
     if constexpr (decltype(more)::value) read_k(kop, sn);
-    bool moved = false;
-    float top[NT];
+    // The maximum follows at once, so that a row's largest probability is exactly 1 (with a slack of 2^8 the products with
+    // the old state's weight were rarer and 128 sequences over 16384 keys 5% faster, but the error against 64 bits 2.2e-3
+    // and not 1.8e-3); 16 rows at a time, most tiles move none of them.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const f32x4 a = sc[nt][0], c = sc[nt][1];
-      top[nt] = p.scale_log2 * top_of_rows(max3(max3(a[0], a[1], a[2]), max3(a[3], c[0], c[1]), max3(c[2], c[3], c[3])));
-      moved |= top[nt] > red.m[nt];
-    }
-    if (__any(moved)) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float m = fmaxf(red.m[nt], top[nt]);
+      const float top = p.scale_log2 * top_of_rows(max3(max3(a[0], a[1], a[2]), max3(a[3], c[0], c[1]), max3(c[2], c[3], c[3])));
+      if (__any(top > red.m[nt])) {
+        const float m = fmaxf(red.m[nt], top);
         const float alpha = __builtin_amdgcn_exp2f(red.m[nt] - m);
         red.m[nt] = m;
         red.l[nt] *= alpha;
@@ -857,73 +856,28 @@ __global__ void __launch_bounds__(64 * kUnitWaves, 2) unit_kernel(PrefixParams p
   const bool by_wave = __builtin_amdgcn_readfirstlane(p.head[2]) != 0;
   const int need = by_wave ? (n_own + kOwnWaves - 1) / kOwnWaves : n_own;  // workgroups that the own units can use
   const int front = min(slots - min(slots / 2, need), n_group);
-  Next group{p.units, p.tickets + 64 * xcd, place, n_group, front, xcd, tid, lane, 0, 0, 0, 0};
   // workgroups [0, front) begin with the groups' units, the others with the sequences'
   const int own_given = (slots - front) * (by_wave ? kOwnWaves : 1);
-  Next own{p.units + p.most_units, p.tickets + 64 * xcd + 32, place, n_own, own_given, xcd, tid, lane, 0, 0, 0, 0};
-
-  auto run_group = [&](bool begin) {
-    if (begin) {
-      group.index = at;
-      group.word = begins;
-    } else {
-      if (group.given >= n_group) return;
-      group.skip();
-    }
-    while (group.index >= 0) {
-      const Unit u = unit_of(group.word);
-      const int rows = u.rows_kvh & 255;
-      // opaque, so that the addresses of all kinds are not kept (and spilled) from unit to unit
-      int ln = lane;
-      asm volatile("" : "+v"(ln));
-      if (rows == 0)  // fills a bundle
-        group.skip();
-      else if (rows <= 16)
-        stream_unit<1>(p, u, smem, ln, wave, group);
-      else if (rows <= 32)
-        stream_unit<2>(p, u, smem, ln, wave, group);
-      else if (rows <= 64)
-        shared_unit<1>(p, u, smem, ln, wave, group);
-      else
-        shared_unit<2>(p, u, smem, ln, wave, group);
-    }
-    __syncthreads();
-  };
-  auto run_own = [&](bool begin) {
-    if (!begin && own_given >= n_own) return;
-    if (!by_wave) {
-      if (begin) {
-        own.index = at - front;
-        if (own.index >= n_own) return;
-        own.load();
-      } else {
-        own.skip();
-      }
-      while (own.index >= 0) {
-        const Unit u = unit_of(own.word);
-        int ln = lane;
-        asm volatile("" : "+v"(ln));
-        if ((u.rows_kvh & 255) == 0)
-          own.skip();
-        else if ((u.rows_kvh & 255) <= 16)
-          stream_unit<1>(p, u, smem, ln, wave, own);
-        else
-          stream_unit<2>(p, u, smem, ln, wave, own);
-      }
-    } else {
+  // one body for both lists: the kernel is long, and what a CU has not run yet it fetches in the middle of its work
+#pragma nounroll
+  for (int turn = 0; turn < 2; ++turn) {
+    const bool of_group = (turn == 0) == (at < front);
+    Next list{of_group ? p.units : p.units + p.most_units, p.tickets + 64 * xcd + (of_group ? 0 : 32), place,
+              of_group ? n_group : n_own, of_group ? front : own_given, xcd, tid, lane, 0, -1, 0, 0};
+    if (!of_group && by_wave) {
       auto take = [&]() {
         uint32_t t = 0;
         if (own_given < n_own && lane == 0)
-          t = __hip_atomic_fetch_add(own.tickets, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          t = __hip_atomic_fetch_add(list.tickets, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         return t;
       };
       auto number = [&](uint32_t t) {
         const uint32_t i = (uint32_t)own_given + (uint32_t)__builtin_amdgcn_readfirstlane((int)t);
         return own_given < n_own && i < (uint32_t)n_own ? (int)i : n_own;
       };
-      int i = wave >= kOwnWaves ? n_own : begin ? (at - front) * kOwnWaves + wave : number(take());
+      int i = wave >= kOwnWaves ? n_own : turn == 0 ? (at - front) * kOwnWaves + wave : number(take());
       while (i < n_own) {
-        const Unit u = unit_of(reinterpret_cast<const int32_t*>(own.list + 8 * i + xcd)[lane & 7]);
+        const Unit u = unit_of(reinterpret_cast<const int32_t*>(list.list + 8 * i + xcd)[lane & 7]);
         const uint32_t t = take();
         int ln = lane;
         asm volatile("" : "+v"(ln));
@@ -935,15 +889,34 @@ __global__ void __launch_bounds__(64 * kUnitWaves, 2) unit_kernel(PrefixParams p
           wave_unit<2>(p, u, smem, ln, wave);
         i = number(t);
       }
+      __syncthreads();
+      continue;
+    }
+    if (turn == 0) {
+      list.index = of_group ? at : at - front < n_own ? at - front : -1;
+      list.word = begins;
+      if (!of_group) list.load();
+    } else if (list.given < list.n) {
+      list.skip();
+    }
+    while (list.index >= 0) {
+      const Unit u = unit_of(list.word);
+      const int rows = u.rows_kvh & 255;
+      // opaque, so that the addresses of all kinds are not kept (and spilled) from unit to unit
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      if (rows == 0)  // fills a bundle
+        list.skip();
+      else if (rows <= 16)
+        stream_unit<1>(p, u, smem, ln, wave, list);
+      else if (rows <= 32)
+        stream_unit<2>(p, u, smem, ln, wave, list);
+      else if (rows <= 64)
+        shared_unit<1>(p, u, smem, ln, wave, list);
+      else
+        shared_unit<2>(p, u, smem, ln, wave, list);
     }
     __syncthreads();
-  };
-  if (at < front) {
-    run_group(true);
-    run_own(false);
-  } else {
-    run_own(true);
-    run_group(false);
   }
 }
 
