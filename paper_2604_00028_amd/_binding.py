@@ -1143,6 +1143,7 @@ def da_decode_attn_kv4(q: torch.Tensor, cache: torch.Tensor, block_table: torch.
 
 
 # ---------------------------------------------------------------- a shared and bounded cache
+# (an empty tensor's data_ptr() is 0: NULL)
 
 
 def _paged_pool(name: str, cache: torch.Tensor, dev: torch.device) -> Tuple[int, int, int, int]:
@@ -1200,10 +1201,10 @@ def da_decode_attn_prefix(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
     L, chunk_keys = _int(int(L_K_max)), _int(int(chunk_keys))
     ws, capture = (_usable(workspace, dev), 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
-        rc = load().da_decode_attn_prefix(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
-                                          _ptr(cu_groups), _ptr(prefix_lens), _ptr(out), _ptr(lse_out), B, G, H_Q, H_KV,
-                                          _int(page_size), max_pages, _int(num_pages), L, d, softmax_scale, chunk_keys,
-                                          _ptr(ws), _nbytes(ws), s_handle)
+        rc = load().da_decode_attn_prefix(
+            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+            cu_groups.data_ptr(), prefix_lens.data_ptr(), out.data_ptr(), _ptr(lse_out), B, G, H_Q, H_KV, _int(page_size),
+            max_pages, _int(num_pages), L, d, softmax_scale, chunk_keys, _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
         workspace = ws = _grown(dev, s_handle, capture, da_prefix_workspace_bytes(B, G, H_Q, H_KV))
@@ -1240,10 +1241,10 @@ def da_add_key_weights(q: torch.Tensor, k_cache: torch.Tensor, block_table: torc
     if dev.index != _get_device():
         return _on_device(dev, da_add_key_weights, q, k_cache, block_table, seq_lens, lse, weights, L_K_max, decay,
                           weights_out, softmax_scale=softmax_scale, stream=stream)
-    rc = load().da_add_key_weights(_ptr(q), _ptr(k_cache), _ptr(block_table), _ptr(seq_lens), _ptr(lse),
-                                   weights.data_ptr() or None, weights_out.data_ptr() or None, stride, B, H_Q, H_KV,
-                                   _int(page_size), max_pages, _int(num_pages), _int(int(L_K_max)), d, softmax_scale,
-                                   decay, _stream(dev, stream))
+    rc = load().da_add_key_weights(
+        q.data_ptr(), k_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), lse.data_ptr(), weights.data_ptr(),
+        weights_out.data_ptr(), stride, B, H_Q, H_KV, _int(page_size), max_pages, _int(num_pages), _int(int(L_K_max)), d,
+        softmax_scale, decay, _stream(dev, stream))
     if rc:
         _check(rc)
     return weights_out
@@ -1305,11 +1306,11 @@ def da_evict_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch
     s_handle = _stream(dev, stream)
     ws, capture = (_usable(workspace, dev), 0) if workspace is not None else _offered_now(dev, stream, s_handle)
     while True:
-        rc = load().da_evict_kv(_ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens), _ptr(totals),
-                                _ptr(weights), _ptr(positions), _ptr(outs[1]), _ptr(outs[2]), shape[2], _ptr(outs[0]),
-                                _ptr(free_pages), _ptr(taken), _ptr(outs[3]), num_free, B, H_KV, _int(page_size),
-                                max_pages, _int(num_pages), L, d, budget, _int(int(sinks)), _int(int(recent)), _ptr(ws),
-                                _nbytes(ws), s_handle)
+        rc = load().da_evict_kv(
+            k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), totals.data_ptr(),
+            weights.data_ptr(), positions.data_ptr(), outs[1].data_ptr(), outs[2].data_ptr(), shape[2], outs[0].data_ptr(),
+            _ptr(free_pages), _ptr(taken), _ptr(outs[3]), num_free, B, H_KV, _int(page_size), max_pages, _int(num_pages),
+            L, d, budget, _int(int(sinks)), _int(int(recent)), _ptr(ws), _nbytes(ws), s_handle)
         if rc != DA_ERR_WORKSPACE or workspace is not None:
             break
         workspace = ws = _grown(dev, s_handle, capture, da_evict_workspace_bytes(B, H_KV, L, budget))
