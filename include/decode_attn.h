@@ -693,15 +693,18 @@ size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t poo
  *                the group's first sequence that has keys, up to the last whole
  *                32 keys that all of its sequences with keys have; what follows,
  *                through each sequence's own
- *   chunk_keys   <= 0: the length of chunks that the work is cut into is chosen on
- *                the device by the batch's lengths and groups; else that many
- *                keys, in whole tiles of 32 (at most 64 chunks of a prefix or of
- *                a sequence's own keys, and longer ones where the workspace
- *                holds no more)
- *   workspace    >= da_prefix_workspace_bytes(B, G, H_Q, H_KV, 0); its last
- *                DA_ARRIVAL_BYTES are not touched, so the other calls' may be
- *                shared
- * Three launches; replays of a captured call follow the lengths and groups the
+ *   chunk_keys   0: chosen.  A batch that holds few keys (B L_K_max of at most 384
+ *                MiB of K and V, 768 for more than 16 heads a KV head) is not worth
+ *                sharing: it takes the launch of da_decode_attn_window with nothing
+ *                hidden.  Others are cut into chunks of lengths chosen on the device
+ *                by the batch's lengths and groups.  Negative: the latter whatever
+ *                the size.  Positive: chunks of that many keys, in whole tiles of 32
+ *                (at most 64 chunks of a prefix or of a sequence's own keys, and
+ *                longer ones where the workspace holds no more)
+ *   workspace    >= da_prefix_workspace_bytes(B, G, H_Q, H_KV, 0), counters in its
+ *                last DA_ARRIVAL_BYTES zero before the first call, as for
+ *                da_decode_attn
+ * One launch or three; replays of a captured call follow the lengths and groups the
  * device then holds.  Results are bit-identical across runs for the same
  * arguments, lengths and groups of the whole batch.  Probabilities are rounded to
  * bf16 for the product with V, as in da_decode_attn; lse takes them in 32 bits.

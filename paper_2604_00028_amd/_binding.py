@@ -1177,7 +1177,8 @@ def da_decode_attn_prefix(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
     the same keys, which are read once a group; returns `out`.  Group i is the
     sequences [cu_groups[i], cu_groups[i + 1]), whose first prefix_lens[i] keys are
     the same; block_table and seq_lens hold whole sequences, as for
-    da_decode_attn_paged."""
+    da_decode_attn_paged.  A batch too small to gain by it is read as it is, unless
+    chunk_keys is given (negative: chunks of a chosen length)."""
     dev = q.device
     if q.dim() != 3 or q.dtype is not _BF16 or not q.is_contiguous() or not q.is_cuda:
         raise ValueError("q must be a contiguous bfloat16 CUDA tensor [B, H_Q, d]")

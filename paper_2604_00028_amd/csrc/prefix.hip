@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* tiles = lds;            // [B] keys, then tiles of the sequence's own keys
   int32_t* group = tiles + p.B;    // [B] its group, or -1
-  int32_t* unit_b = group + p.B;   // [B] its first unit
+  int32_t* unit_b = group + p.B;   // [B] its first chunk, counted over the batch
   int32_t* state_b = unit_b + p.B; // [B] its first state row / H_Q
   int32_t* cu = state_b + p.B;     // [G + 1]
   int32_t* shared = cu + p.G + 1;  // [G] shared keys, then tiles
@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
   auto row_tiles = [&](int i) { return ((cu[i + 1] - cu[i]) * p.g + kSharedRows - 1) / kSharedRows; };
   // units of `streams` streams of keys that `readers` units each read
   auto units_of = [&](int streams, int readers) { return readers == 1 ? streams : (streams + 7) / 8 * 8 * readers; };
+  const int own_readers = p.H_KV * own_tiles;  // units that read a sequence's chunk, together whole rows of it
   // Lengths by the work there is.  Wave w tries them 2^w times as long; the first that fit the workspace are taken.
   int length_g, length_b;
   bool waves;  // a sequence's own chunks are a wave's work each, not a workgroup's
@@ -172,24 +173,22 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     // Half as many of a sequence's own keys by a workgroup each, or long ones for a wave each where there are many.
     waves = work_b >= 24 * p.slots;
     length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 128);
-    length_b = p.chunk_tiles > 0 ? p.chunk_tiles : waves ? 64 : min(max(work_b / (p.slots / 4), 4), 64);
+    length_b = p.chunk_tiles > 0 ? p.chunk_tiles : waves ? min(max(work_b / (3 * p.slots / 2), 8), 64) : min(max(work_b / (p.slots / 4), 4), 64);
     auto longer = [&](int length, int w) { return (int)min((int64_t)length << w, (int64_t)kWhole); };
     int w = 0;
     for (;; w += kPlanWaves) {
       const int lg = longer(length_g, w + wave), lb = longer(length_b, w + wave);
-      int units = 0, rows = 0;
+      int units = 0, rows = 0, chunks = 0;
       for (int i = lane; i < G; i += 64) {
         const int n = chunks_of(shared[i], lg);
         units += units_of(n * p.H_KV, row_tiles(i));
         rows += n * (cu[i + 1] - cu[i]);
       }
-      for (int b = lane; b < p.B; b += 64) {
-        const int n = chunks_of(tiles[b], lb);
-        units += units_of(n * p.H_KV, own_tiles);
-        rows += n;
-      }
+      for (int b = lane; b < p.B; b += 64) chunks += chunks_of(tiles[b], lb);
+      rows += chunks;
       const int u = wave_total(min(units, 1 << 24)), r = wave_total(min(rows, 1 << 24));
-      const bool fits = u + 14 <= p.most_units && (int64_t)r * p.H_Q <= p.most_rows;
+      const int64_t own_units = (int64_t)((wave_total(chunks) + 7) / 8 * 8) * own_readers;
+      const bool fits = u + 7 <= p.most_units && own_units <= p.most_units && (int64_t)r * p.H_Q <= p.most_rows;
       if (lane == 0) price[wave] = fits;
       __syncthreads();
       int k = 0;
@@ -221,7 +220,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     const int n = chunks_of(tiles[b], length_b);
     unit_b[b] = mine.z;
     state_b[b] = mine.w;
-    mine.z += units_of(n * p.H_KV, own_tiles);
+    mine.z += n;
     mine.w += state_chunks(b, n);
   }
   int4 upto = make_int4(wave_scan(mine.x), wave_scan(mine.y), wave_scan(mine.z), wave_scan(mine.w));
@@ -253,8 +252,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     s.own = n > 0 && state_chunks(b, n) == 0 ? -1 : n;
     p.seqs[b] = s;
   }
-  // two lists, each in whole eights: the groups' units, then the sequences'
-  const int padded = (all.x + 7) / 8 * 8, total = padded + (all.z + 7) / 8 * 8;
+  // two lists, each in whole eights: the groups' units, then the sequences', whose chunks are dealt to the XCDs and
+  // read there by all heads one behind the other
+  const int padded = (all.x + 7) / 8 * 8, total = padded + (all.z + 7) / 8 * 8 * own_readers;
   Unit* const own_units = p.units + p.most_units;
   if (tid == 0) {
     p.head[0] = padded;
@@ -265,27 +265,42 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     Unit u{};
     const bool of_group = i < padded;
     const int w = of_group ? i : i - padded;
-    if (w < (of_group ? all.x : all.z)) {
+    // where the unit stands: of the groups' by itself, of the sequences' its chunk's number and which of its readers it is
+    int number = w, own_reader = 0;
+    if (!of_group) {
+      const uint32_t bundle = (uint32_t)w / (uint32_t)(8 * own_readers), in = (uint32_t)w - bundle * 8 * own_readers;
+      own_reader = (int)(in / 8);
+      number = (int)(bundle * 8 + in % 8);
+    }
+    if (number < (of_group ? all.x : all.z)) {
       const int32_t* starts = of_group ? unit_g : unit_b;
-      int lo = 0, hi = of_group ? G : p.B;  // the last that starts at or before w
+      int lo = 0, hi = of_group ? G : p.B;  // the last that starts at or before it
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (starts[mid] <= w)
+        if (starts[mid] <= number)
           lo = mid;
         else
           hi = mid;
       }
-      const uint32_t at = (uint32_t)(w - starts[lo]);
+      const uint32_t at = (uint32_t)(number - starts[lo]);
       const uint32_t T = (uint32_t)(of_group ? shared[lo] : tiles[lo]);
       const uint32_t n = (uint32_t)chunks_of((int)T, of_group ? length_g : length_b);
-      const uint32_t readers = (uint32_t)(of_group ? row_tiles(lo) : own_tiles);
-      uint32_t stream = at, reader_at = 0;
-      if (readers > 1) {
-        const uint32_t bundle = at / (8 * readers), in = at - bundle * 8 * readers;
-        reader_at = in / 8;
-        stream = bundle * 8 + in % 8;
+      int kvh, chunk, reader_at = 0;
+      if (of_group) {
+        const uint32_t readers = (uint32_t)row_tiles(lo);
+        uint32_t stream = at;
+        if (readers > 1) {
+          const uint32_t bundle = at / (8 * readers), in = at - bundle * 8 * readers;
+          reader_at = (int)(in / 8);
+          stream = bundle * 8 + in % 8;
+        }
+        kvh = (int)(stream / n);
+        chunk = (int)(stream - kvh * n);
+      } else {
+        chunk = (int)at;
+        kvh = own_reader / own_tiles;
+        reader_at = own_reader - kvh * own_tiles;
       }
-      const int kvh = (int)(stream / n), chunk = (int)(stream - kvh * n);
       if (kvh < p.H_KV) {
         const int first = of_group || group[lo] < 0 ? 0 : shared[group[lo]];
         u.t0 = first + (int)(T * (uint32_t)chunk / n);  // T < 2^26, at most 64 chunks
@@ -295,14 +310,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
           u.table = reader[lo];
           u.end = (int)T * kKeysPerTile;
           u.seq0 = cu[lo];
-          u.row0 = (int)reader_at * kSharedRows;
+          u.row0 = reader_at * kSharedRows;
           u.rows_kvh = min(rows - u.row0, kSharedRows) | kvh << 8;
           u.state0 = (state_g[lo] + chunk * (cu[lo + 1] - cu[lo])) * p.H_Q;
         } else {
           u.table = lo;
           u.end = max(0, min(p.seq_lens[lo], p.L_K));
           u.seq0 = lo;
-          u.row0 = (int)reader_at * p.hpt;
+          u.row0 = reader_at * p.hpt;
           u.rows_kvh = p.hpt | kvh << 8;
           u.state0 = n == 1 && first == 0 ? -1 : (state_b[lo] + chunk) * p.H_Q;
         }
@@ -508,13 +523,13 @@ __device__ __forceinline__ void stream_unit(const PrefixParams& p, const Unit& u
 
 // The same by one wave, tile after tile, without the others: what a batch of many
 // sequences has behind its prefixes.
-template <int NT>
-__device__ __forceinline__ void wave_unit(const PrefixParams& p, const Unit& u, unsigned char* smem, int lane,
-                                          int wave) {
+template <int NT, typename Ready>
+__device__ __forceinline__ void wave_unit(const PrefixParams& p, const Unit& u, unsigned char* smem, int lane, int wave,
+                                          Ready ready) {
   const int rows = u.rows_kvh & 255, kvh = u.rows_kvh >> 8;
   const int col = lane & 15, quad = lane >> 4;
   TileReducer<NT, 8> red;
-  stream_tiles(p, u, red, smem + wave * kWaveStage, u.t0, std::integral_constant<int, 1>{}, lane, [] {});
+  stream_tiles(p, u, red, smem + wave * kWaveStage, u.t0, std::integral_constant<int, 1>{}, lane, ready);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = nt * 16 + col;
@@ -875,19 +890,27 @@ __global__ void __launch_bounds__(64 * kUnitWaves, 2) unit_kernel(PrefixParams p
         const uint32_t i = (uint32_t)own_given + (uint32_t)__builtin_amdgcn_readfirstlane((int)t);
         return own_given < n_own && i < (uint32_t)n_own ? (int)i : n_own;
       };
+      auto words = [&](int i) {
+        return i < n_own ? reinterpret_cast<const int32_t*>(list.list + 8 * i + xcd)[lane & 7] : 0;
+      };
       int i = wave >= kOwnWaves ? n_own : turn == 0 ? (at - front) * kOwnWaves + wave : number(take());
+      int word = words(i);
       while (i < n_own) {
-        const Unit u = unit_of(reinterpret_cast<const int32_t*>(list.list + 8 * i + xcd)[lane & 7]);
+        const Unit u = unit_of(word);
         const uint32_t t = take();
+        // the next unit's words are on their way while this one's tiles are read
+        auto ready = [&]() {
+          i = number(t);
+          word = words(i);
+        };
         int ln = lane;
         asm volatile("" : "+v"(ln));
         if ((u.rows_kvh & 255) == 0)
-          ;
+          ready();
         else if ((u.rows_kvh & 255) <= 16)
-          wave_unit<1>(p, u, smem, ln, wave);
+          wave_unit<1>(p, u, smem, ln, wave, ready);
         else
-          wave_unit<2>(p, u, smem, ln, wave);
-        i = number(t);
+          wave_unit<2>(p, u, smem, ln, wave, ready);
       }
       __syncthreads();
       continue;
@@ -983,6 +1006,13 @@ int launched(hipError_t e, const char* what) {
   return e == hipSuccess ? (int)DA_OK : da::fail(DA_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
 }
 
+// Bytes of K and V that the batch's sequences hold at most, shared keys counted for each, up to which they are all read:
+// what is shared then comes out of L2 and the last-level cache at twice HBM's rate and more, and one launch does.  By
+// those bytes, this call's sharing launches and the one launch (us; 64/8 heads): 5 MB 15 and 6.6, 75 MB 23 and 8.1, 276
+// MB 30 and 18, 330 MB 30 and 25, 598 MB 34 and 43, 1140 MB 41 and 79.  Groups of more than 16 heads need the matrix
+// cores twice as long for as many bytes: 32/1 heads 270 MB 42 and 27, 1080 MB 76 and 76.
+constexpr int64_t kUnsharedBytes = 384ll << 20;
+
 // Sizes of a call's workspace: room for what the plan may choose, and at the
 // least for one chunk of each prefix and of each sequence.
 struct PrefixSizes {
@@ -995,9 +1025,9 @@ PrefixSizes prefix_sizes(int B, int G, int H_Q, int H_KV, int cus) {
   const int hpt = da::heads_per_tile(H_Q, H_KV, 1);
   const int64_t readers = g / hpt;
   PrefixSizes z{};
-  // row tiles of all groups, their streams in whole bundles of 8; the list itself in whole eights
+  // of either list: row tiles of all groups, their streams in whole bundles of 8, or a chunk of each sequence
   const int64_t tiles = B * g / kSharedRows + G;
-  z.units = 16 + 8 * slots + tiles * (H_KV + 7) + B * readers * (H_KV + (readers > 1 ? 7 : 0));
+  z.units = 16 + 8 * slots + std::max<int64_t>(tiles * (H_KV + 7), (B + 7ll) * H_KV * readers);
   z.rows = kSharedRows * slots + 2ll * B * H_Q;
   auto up = [](int64_t x) { return (size_t)((x + 255) / 256 * 256); };
   z.unit_at = 256 + 16 * 128;
@@ -1055,6 +1085,15 @@ int da_decode_attn_prefix(const void* q, const void* k_cache, const void* v_cach
   rc = ensure_gfx950(&cus);
   if (rc) return rc;
   const PrefixSizes z = prefix_sizes(B, G, H_Q, H_KV, cus);
+  const int64_t bytes = (int64_t)B * L_K_max * H_KV * D * 4;
+  if (chunk_keys == 0 && workspace && workspace_bytes >= z.total && bytes <= kUnsharedBytes * (H_Q / H_KV > 16 ? 2 : 1)) {
+    // a window that hides nothing
+    const int rc1 = da_decode_attn_window(q, k_cache, v_cache, nullptr, block_table, seq_lens, page_size, max_pages,
+                                          num_pages, out, lse_out, B, H_Q, H_KV, L_K_max, d, softmax_scale,
+                                          std::max(L_K_max, 1), 0, 0, -1, workspace, workspace_bytes, stream);
+    if (rc1 != DA_ERR_WORKSPACE) return rc1;
+    da::clear_error();
+  }
   if (!workspace || workspace_bytes < z.total)
     return da::fail(DA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", z.total, workspace ? workspace_bytes : 0);
   PrefixParams p{};

@@ -85,11 +85,14 @@ class Groups:
         return torch.full(self.q.shape[:2], 7.0, dtype=torch.float32, device="cuda")
 
     def check(self, what, **kw):
-        say(f"prefix {what}")
-        lse = self.lse()
-        out = self.call(lse, **kw)
-        torch.cuda.synchronize()
-        check_attention(out, lse, self.reference(), what)
+        """The sharing launches with chosen chunks (or those that kw asks for), and what the call takes by itself."""
+        ref = self.reference()
+        for chunk in [kw.pop("chunk_keys", -1), 0]:
+            say(f"prefix {what} chunk_keys {chunk}")
+            lse = self.lse()
+            out = self.call(lse, chunk_keys=chunk, **kw)
+            torch.cuda.synchronize()
+            check_attention(out, lse, ref, f"{what}, chunk_keys {chunk}")
         return out
 
 
@@ -144,10 +147,11 @@ def test_empty_and_short_sequences_within_a_group():
     Groups([(8, 512)], [0], 16, 2, 32, seed=5, lens=lens).check("shorter than the prefix")
     Groups([(8, 512)], [0], 16, 2, 32, seed=6, lens=[0] * 7 + [40]).check("one that has keys")
     g = Groups([(5, 512)], [0], 16, 2, 32, seed=7, lens=[0] * 5)
-    lse = g.lse()
-    out = g.call(lse, L=0)
-    torch.cuda.synchronize()
-    assert (out == 0).all() and torch.isneginf(lse).all()
+    for chunk in (0, -1):
+        lse = g.lse()
+        out = g.call(lse, L=0, chunk_keys=chunk)
+        torch.cuda.synchronize()
+        assert (out == 0).all() and torch.isneginf(lse).all()
 
 
 @pytest.mark.parametrize("chunk", [1, 32, 64, 100, 512, 10 ** 6, 2 ** 31 - 1])
@@ -181,9 +185,9 @@ def test_most_requests():
 def test_a_bound_below_the_lengths_cuts_them():
     g = Groups([(6, 300)], [200, 10], 16, 2, 32, seed=14)
     say("prefix under a lower L_K_max")
-    for L in (320, 256):
+    for L, chunk in ((320, -1), (256, -1), (256, 0)):
         lse = g.lse()
-        out = g.call(lse, L=L)
+        out = g.call(lse, L=L, chunk_keys=chunk)
         torch.cuda.synchronize()
         check_attention(out, lse, g.reference(lens=[min(n, L) for n in g.lens]), f"L_K_max {L}")
 
@@ -202,14 +206,16 @@ def test_pages_outside_the_pool_read_as_zeros(rows):
         ks.append(k[r] * ok[:, None, None])
         vs.append(v[r] * ok[:, None, None])
     say("prefix pages outside")
-    lse = g.lse()
-    out = g.call(lse)
-    torch.cuda.synchronize()
-    check_attention(out, lse, attend(bf16_bits_to_f64(g.q), ks, vs, None), "pages outside")
+    for chunk in (-1, 0):
+        lse = g.lse()
+        out = g.call(lse, chunk_keys=chunk)
+        torch.cuda.synchronize()
+        check_attention(out, lse, attend(bf16_bits_to_f64(g.q), ks, vs, None), f"pages outside, chunk_keys {chunk}")
 
 
 @pytest.mark.parametrize("n", [2, 6, 20])
-def test_values_that_are_not_finite_reach_their_rows_only(n):
+@pytest.mark.parametrize("chunk", [-1, 0])
+def test_values_that_are_not_finite_reach_their_rows_only(n, chunk):
     g = Groups([(n, 320), (2, 64)], [40], 16, 2, 32, seed=16)
     g.q[1, 3, 5] = 0x7FC0                                      # a query
     g.k.reshape(-1, 2, 128)[g.rows(n)[70], 1, 9] = 0x7FC0      # an own key of the second group
@@ -220,9 +226,9 @@ def test_values_that_are_not_finite_reach_their_rows_only(n):
         seen[g.rows(b)] = True
     for x in (g.k, g.v):
         x.reshape(-1, 2, 128)[~seen] = 0x7FC0
-    say(f"prefix NaN n={n}")
+    say(f"prefix NaN n={n} chunk_keys {chunk}")
     lse = g.lse()
-    out = g.call(lse)
+    out = g.call(lse, chunk_keys=chunk)
     torch.cuda.synchronize()
     o, l = to_f64(out), lse.cpu().numpy()
     bad = np.zeros(o.shape[:2], bool)
@@ -247,7 +253,7 @@ def test_scales(scale):
     g = Groups([(7, 300)], [33], 16, 2, 32, seed=17)
     lse = g.lse()
     say(f"prefix scale {scale}")
-    out = g.call(lse, softmax_scale=scale)
+    out = g.call(lse, softmax_scale=scale, chunk_keys=-1)
     torch.cuda.synchronize()
     o, l, size = g.reference(float(np.float32(scale)))
     tol = (2.0 ** -8 + 2.0 ** -12) * size + 2.0 ** -8 * np.abs(o) * (1 + 2.0 ** -7)
@@ -274,24 +280,25 @@ def test_same_as_the_paged_call_without_groups():
     g = Groups([(5, 0)], [300, 64, 1], 64, 8, 64, seed=19)
     a = g.lse()
     b = g.lse()
-    g.call(a, cu=np.zeros(1, np.int32), pre=np.zeros(0, np.int32))
+    g.call(a, cu=np.zeros(1, np.int32), pre=np.zeros(0, np.int32), chunk_keys=-1)
     da.da_decode_attn_paged(to_dev(g.q), to_dev(g.k), to_dev(g.v), torch.from_numpy(g.table).cuda(),
                             torch.tensor(g.lens, dtype=torch.int32, device="cuda"), g.L, lse_out=b)
     torch.cuda.synchronize()
     assert torch.allclose(a, b, rtol=0, atol=2.0 ** -12)
 
 
-def test_captured_replays_follow_lengths_and_groups():
+@pytest.mark.parametrize("chunk", [-1, 0])
+def test_captured_replays_follow_lengths_and_groups(chunk):
     g = Groups([(9, 640), (3, 100)], [100], 16, 2, 32, seed=20)
     ints = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
     lens = ints(np.array(g.lens, np.int32))
     cu, pre = ints(g.cu), ints(g.pre)
     q, k, v, table, lse = to_dev(g.q), to_dev(g.k), to_dev(g.v), ints(g.table), g.lse()
-    eager_out = da.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, g.L)
+    eager_out = da.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, g.L, chunk_keys=chunk)
     graph = torch.cuda.CUDAGraph()
     say("prefix captured")
     with torch.cuda.graph(graph):
-        out = da.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, g.L, lse_out=lse)
+        out = da.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, g.L, lse_out=lse, chunk_keys=chunk)
     full = list(g.lens)
     for i, (cut, groups) in enumerate([(0, g.pre), (60, g.pre), (99, np.array([200, 0])), (0, np.array([640, 64]))]):
         g.lens = [n - (cut if b % 2 else 0) for b, n in enumerate(full)]
@@ -303,7 +310,7 @@ def test_captured_replays_follow_lengths_and_groups():
         check_attention(out, lse, g.reference(), f"replay {i}")
         if i == 0:
             assert torch.equal(out, eager_out)
-        da.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, g.L)  # eager work between the replays
+        da.da_decode_attn_prefix(q, k, v, table, lens, cu, pre, g.L, chunk_keys=-1)  # eager work between the replays
         torch.cuda.synchronize()
 
 
@@ -311,26 +318,37 @@ def test_a_callers_workspace_and_stream():
     g = Groups([(9, 640)], [100], 16, 2, 32, seed=21)
     need = da.da_prefix_workspace_bytes(9, 1, 16, 2)
     ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    ws[-(1 << 20):] = 0
     other = torch.cuda.Stream()
     torch.cuda.synchronize()
     say("prefix on another stream")
-    lse = g.lse()
-    torch.cuda.synchronize()
-    out = g.call(lse, workspace=ws, stream=other)
-    torch.cuda.synchronize()
-    check_attention(out, lse, g.reference(), "own workspace")
-    assert (ws[-(1 << 20):] == 0xFF).all()
+    for chunk in (-1, 0, -1):
+        lse = g.lse()
+        torch.cuda.synchronize()
+        out = g.call(lse, workspace=ws, stream=other, chunk_keys=chunk)
+        torch.cuda.synchronize()
+        check_attention(out, lse, g.reference(), "own workspace")
+        assert not ws[-(1 << 20):].any()
     with pytest.raises(da.DecodeAttnError):
         g.call(workspace=ws[:need - 256])
+    with pytest.raises(da.DecodeAttnError):
+        g.call(workspace=ws[:need - 256], chunk_keys=-1)
+
+
+@pytest.mark.parametrize("H_Q,H_KV,B,L", [(16, 16, 3, 16384), (16, 16, 3, 16385), (32, 1, 96, 16384), (32, 1, 97, 16384)])
+def test_both_sides_of_the_size_that_is_worth_sharing(H_Q, H_KV, B, L):
+    """384 MiB of keys and values (768 where more than 16 heads share them) by the bound, for lengths far below it."""
+    say(f"prefix bound {B} x {L}")
+    Groups([(B, 300)], [40, 0, 7], H_Q, H_KV, 32, seed=23, max_pages=513).check(f"bound {B} x {L}", L=L)
 
 
 def test_two_streams_at_once():
     g = Groups([(12, 2000)], [300, 10], 32, 4, 32, seed=22)
     streams = [torch.cuda.Stream() for _ in range(2)]
     args = dict(kv=(to_dev(g.k), to_dev(g.v)), q=to_dev(g.q))
-    want = g.call(**args)
+    want = g.call(chunk_keys=-1, **args)
     torch.cuda.synchronize()
     say("prefix on two streams")
-    got = [g.call(stream=s, **args) for _ in range(5) for s in streams]
+    got = [g.call(stream=s, chunk_keys=-1, **args) for _ in range(5) for s in streams]
     torch.cuda.synchronize()
     assert all(torch.equal(x, want) for x in got)

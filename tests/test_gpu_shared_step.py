@@ -24,7 +24,8 @@ def bits(t):
 class Server:
     """Five requests: three after one prompt of 96 tokens, two after another of 64; their pages off one free list."""
 
-    def __init__(self, seed=0):
+    def __init__(self, chunk_keys=0, seed=0):
+        self.chunk_keys = chunk_keys
         rng = np.random.default_rng(seed)
         ints = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
         self.groups, own = [(3, 96), (2, 64)], [10, 33, 1, 60, 25]
@@ -75,7 +76,7 @@ class Server:
 
     def attend(self):
         self.out = da.da_decode_attn_prefix(self.q, self.k, self.v, self.table, self.lens, self.cu, self.pre, L_MAX,
-                                            lse_out=self.lse)
+                                            lse_out=self.lse, chunk_keys=self.chunk_keys)
 
     def weigh(self):
         da.da_add_key_weights(self.q, self.k, self.table, self.lens, self.lse, self.weights, L_MAX, 0.9)
@@ -98,8 +99,10 @@ def rows(table, b, n):
     return table[b, j // PAGE].astype(np.int64) * PAGE + j % PAGE
 
 
-def test_each_call_of_a_step_against_the_oracle():
-    s = Server()
+# negative: the sharing launches, which so small a batch does not take by itself
+@pytest.mark.parametrize("chunk_keys", [0, -1])
+def test_each_call_of_a_step_against_the_oracle(chunk_keys):
+    s = Server(chunk_keys)
     evicted = returned = 0
     for t in range(40):
         say(f"step {t}")
@@ -166,13 +169,14 @@ def test_each_call_of_a_step_against_the_oracle():
         assert np.array_equal(bits(first.k).reshape(-1, H_KV, 128)[r], bits(s.k).reshape(-1, H_KV, 128)[r])
 
 
-def test_a_captured_step_gives_the_bits_of_the_eager_one():
-    eager, s = Server(), Server()
+@pytest.mark.parametrize("chunk_keys", [0, -1])
+def test_a_captured_step_gives_the_bits_of_the_eager_one(chunk_keys):
+    eager, s = Server(chunk_keys), Server(chunk_keys)
     s.draw(0)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):  # before the capture, on a state of its own
-        warm = Server()
+        warm = Server(chunk_keys)
         warm.draw(0)
         warm.step()
     torch.cuda.current_stream().wait_stream(side)
