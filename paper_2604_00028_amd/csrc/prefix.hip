@@ -170,10 +170,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     // About a unit a CU of shared keys (128 tiles at most: more are dealt as they run out).  Shorter ones write more
     // states, whose merge costs as much: 32 sequences over 8192 keys in 256 units of 16 tiles 38.8 us, in 512 of 8 47.8;
     // 128 over 16384, with own parts, in units of 128 tiles 150 us, of 64 161 (without own parts 119 and 112).
-    // Half as many of a sequence's own keys by a workgroup each, or long ones for a wave each where there are many.
+    // Half as many of a sequence's own keys by a workgroup each; where there are many, twice a wave's share for a wave
+    // each (100 sequences of 50 and 1627 keys in chunks of 16 tiles 64 us, of 64 114; 128 of 100 to 1500 in chunks of 33
+    // 116, of 64 96).
     waves = work_b >= 24 * p.slots;
     length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 128);
-    length_b = p.chunk_tiles > 0 ? p.chunk_tiles : waves ? min(max(work_b / (3 * p.slots / 2), 8), 64) : min(max(work_b / (p.slots / 4), 4), 64);
+    length_b = p.chunk_tiles > 0 ? p.chunk_tiles : waves ? min(max(work_b / p.slots, 8), 64) : min(max(work_b / (p.slots / 4), 4), 64);
     auto longer = [&](int length, int w) { return (int)min((int64_t)length << w, (int64_t)kWhole); };
     int w = 0;
     for (;; w += kPlanWaves) {
