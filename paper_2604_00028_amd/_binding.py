@@ -1018,7 +1018,7 @@ def da_append_kv4(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, p
 def _axis_bytes(axes, rope) -> bytes:
     if rope is None:
         raise ValueError("rope is required")
-    return axes if isinstance(axes, bytes) else bytes(axes)
+    return axes if isinstance(axes, bytes) else bytes(list(axes))  # of an array its numbers, not its memory
 
 
 def da_append_kv_axes(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,

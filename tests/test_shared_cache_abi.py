@@ -7,6 +7,7 @@ import torch
 
 import paper_2604_00028_amd as da
 from oracle.cache import norm_rotate, norm_rotate_axes
+from paper_2604_00028_amd._binding import _axis_bytes
 from tests.test_cache_abi import ALIGN, ARG, FAKE, NULL, SHAPE, UNSUP, refused
 
 
@@ -40,6 +41,18 @@ def test_axes_python_refusals():
     with pytest.raises(ValueError, match="GPU"):
         da.da_append_kv_axes(bf(1, 8, 128), bf(1, 1, 128), bf(1, 1, 128), torch.zeros(3, 1, dtype=torch.int32), None,
                              bf(4, 1, 128), bf(4, 1, 128), rope=torch.zeros(4, 16), axes=[0] * 8)
+
+
+@pytest.mark.parametrize("axes", [[0, 2, 1, 0, 2, 1, 0, 0], range(8), np.arange(8), np.arange(8, dtype=np.uint8),
+                                  torch.arange(8), bytearray(range(8))])
+def test_axes_are_taken_by_their_numbers(axes):
+    assert _axis_bytes(axes, torch.zeros(4, 16)) == bytes(int(a) for a in axes)
+
+
+@pytest.mark.parametrize("axes,error", [(16, TypeError), ([0.0] * 8, TypeError), ([256] * 8, ValueError), ([-1] * 8, ValueError)])
+def test_axes_that_are_no_small_numbers(axes, error):
+    with pytest.raises(error):
+        _axis_bytes(axes, torch.zeros(4, 16))
 
 
 @pytest.mark.parametrize("neighbours", [False, True])
