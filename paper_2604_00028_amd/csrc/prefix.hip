@@ -63,7 +63,7 @@ struct PrefixParams {
   int slots;          // workgroups that run at once
   int own_tiles;      // head tiles of a KV head
   int chunk_tiles;    // 0: chosen on the device
-  Div div_page, div_g, div_heads, div_hq;
+  Div div_page, div_g, div_hq;
   float scale_log2;
 };
 
@@ -82,15 +82,16 @@ __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readl
 // sequence's that has keys if that is less, in whole tiles; a group of one such
 // sequence shares none.  They are cut into chunks for tiles of up to 128 of the
 // group's query rows, and what each sequence has behind them into chunks for
-// the heads of each KV head, by the rules beside the lengths below.  Units are dealt round robin to the XCDs; the row tiles of a chunk, which read
-// the same keys, stand 8 apart, one behind the other in one XCD's list.
+// the heads of each KV head, by the rules beside the lengths below.  Units are
+// dealt round robin to the XCDs; the row tiles of a chunk, which read the same
+// keys, stand 8 apart, one behind the other in one XCD's list.
 // Bound by latency (barriers, dependent LDS reads, a cold instruction cache).
 template <int kPlanThreads>
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
   constexpr int kPlanWaves = kPlanThreads / 64;
   extern __shared__ int32_t lds[];
   __shared__ int4 sums[kPlanWaves];
-  __shared__ int price[kPlanWaves];
+  __shared__ int fit[kPlanWaves];
   __shared__ int backwards[kPlanWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* tiles = lds;            // [B] keys, then tiles of the sequence's own keys
@@ -175,7 +176,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     // 116, of 64 96).
     waves = work_b >= 24 * p.slots;
     length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 128);
-    length_b = p.chunk_tiles > 0 ? p.chunk_tiles : waves ? min(max(work_b / p.slots, 8), 64) : min(max(work_b / (p.slots / 4), 4), 64);
+    length_b = p.chunk_tiles > 0 ? p.chunk_tiles
+               : waves           ? min(max(work_b / p.slots, 8), 64)
+                                 : min(max(work_b / (p.slots / 4), 4), 64);
     auto longer = [&](int length, int w) { return (int)min((int64_t)length << w, (int64_t)kWhole); };
     int w = 0;
     for (;; w += kPlanWaves) {
@@ -191,10 +194,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
       const int u = wave_total(min(units, 1 << 24)), r = wave_total(min(rows, 1 << 24));
       const int64_t own_units = (int64_t)((wave_total(chunks) + 7) / 8 * 8) * own_readers;
       const bool fits = u + 7 <= p.most_units && own_units <= p.most_units && (int64_t)r * p.H_Q <= p.most_rows;
-      if (lane == 0) price[wave] = fits;
+      if (lane == 0) fit[wave] = fits;
       __syncthreads();
       int k = 0;
-      while (k < kPlanWaves && !price[k]) ++k;
+      while (k < kPlanWaves && !fit[k]) ++k;
       if (k < kPlanWaves || w + kPlanWaves >= 32) {  // whole prefixes and sequences always fit
         w += k;
         break;
@@ -1089,11 +1092,15 @@ int da_decode_attn_prefix(const void* q, const void* k_cache, const void* v_cach
   const PrefixSizes z = prefix_sizes(B, G, H_Q, H_KV, cus);
   const int64_t bytes = (int64_t)B * L_K_max * H_KV * D * 4;
   if (chunk_keys == 0 && workspace && workspace_bytes >= z.total && bytes <= kUnsharedBytes * (H_Q / H_KV > 16 ? 2 : 1)) {
-    // a window that hides nothing
+    // a window that hides nothing, in as much workspace as this call asks for, taken at the end (where the counters are): a
+    // larger one does not change which launches run, and with them the result's last bits
+    const size_t spare = (workspace_bytes - z.total) / 256 * 256;
     const int rc1 = da_decode_attn_window(q, k_cache, v_cache, nullptr, block_table, seq_lens, page_size, max_pages,
                                           num_pages, out, lse_out, B, H_Q, H_KV, L_K_max, d, softmax_scale,
-                                          std::max(L_K_max, 1), 0, 0, -1, workspace, workspace_bytes, stream);
-    if (rc1 != DA_ERR_WORKSPACE) return rc1;
+                                          std::max(L_K_max, 1), 0, 0, -1, static_cast<unsigned char*>(workspace) + spare,
+                                          workspace_bytes - spare, stream);
+    // more chunk states than that holds, or than one launch may write
+    if (rc1 != DA_ERR_WORKSPACE && rc1 != DA_ERR_SHAPE) return rc1;
     da::clear_error();
   }
   if (!workspace || workspace_bytes < z.total)
@@ -1133,7 +1140,6 @@ int da_decode_attn_prefix(const void* q, const void* k_cache, const void* v_cach
   p.chunk_tiles = chunk_keys > 0 ? (int)(((int64_t)chunk_keys + kKeysPerTile - 1) / kKeysPerTile) : 0;
   p.div_page = make_div((uint32_t)page_size);
   p.div_g = make_div((uint32_t)p.g);
-  p.div_heads = make_div((uint32_t)H_KV);
   p.div_hq = make_div((uint32_t)H_Q);
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * kLog2e;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1142,7 +1148,7 @@ int da_decode_attn_prefix(const void* q, const void* k_cache, const void* v_cach
   // few sequences: a wave a SIMD, whose instructions do not wait for three others' (B=2: 6.9 -> 5.9 us)
   const int plan_threads = (int64_t)B * H_KV <= 512 ? 256 : 1024;
   const void* plan = plan_threads == 256 ? reinterpret_cast<const void*>(&plan_kernel<256>)
-                              : reinterpret_cast<const void*>(&plan_kernel<1024>);
+                                         : reinterpret_cast<const void*>(&plan_kernel<1024>);
   rc = launched(hipLaunchKernel(plan, dim3(1), dim3(plan_threads), args, plan_smem, s), "prefix plan");
   if (rc) return rc;
   rc = launched(hipLaunchKernel(reinterpret_cast<const void*>(&unit_kernel), dim3((uint32_t)p.slots),

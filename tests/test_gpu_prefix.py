@@ -342,6 +342,24 @@ def test_both_sides_of_the_size_that_is_worth_sharing(H_Q, H_KV, B, L):
     Groups([(B, 300)], [40, 0, 7], H_Q, H_KV, 32, seed=23, max_pages=513).check(f"bound {B} x {L}", L=L)
 
 
+@pytest.mark.parametrize("H_Q,H_KV,B,L", [(128, 1, 33, 20000), (37, 1, 64, 20000), (128, 1, 22, 4000)])
+def test_a_larger_workspace_gives_the_same_bits(H_Q, H_KV, B, L):
+    """Also where the one launch would write more chunk states than the call asks room for."""
+    g = Groups([(B, 600)], [2000, 31], H_Q, H_KV, 32, seed=24, max_pages=625)
+    need = da.da_prefix_workspace_bytes(B, 1, H_Q, H_KV)
+    kv, outs = (to_dev(g.k), to_dev(g.v)), []
+    for more in (0, 100, 256, 7 * need + 12):
+        ws = torch.zeros(need + more, dtype=torch.uint8, device="cuda")
+        say(f"prefix workspace {need} + {more}")
+        lse = g.lse()
+        out = g.call(lse, L=L, kv=kv, workspace=ws)
+        torch.cuda.synchronize()
+        outs.append((out, lse))
+        assert not ws[(len(ws) & -256) - (1 << 20):].any()
+    check_attention(*outs[0], g.reference(), f"bound {L}")
+    assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(o, outs[0]))
+
+
 def test_two_streams_at_once():
     g = Groups([(12, 2000)], [300, 10], 32, 4, 32, seed=22)
     streams = [torch.cuda.Stream() for _ in range(2)]
