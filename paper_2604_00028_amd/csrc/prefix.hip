@@ -630,21 +630,19 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     --in_page;
     ++next_tile;
   };
-  uint32_t kro[2][4], vro[2][8];
+  // K and V of a tile as operands: where this lane's pieces of the tile's first half lie; those of the second, and of the
+  // ring's other places, lie a constant further on
+  uint32_t kro[4], vro[8];
   {
     const int kr = col & 3, vk = col >> 2, vm = col & 3;
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
+    for (int j = 0; j < 4; ++j)
+      kro[j] = lds_offset(smem) +
+               (uint32_t)((col >> 2) * kBlockStride + kr * 256 + 16 * ((4 * j + quad + 2 * kr) & 15));
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        kro[mt][j] = lds_offset(smem) + (uint32_t)((4 * mt + (col >> 2)) * kBlockStride + kr * 256 +
-                                                   16 * ((4 * j + quad + 2 * kr) & 15));
-#pragma unroll
-      for (int nn = 0; nn < 8; ++nn)
-        vro[mt][nn] = lds_offset(smem) +
-                      (uint32_t)(kStages * kLdsTileBytes + (4 * mt + quad) * kBlockStride + vk * 256 +
-                                 16 * ((2 * nn + (vm >> 1) + 2 * vk) & 15) + 8 * (vm & 1));
-    }
+    for (int nn = 0; nn < 8; ++nn)
+      vro[nn] = lds_offset(smem) + (uint32_t)(kStages * kLdsTileBytes + quad * kBlockStride + vk * 256 +
+                                              16 * ((2 * nn + (vm >> 1) + 2 * vk) & 15) + 8 * (vm & 1));
   }
   const int n = u.t1 - u.t0;
   // K waves run one tile further ahead
@@ -663,28 +661,33 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
 #pragma unroll
     for (int nn = 0; nn < 8; ++nn) red.o[nt][nn] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  auto read_k = [&](bf16x8 (&kop)[2][4], uint32_t so) {
+  // of the ring's place `at`, a constant, `more` bytes behind it
+  auto read_k = [&](bf16x8 (&kop)[2][4], auto at, uint32_t more) {
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        kop[mt][j] = as_bf16x8(
-            *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>((uintptr_t)(kro[mt][j] + so)));
+        kop[mt][j] = as_bf16x8(*reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(
+            (uintptr_t)(kro[j] + more + decltype(at)::value * kLdsTileBytes + mt * 4 * kBlockStride)));
   };
   // V of a tile, transposed (TileReducer::pv).  In assembly with its wait: for the
   // compiler's own form of the instruction it waits for every load into LDS.
-  auto read_v = [&](s16x4 (&lo)[8], s16x4 (&hi)[8], uint32_t so) {
-#define DA_READ(x, i) "ds_read_b64_tr_b16 %" #x ", %" #i "\n"
-    asm volatile(DA_READ(0, 16) DA_READ(1, 17) DA_READ(2, 18) DA_READ(3, 19) DA_READ(4, 20) DA_READ(5, 21)
-                     DA_READ(6, 22) DA_READ(7, 23) DA_READ(8, 24) DA_READ(9, 25) DA_READ(10, 26) DA_READ(11, 27)
-                         DA_READ(12, 28) DA_READ(13, 29) DA_READ(14, 30) DA_READ(15, 31) "s_waitcnt lgkmcnt(0)"
+  auto read_v = [&](s16x4 (&lo)[8], s16x4 (&hi)[8], auto at, uint32_t more) {
+    constexpr int kFirst = decltype(at)::value * kLdsTileBytes, kSecond = kFirst + 4 * kBlockStride;
+    static_assert(kSecond < 65536, "an offset has 16 bits");
+    uint32_t from[8];
+#pragma unroll
+    for (int nn = 0; nn < 8; ++nn) from[nn] = vro[nn] + more;
+#define DA_READ(lo, hi, i)                              \
+  "ds_read_b64_tr_b16 %" #lo ", %" #i " offset:%24\n" \
+  "ds_read_b64_tr_b16 %" #hi ", %" #i " offset:%25\n"
+    asm volatile(DA_READ(0, 8, 16) DA_READ(1, 9, 17) DA_READ(2, 10, 18) DA_READ(3, 11, 19) DA_READ(4, 12, 20)
+                     DA_READ(5, 13, 21) DA_READ(6, 14, 22) DA_READ(7, 15, 23) "s_waitcnt lgkmcnt(0)"
                  : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(lo[2]), "=&v"(lo[3]), "=&v"(lo[4]), "=&v"(lo[5]), "=&v"(lo[6]),
                    "=&v"(lo[7]), "=&v"(hi[0]), "=&v"(hi[1]), "=&v"(hi[2]), "=&v"(hi[3]), "=&v"(hi[4]), "=&v"(hi[5]),
                    "=&v"(hi[6]), "=&v"(hi[7])
-                 : "v"(vro[0][0] + so), "v"(vro[0][1] + so), "v"(vro[0][2] + so), "v"(vro[0][3] + so),
-                   "v"(vro[0][4] + so), "v"(vro[0][5] + so), "v"(vro[0][6] + so), "v"(vro[0][7] + so),
-                   "v"(vro[1][0] + so), "v"(vro[1][1] + so), "v"(vro[1][2] + so), "v"(vro[1][3] + so),
-                   "v"(vro[1][4] + so), "v"(vro[1][5] + so), "v"(vro[1][6] + so), "v"(vro[1][7] + so)
+                 : "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]), "v"(from[4]), "v"(from[5]), "v"(from[6]),
+                   "v"(from[7]), "n"(kFirst), "n"(kSecond)
                  : "memory");
 #undef DA_READ
   };
@@ -712,9 +715,10 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  // Tile i from `sc`, its scores; leaves those of tile i + 1 there.  so, sn: where their stages start.
-  // full: the loads go on behind tile i as far as the rings reach; more: there is a tile i + 1.
-  auto step = [&](f32x4 (&sc)[NT][2], int i, uint32_t so, uint32_t sn, int place, auto more, auto full) {
+  // Tile i from `sc`, its scores; leaves those of tile i + 1 there.  They lie in the ring's places at0 and at1, s0 and
+  // s1 bytes further on.  full: the loads go on behind tile i as far as the rings reach; more: there is a tile i + 1.
+  auto step = [&](f32x4 (&sc)[NT][2], int i, auto at0, auto at1, uint32_t s0, uint32_t s1, int place, auto more,
+                  auto full) {
     // K(i + 1) and V(i) are needed, K up to i + 3 and V up to i + 2 on their way
     if constexpr (decltype(full)::value) {
       arrive(2);
@@ -724,7 +728,7 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
       if (i + deep < n) fetch((place + deep) % kStages);
     }
     bf16x8 kop[2][4];
-    if constexpr (decltype(more)::value) read_k(kop, sn);
+    if constexpr (decltype(more)::value) read_k(kop, at1, s1);
     // The maximum follows at once, so that a row's largest probability is exactly 1 (with a slack of 2^8 the products with
     // the old state's weight were rarer and 128 sequences over 16384 keys 5% faster, but the error against 64 bits 2.2e-3
     // and not 1.8e-3); 16 rows at a time, most tiles move none of them.
@@ -744,7 +748,7 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     f32x4 next[NT][2];
     if constexpr (decltype(more)::value) scores(kop, next);
     s16x4 vlo[8], vhi[8];
-    read_v(vlo, vhi, so);
+    read_v(vlo, vhi, at0, s0);
     bf16x8 pb[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -772,27 +776,31 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
         for (int mt = 0; mt < 2; ++mt) sc[nt][mt] = next[nt][mt];
     }
   };
+  constexpr std::integral_constant<int, 0> place0{};
   f32x4 sc[NT][2];
   {
     arrive(n - 1);  // K(0)
     bf16x8 kop[2][4];
-    read_k(kop, 0);
+    read_k(kop, place0, 0u);
     scores(kop, sc);
   }
   static_assert(kStages == 4, "the loop below takes the stages in turn");
   constexpr uint32_t T = kLdsTileBytes;
+  constexpr std::integral_constant<int, 1> place1{};
+  constexpr std::integral_constant<int, 2> place2{};
+  constexpr std::integral_constant<int, 3> place3{};
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
   int i = 0;
   for (; i + 3 + kStages < n; i += 4) {
-    step(sc, i, 0, T, 0, yes, yes);
-    step(sc, i + 1, T, 2 * T, 1, yes, yes);
-    step(sc, i + 2, 2 * T, 3 * T, 2, yes, yes);
-    step(sc, i + 3, 3 * T, 0, 3, yes, yes);
+    step(sc, i, place0, place1, 0, 0, 0, yes, yes);
+    step(sc, i + 1, place1, place2, 0, 0, 1, yes, yes);
+    step(sc, i + 2, place2, place3, 0, 0, 2, yes, yes);
+    step(sc, i + 3, place3, place0, 0, 0, 3, yes, yes);
   }
-  for (; i + 1 < n; ++i) step(sc, i, (uint32_t)(i & 3) * T, (uint32_t)((i + 1) & 3) * T, i & 3, yes, no);
+  for (; i + 1 < n; ++i) step(sc, i, place0, place0, (uint32_t)(i & 3) * T, (uint32_t)((i + 1) & 3) * T, i & 3, yes, no);
   next.take();
-  step(sc, i, (uint32_t)(i & 3) * T, 0, i & 3, no, no);
+  step(sc, i, place0, place0, (uint32_t)(i & 3) * T, 0, i & 3, no, no);
   next.post();
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
