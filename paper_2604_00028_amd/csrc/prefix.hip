@@ -21,7 +21,6 @@ using da::ensure_gfx950;
 constexpr int kMostGroupChunks = 64;  // of a prefix, and of a sequence's own keys: one a lane in the merge
 constexpr int kSharedRows = 128;      // query rows of the largest unit
 constexpr int kUnitWaves = 4;
-constexpr int kOwnWaves = 2;          // waves of a workgroup that take sequences' units by themselves
 
 // A unit: `rows` query rows against the tiles [t0, t1) of one KV head.  Row r is
 // query head kvh g + (row0 + r) mod g of sequence seq0 + (row0 + r) / g, its
@@ -63,12 +62,14 @@ struct PrefixParams {
   int slots;          // workgroups that run at once
   int own_tiles;      // head tiles of a KV head
   int chunk_tiles;    // 0: chosen on the device
-  Div div_page, div_g, div_hq;
+  Div div_page, div_g, div_hq, div_readers, div_tiles;
   float scale_log2;
 };
 
 // ---------------------------------------------------------------- plan
 
+constexpr int kFewGroups = 16;    // the chunks of so many are weighed against each other; of more, any will do
+constexpr float kUnitTiles = 24;  // what a unit of a group costs besides its tiles, in tiles
 constexpr int kWhole = 1 << 26;  // tiles: longer than any sequence
 
 __device__ __forceinline__ int chunks_of(int tiles, int length) {
@@ -159,9 +160,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
   // units of `streams` streams of keys that `readers` units each read
   auto units_of = [&](int streams, int readers) { return readers == 1 ? streams : (streams + 7) / 8 * 8 * readers; };
   const int own_readers = p.H_KV * own_tiles;  // units that read a sequence's chunk, together whole rows of it
-  // Lengths by the work there is.  Wave w tries them 2^w times as long; the first that fit the workspace are taken.
+  // Lengths by the work there is; wave w tries them 2^w times as long, and the first that fit the workspace are taken.
   int length_g, length_b;
-  bool waves;  // a sequence's own chunks are a wave's work each, not a workgroup's
+  int waves;  // of a workgroup that take a sequence's own chunks, each by itself; 0: a chunk is a workgroup's work
   {
     int work_g = 0, work_b = 0;
     for (int i = lane; i < G; i += 64) work_g += (int)min((int64_t)shared[i] * row_tiles(i), (int64_t)1 << 16);
@@ -170,15 +171,33 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     work_b = min(wave_total(work_b), (1 << 30) / (p.H_KV * own_tiles)) * (p.H_KV * own_tiles);
     // About a unit a CU of shared keys (128 tiles at most: more are dealt as they run out).  Shorter ones write more
     // states, whose merge costs as much: 32 sequences over 8192 keys in 256 units of 16 tiles 38.8 us, in 512 of 8 47.8;
-    // 128 over 16384, with own parts, in units of 128 tiles 150 us, of 64 161 (without own parts 119 and 112).
-    // Half as many of a sequence's own keys by a workgroup each; where there are many, twice a wave's share for a wave
-    // each (100 sequences of 50 and 1627 keys in chunks of 16 tiles 64 us, of 64 114; 128 of 100 to 1500 in chunks of 33
-    // 116, of 64 96).
-    waves = work_b >= 24 * p.slots;
+    // 128 over 16384, with own parts, in units of 128 tiles 145 us, of 64 151.
+    // Half as many of a sequence's own keys, a workgroup each.  Where there are many, a wave each: by four waves of a
+    // workgroup, or by two where the shared keys are the larger work, whose tiles would wait behind them (128 sequences of
+    // 100 to 1500 own keys, by two and by four: over 16384 shared ones 144 and 157 us, over 8192 134 and 117).  Chunks are
+    // as long as two shares of the first waves (64 of 100 to 2000 keys over 8192: one share 87.5, two 84, four 110), or half
+    // of one where there are two (the 144 us: 136).
+    waves = work_b < 24 * p.slots ? 0 : work_b > work_g ? 4 : 2;
     length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 128);
     length_b = p.chunk_tiles > 0 ? p.chunk_tiles
-               : waves           ? min(max(work_b / p.slots, 8), 64)
+               : waves > 0       ? min(max(waves == 2 ? work_b / (2 * p.slots) : work_b / p.slots, 8), 64)
                                  : min(max(work_b / (p.slots / 4), 4), 64);
+    if (G <= kFewGroups && p.chunk_tiles == 0) {
+      // A lane a length, from half of that to two and a half times: of the rounds in which the CUs take the units, and what
+      // one costs, the least product (three groups of 64 sequences over 8192 keys: 288 units of 86 tiles, two rounds, 163 us;
+      // 192 of 128 129).
+      const int tried = max(length_g * (16 + lane) / 32, 4);
+      const float of_length = __builtin_amdgcn_rcpf((float)tried);
+      float units = 0.f, longest = 0.f;
+      for (int i = 0; i < G; ++i) {
+        const float T = (float)shared[i], n = fminf(ceilf(T * of_length - 1e-3f), (float)kMostGroupChunks);
+        units = fmaf(n, (float)row_tiles(i), units);
+        longest = fmaxf(longest, n > 0.f ? T * __builtin_amdgcn_rcpf(n) : 0.f);
+      }
+      const float cost = ceilf(units * (float)p.H_KV / (float)(p.slots / 2)) * (longest + kUnitTiles);
+      const uint64_t least = __ballot(cost == -wave_max(-cost));
+      length_g = __builtin_amdgcn_readlane(tried, least ? 63 - __builtin_clzll(least) : 16);
+    }
     auto longer = [&](int length, int w) { return (int)min((int64_t)length << w, (int64_t)kWhole); };
     int w = 0;
     for (;; w += kPlanWaves) {
@@ -260,75 +279,72 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
   // two lists, each in whole eights: the groups' units, then the sequences', whose chunks are dealt to the XCDs and
   // read there by all heads one behind the other
   const int padded = (all.x + 7) / 8 * 8, total = padded + (all.z + 7) / 8 * 8 * own_readers;
-  Unit* const own_units = p.units + p.most_units;
   if (tid == 0) {
     p.head[0] = padded;
     p.head[1] = total - padded;
     p.head[2] = waves;
   }
-  for (int i = tid; i < total; i += kPlanThreads) {
+  for (int i = tid; i < padded; i += kPlanThreads) {
     Unit u{};
-    const bool of_group = i < padded;
-    const int w = of_group ? i : i - padded;
-    // where the unit stands: of the groups' by itself, of the sequences' its chunk's number and which of its readers it is
-    int number = w, own_reader = 0;
-    if (!of_group) {
-      const uint32_t bundle = (uint32_t)w / (uint32_t)(8 * own_readers), in = (uint32_t)w - bundle * 8 * own_readers;
-      own_reader = (int)(in / 8);
-      number = (int)(bundle * 8 + in % 8);
-    }
-    if (number < (of_group ? all.x : all.z)) {
-      const int32_t* starts = of_group ? unit_g : unit_b;
-      int lo = 0, hi = of_group ? G : p.B;  // the last that starts at or before it
+    if (i < all.x) {
+      int lo = 0, hi = G;  // the last group that starts at or before it
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (starts[mid] <= number)
+        if (unit_g[mid] <= i)
           lo = mid;
         else
           hi = mid;
       }
-      const uint32_t at = (uint32_t)(number - starts[lo]);
-      const uint32_t T = (uint32_t)(of_group ? shared[lo] : tiles[lo]);
-      const uint32_t n = (uint32_t)chunks_of((int)T, of_group ? length_g : length_b);
-      int kvh, chunk, reader_at = 0;
-      if (of_group) {
-        const uint32_t readers = (uint32_t)row_tiles(lo);
-        uint32_t stream = at;
-        if (readers > 1) {
-          const uint32_t bundle = at / (8 * readers), in = at - bundle * 8 * readers;
-          reader_at = (int)(in / 8);
-          stream = bundle * 8 + in % 8;
-        }
-        kvh = (int)(stream / n);
-        chunk = (int)(stream - kvh * n);
-      } else {
-        chunk = (int)at;
-        kvh = own_reader / own_tiles;
-        reader_at = own_reader - kvh * own_tiles;
+      const uint32_t T = (uint32_t)shared[lo], n = (uint32_t)chunks_of((int)T, length_g);
+      const uint32_t readers = (uint32_t)row_tiles(lo);
+      uint32_t stream = (uint32_t)(i - unit_g[lo]), reader_at = 0;
+      if (readers > 1) {
+        const uint32_t bundle = stream / (8 * readers), in = stream - bundle * 8 * readers;
+        reader_at = in / 8;
+        stream = bundle * 8 + in % 8;
       }
-      if (kvh < p.H_KV) {
-        const int first = of_group || group[lo] < 0 ? 0 : shared[group[lo]];
-        u.t0 = first + (int)(T * (uint32_t)chunk / n);  // T < 2^26, at most 64 chunks
-        u.t1 = first + (int)(T * (uint32_t)(chunk + 1) / n);
-        if (of_group) {
-          const int rows = (cu[lo + 1] - cu[lo]) * p.g;
-          u.table = reader[lo];
-          u.end = (int)T * kKeysPerTile;
-          u.seq0 = cu[lo];
-          u.row0 = reader_at * kSharedRows;
-          u.rows_kvh = min(rows - u.row0, kSharedRows) | kvh << 8;
-          u.state0 = (state_g[lo] + chunk * (cu[lo + 1] - cu[lo])) * p.H_Q;
-        } else {
-          u.table = lo;
-          u.end = max(0, min(p.seq_lens[lo], p.L_K));
-          u.seq0 = lo;
-          u.row0 = reader_at * p.hpt;
-          u.rows_kvh = p.hpt | kvh << 8;
-          u.state0 = n == 1 && first == 0 ? -1 : (state_b[lo] + chunk) * p.H_Q;
-        }
+      const int kvh = (int)(stream / n);
+      const uint32_t chunk = stream - (uint32_t)kvh * n;
+      if (kvh < p.H_KV) {  // else it fills a bundle
+        const int size = cu[lo + 1] - cu[lo];
+        u.table = reader[lo];
+        u.end = (int)T * kKeysPerTile;
+        u.t0 = (int)(T * chunk / n);  // T < 2^26, at most 64 chunks
+        u.t1 = (int)(T * (chunk + 1) / n);
+        u.seq0 = cu[lo];
+        u.row0 = (int)reader_at * kSharedRows;
+        u.rows_kvh = min(size * p.g - u.row0, kSharedRows) | kvh << 8;
+        u.state0 = (state_g[lo] + (int)chunk * size) * p.H_Q;
       }
     }
-    (of_group ? p.units : own_units)[w] = u;
+    p.units[i] = u;
+  }
+  // a sequence's chunk for one of its readers: chunk number c of the batch stands c mod 8 in bundle c / 8
+  auto own_place = [&](int number, int own_reader) {
+    return p.units + p.most_units + (int64_t)(number / 8) * 8 * own_readers + 8 * own_reader + number % 8;
+  };
+  for (int i = tid; i < p.B * own_readers; i += kPlanThreads) {
+    const int b = div_by(i, p.div_readers), own_reader = i - b * own_readers;
+    const uint32_t T = (uint32_t)tiles[b];
+    const int n = chunks_of((int)T, length_b), first = group[b] < 0 ? 0 : shared[group[b]];
+    const int kvh = div_by(own_reader, p.div_tiles);
+    Unit u;
+    u.table = b;
+    u.end = max(0, min(p.seq_lens[b], p.L_K));
+    u.seq0 = b;
+    u.row0 = (own_reader - kvh * own_tiles) * p.hpt;
+    u.rows_kvh = p.hpt | kvh << 8;
+    for (int chunk = 0; chunk < n; ++chunk) {
+      u.t0 = first + (int)(T * (uint32_t)chunk / (uint32_t)n);
+      u.t1 = first + (int)(T * (uint32_t)(chunk + 1) / (uint32_t)n);
+      u.state0 = n == 1 && first == 0 ? -1 : (state_b[b] + chunk) * p.H_Q;
+      *own_place(unit_b[b] + chunk, own_reader) = u;
+    }
+  }
+  const int fill = (8 - all.z % 8) % 8;  // of the last bundle
+  for (int i = tid; i < fill * own_readers; i += kPlanThreads) {
+    const int own_reader = i / fill;
+    *own_place(all.z + i - own_reader * fill, own_reader) = Unit{};
   }
 }
 
@@ -881,11 +897,12 @@ __global__ void __launch_bounds__(64 * kUnitWaves, 2) unit_kernel(PrefixParams p
   const int begins = reinterpret_cast<const int32_t*>(p.units + 8 * at + xcd)[lane & 7];
   const int n_group = __builtin_amdgcn_readfirstlane(p.head[0]) / 8;
   const int n_own = __builtin_amdgcn_readfirstlane(p.head[1]) / 8;
-  const bool by_wave = __builtin_amdgcn_readfirstlane(p.head[2]) != 0;
-  const int need = by_wave ? (n_own + kOwnWaves - 1) / kOwnWaves : n_own;  // workgroups that the own units can use
+  const int own_waves = __builtin_amdgcn_readfirstlane(p.head[2]);
+  const bool by_wave = own_waves > 0;
+  const int need = by_wave ? (n_own + own_waves - 1) >> (own_waves == 2 ? 1 : 2) : n_own;  // workgroups that the own units can use
   const int front = min(slots - min(slots / 2, need), n_group);
   // workgroups [0, front) begin with the groups' units, the others with the sequences'
-  const int own_given = (slots - front) * (by_wave ? kOwnWaves : 1);
+  const int own_given = (slots - front) * (by_wave ? own_waves : 1);
   // one body for both lists: the kernel is long, and what a CU has not run yet it fetches in the middle of its work
 #pragma nounroll
   for (int turn = 0; turn < 2; ++turn) {
@@ -906,7 +923,7 @@ __global__ void __launch_bounds__(64 * kUnitWaves, 2) unit_kernel(PrefixParams p
       auto words = [&](int i) {
         return i < n_own ? reinterpret_cast<const int32_t*>(list.list + 8 * i + xcd)[lane & 7] : 0;
       };
-      int i = wave >= kOwnWaves ? n_own : turn == 0 ? (at - front) * kOwnWaves + wave : number(take());
+      int i = wave >= own_waves ? n_own : turn == 0 ? (at - front) * own_waves + wave : number(take());
       int word = words(i);
       while (i < n_own) {
         const Unit u = unit_of(word);
@@ -1149,6 +1166,8 @@ int da_decode_attn_prefix(const void* q, const void* k_cache, const void* v_cach
   p.div_page = make_div((uint32_t)page_size);
   p.div_g = make_div((uint32_t)p.g);
   p.div_hq = make_div((uint32_t)H_Q);
+  p.div_readers = make_div((uint32_t)(H_KV * p.own_tiles));
+  p.div_tiles = make_div((uint32_t)p.own_tiles);
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * kLog2e;
   hipStream_t s = static_cast<hipStream_t>(stream);
   void* args[] = {&p};
