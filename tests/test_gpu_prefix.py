@@ -175,6 +175,20 @@ def test_many_sequences():
     g.check(f"{sum(sizes)} sequences")
 
 
+@pytest.mark.parametrize("groups", [[(35, 64)], [(17, 28000), (18, 28000)]], ids=["four waves", "two waves"])
+def test_own_keys_by_single_waves(groups):
+    """Enough of the sequences' own keys for a wave each, without and with as much work over shared ones; the last of
+    the places that eight chunks share stay empty."""
+    Groups(groups, [1500, 1, 2900, 1700], 8, 8, 32, seed=25).check(f"own keys by waves, {groups}")
+
+
+def test_groups_whose_chunks_fill_the_cus():
+    """Chunk lengths that are weighed against each other: few groups, and one more than are weighed."""
+    for n in (1, 3, 16, 17):
+        g = Groups([(9, 700 + 64 * i) for i in range(n)], [40, 3], 32, 4, 32, seed=26)
+        g.check(f"{n} groups")
+
+
 def test_most_requests():
     """4096 requests, each two a group."""
     g = Groups([(4096, 0)], [1, 40, 3, 0], 2, 2, 32, seed=13)
