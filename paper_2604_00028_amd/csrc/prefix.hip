@@ -591,19 +591,18 @@ struct SharedRows {
   f32x4 o[NT][8];
 };
 
-// The largest of three, without the quieting of NaNs that fmaxf asks for.
+// The largest of three, NaN where one is (v_maximum3_f32): fmaxf would have every product quieted first.  The compiler has
+// to see that a product's result is read, and puts the wait there that the hardware does not have; it sees into no assembly.
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // max_rows (tile.h) with it.
 __device__ __forceinline__ float top_of_rows(float x) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = max3(__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[1]));
+  x = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
   const auto c = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max3(__uint_as_float(c[0]), __uint_as_float(c[1]), __uint_as_float(c[1]));
+  return __builtin_elementwise_maximum(__uint_as_float(c[0]), __uint_as_float(c[1]));
 }
 
 template <int NT, typename Next>
@@ -731,8 +730,18 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  // Tile i from `sc`, its scores; leaves those of tile i + 1 there.  They lie in the ring's places at0 and at1, s0 and
-  // s1 bytes further on.  full: the loads go on behind tile i as far as the rings reach; more: there is a tile i + 1.
+  float tops[NT];  // of the scores in hand, over the rows' keys
+  auto top_of = [&](const f32x4 (&sc)[NT][2]) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const f32x4 a = sc[nt][0], c = sc[nt][1];
+      const float last = __builtin_elementwise_maximum(c[2], c[3]);
+      tops[nt] = p.scale_log2 * top_of_rows(max3(max3(a[0], a[1], a[2]), max3(a[3], c[0], c[1]), last));
+    }
+  };
+  // Tile i from its scores `sc` and their maxima `tops`; leaves those of tile i + 1 there.  The tiles lie in the ring's
+  // places at0 and at1, s0 and s1 bytes further on.  full: the loads go on behind tile i as far as the rings reach; more:
+  // there is a tile i + 1.
   auto step = [&](f32x4 (&sc)[NT][2], int i, auto at0, auto at1, uint32_t s0, uint32_t s1, int place, auto more,
                   auto full) {
     // K(i + 1) and V(i) are needed, K up to i + 3 and V up to i + 2 on their way
@@ -750,10 +759,8 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     // and not 1.8e-3); 16 rows at a time, most tiles move none of them.
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const f32x4 a = sc[nt][0], c = sc[nt][1];
-      const float top = p.scale_log2 * top_of_rows(max3(max3(a[0], a[1], a[2]), max3(a[3], c[0], c[1]), max3(c[2], c[3], c[3])));
-      if (__any(top > red.m[nt])) {
-        const float m = fmaxf(red.m[nt], top);
+      if (__any(tops[nt] > red.m[nt])) {
+        const float m = fmaxf(red.m[nt], tops[nt]);
         const float alpha = __builtin_amdgcn_exp2f(red.m[nt] - m);
         red.m[nt] = m;
         red.l[nt] *= alpha;
@@ -763,20 +770,24 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     }
     f32x4 next[NT][2];
     if constexpr (decltype(more)::value) scores(kop, next);
-    s16x4 vlo[8], vhi[8];
-    read_v(vlo, vhi, at0, s0);
     bf16x8 pb[NT];
+    float xs[NT][8];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float x[8], sum = 0.f;
+      float(&x)[8] = xs[nt];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(fmaf(sc[nt][e / 4][e % 4], p.scale_log2, -red.m[nt]));
-        sum += x[e];
-      }
-      red.l[nt] += sum;
+      for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(sc[nt][e / 4][e % 4], p.scale_log2, -red.m[nt]));
       pb[nt] = as_bf16x8(u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                                pack_bf16x2(x[6], x[7])});
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    s16x4 vlo[8], vhi[8];
+    read_v(vlo, vhi, at0, s0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float(&x)[8] = xs[nt];
+      red.l[nt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
     }
 #pragma unroll
     for (int nn = 0; nn < 8; ++nn) {
@@ -786,11 +797,22 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
         red.o[nt][nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb[nt], red.o[nt][nn], 0, 0, 0);
     }
     if constexpr (decltype(more)::value) {
+      top_of(next);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) sc[nt][mt] = next[nt][mt];
     }
+    // What the compiler would leave for the next step, which begins with a wait, is done behind this one's products, two
+    // vector instructions each (128 sequences over 16384 shared keys alone 118 -> 111 us).
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) asm volatile("" : "+v"(red.l[nt]), "+v"(tops[nt]));
+#pragma unroll
+    for (int i = 0; i < 8 * NT; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
   constexpr std::integral_constant<int, 0> place0{};
   f32x4 sc[NT][2];
@@ -799,6 +821,7 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     bf16x8 kop[2][4];
     read_k(kop, place0, 0u);
     scores(kop, sc);
+    top_of(sc);
   }
   static_assert(kStages == 4, "the loop below takes the stages in turn");
   constexpr uint32_t T = kLdsTileBytes;
