@@ -3,8 +3,10 @@
     python -m paper_2604_00028_amd.build
 
 Compiles the HIP kernels and entry points (csrc/decode_attn.hip, the 4-bit
-cache's attention csrc/kv4.hip, the cache operators csrc/cache_ops.hip) and the
-host planner (csrc/plan.cpp), the sources side by side, and links them into a shared library next to this file.  One more
+cache's attention csrc/kv4.hip, the cache operators csrc/cache_ops.hip, shared
+prefixes csrc/prefix.hip, key weights and eviction csrc/evict.hip) and the host
+planner (csrc/plan.cpp), the sources side by side, and links them into a shared
+library next to this file.  One more
 builds libhbm_probe.so, the plain streaming-read kernel the benchmark measures
 the HBM read ceiling with (csrc/hbm_probe.hip; not part of the decode-attention
 boundary).  Packed-fp32 VALU instructions are disabled for
@@ -26,7 +28,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libdecode_attn.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
-SOURCES = [os.path.join(CSRC, f) for f in ("decode_attn.hip", "kv4.hip", "cache_ops.hip", "evict.hip", "prefix.hip", "plan.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("decode_attn.hip", "kv4.hip", "cache_ops.hip", "evict.hip", "prefix.hip",
+                                           "plan.cpp")]
 PROBE_NAME = "libhbm_probe.so"
 PROBE_PATH = os.path.join(HERE, PROBE_NAME)
 PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]

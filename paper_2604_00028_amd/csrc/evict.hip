@@ -49,7 +49,7 @@ struct WeightParams {
 // score; in 32 bits throughout.  Up to 16 NT heads stay in registers; more (g >
 // 64) are read anew for each tile.  AUX: the loads' cache policy (2: streaming).
 //
-// Bound by HBM: 32 sequences of 8192 keys of 8 heads (516 MB of K, 34 of
+// Bound by HBM: 32 sequences of 8192 keys of 8 heads (535 MB of K, 17 of
 // weights) 95 us, 5.8 TB/s; K straight into the operand layout 112.
 template <int NT, int AUX>
 __global__ void __launch_bounds__(64 * kWeightWaves) weights_kernel(WeightParams p) {
