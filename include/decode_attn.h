@@ -779,10 +779,11 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
  *                *taken the first ones find no place.  The table keeps its
  *                entries; those behind the new length are stale
  *   budget >= 1, sinks, recent >= 0, sinks + recent <= budget
- *   workspace    >= da_evict_workspace_bytes(B, H_KV, L_K_max, budget); its last
- *                DA_ARRIVAL_BYTES are not touched, so the other calls' may be
- *                shared
- * Two launches.  Errors as for da_decode_attn_paged, and DA_ERR_ARG for budget,
+ *   workspace    >= da_evict_workspace_bytes(B, H_KV, L_K_max, budget), counters in
+ *                its last DA_ARRIVAL_BYTES zero before the first call, as for
+ *                da_decode_attn
+ * One launch where L_K_max is a few keys past the budget (or the budget a few),
+ * else two.  Errors as for da_decode_attn_paged, and DA_ERR_ARG for budget,
  * sinks and recent. */
 int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* seq_lens,
                 const int32_t* totals, const float* weights, const int32_t* positions, float* weights_out,

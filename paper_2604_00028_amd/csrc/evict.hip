@@ -176,6 +176,8 @@ constexpr int kCopies = 16;
 constexpr int kListed = kBins / 2;  // moves whose rows are listed in LDS, in the histogram's place
 constexpr int kMostKeys = 32768;    // keys that stay in LDS
 constexpr int kMoveRows = 64;  // rows a workgroup of move_kernel takes at a time
+constexpr int kFew = 8;        // evicted rows that are found one after the other
+constexpr int kMovedAtOnce = 64;  // moves of a (sequence, KV head) that select_kernel makes itself
 
 struct EvictParams {
   const int32_t* block_table;
@@ -191,7 +193,7 @@ struct EvictParams {
   int most;
   int B, H_KV, L_K, budget, sinks, recent, page_size, max_pages, num_pages;
   Div div_page, div_heads;
-  // move_kernel
+  // moves, lengths and pages
   uint16_t* k;
   uint16_t* v;
   int32_t* lens_out;
@@ -199,6 +201,7 @@ struct EvictParams {
   const int32_t* taken;
   int32_t* taken_out;   // nullable: pages are not given back
   int num_free;
+  uint32_t* arrivals;   // no second launch: the workgroups that have ended
   int groups;           // workgroups a (sequence, KV head)
   Div div_groups;
 };
@@ -232,6 +235,79 @@ __device__ __forceinline__ int2 scan_before(int x, int y, int2* sums, int2* tota
   return make_int2(sx - x + row_sum_before(s.x, wave), sy - y + row_sum_before(s.y, wave));
 }
 
+// The lengths after the eviction, and the pages that come free: sequences in order,
+// THREADS at a time, their pages past the budget by one scan, then a page a
+// thread, its sequence by bisection.  One workgroup, after all others have read
+// the lengths.
+template <int THREADS>
+__device__ __forceinline__ void give_back(const EvictParams& p) {
+  constexpr int WAVES = THREADS / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ int32_t wave_sum[WAVES];
+  __shared__ int32_t starts[THREADS];
+  const int first_page = (p.budget + p.page_size - 1) / p.page_size;
+  auto length = [&](int b) { return b < p.B ? max(0, min(p.seq_lens[b], p.L_K)) : 0; };
+  auto pages_gone = [&](int L) { return L > p.budget ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
+  int all = 0;
+  if (p.taken_out) {
+    for (int b = tid; b < p.B; b += THREADS) all += pages_gone(length(b));
+    all = __builtin_amdgcn_readlane(wave_scan(all), 63);
+    if (lane == 0) wave_sum[wave] = all;
+    __syncthreads();
+    all = 0;
+    for (int w = 0; w < WAVES; ++w) all += wave_sum[w];
+    __syncthreads();
+  }
+  const int taken = p.taken_out ? max(0, min(*p.taken, p.num_free)) : 0;
+  int at0 = taken - all;  // the place of the first page; the list has none for those below 0
+  for (int b0 = 0; b0 < p.B; b0 += THREADS) {
+    const int L = length(b0 + tid);
+    if (p.taken_out) {
+      const int n = pages_gone(L), upto = wave_scan(n);
+      if (lane == 63) wave_sum[wave] = upto;
+      __syncthreads();
+      int before = upto - n;
+      for (int w = 0; w < wave; ++w) before += wave_sum[w];
+      starts[tid] = before;
+      int sum = 0;
+      for (int w = 0; w < WAVES; ++w) sum += wave_sum[w];
+      __syncthreads();
+      for (int e = tid; e < sum; e += THREADS) {
+        int lo = 0, hi = THREADS;  // the last sequence that starts at or before e
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (starts[mid] <= e)
+            lo = mid;
+          else
+            hi = mid;
+        }
+        if (at0 + e >= 0)
+          p.free_pages[at0 + e] = p.block_table[(int64_t)(b0 + lo) * p.max_pages + first_page + (e - starts[lo])];
+      }
+      at0 += sum;
+      __syncthreads();
+    }
+    if (b0 + tid < p.B) p.lens_out[b0 + tid] = min(L, p.budget);
+  }
+  if (p.taken_out && tid == 0) *p.taken_out = max(0, taken - all);
+}
+
+// The least of a row of 16 lanes, for each of them.
+__device__ __forceinline__ uint64_t least_of_row(uint64_t x) {
+  auto step = [&](auto turn) {
+    constexpr int kTurn = 0x120 + decltype(turn)::value;  // row_ror
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, kTurn, 0xf, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), kTurn, 0xf, 0xf, false);
+    const uint64_t y = (uint64_t)hi << 32 | lo;
+    x = y < x ? y : x;
+  };
+  step(std::integral_constant<int, 8>{});
+  step(std::integral_constant<int, 4>{});
+  step(std::integral_constant<int, 2>{});
+  step(std::integral_constant<int, 1>{});
+  return x;
+}
+
 // The rows of one (sequence, KV head) that stay.  With more than `budget` rows,
 // those of the `budget` largest keys do, where a key is the row's weight (all
 // ones for a protected row), of equal ones the lowest rows.  The budget-th
@@ -251,13 +327,15 @@ __device__ __forceinline__ int2 scan_before(int x, int y, int2* sums, int2* tota
 // the first histogram 18.0, a third of it for the stores; eight of 16000 rows
 // 36.6, a third for that histogram).
 template <int THREADS, bool KEEP>
-__global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
+__device__ __forceinline__ void select_rows(const EvictParams& p) {
   constexpr int WAVES = THREADS / 64;
   static_assert(WAVES <= 16 && THREADS >= 256, "the waves' sums are scanned by 16 lanes; 256 threads have a first digit each");
   extern __shared__ uint32_t keys[];  // KEEP: [L_K]
   __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
   __shared__ int2 sums[5][WAVES];
   __shared__ uint32_t found[3][2];
+  __shared__ uint64_t lows[2][WAVES];
+  __shared__ int gone[kFew];
   __shared__ int ties;  // not all keys equal to the last that stays do
   const int tid = threadIdx.x, lane = tid & 63;
   const int unit = blockIdx.x, b = div_by(unit, p.div_heads);
@@ -268,7 +346,7 @@ __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
   int32_t* p_out = p.p_out + unit * p.stride;
   int32_t* moves = p.moves + unit * p.move_ints;
   if (L <= p.budget) {
-    if (tid == 0) moves[0] = 0;
+    if (tid == 0 && !p.arrivals) moves[0] = 0;
     if (w_in != w_out)
       for (int r = tid; r < L; r += THREADS) w_out[r] = w_in[r];
     if (p_in != p_out)
@@ -285,142 +363,191 @@ __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
     else
       return key_of(placed(r, p_in[r]), w_in[r]);
   };
-  for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
+  const int evicted = L - p.budget;
+  const bool few = evicted <= kFew;
+  if (!few) {
+    for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
+    __syncthreads();
+  }
+  // rows below the budget are written as if they stayed; what moves into the others follows
+  for (int r8 = tid; r8 < L; r8 += 8 * THREADS) {
+    float w[8];
+    int at[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = min(r8 + i * THREADS, L - 1);
+      w[i] = w_in[r];
+      at[i] = p_in[r];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r8 + i * THREADS;
+      if (r >= L) break;
+      const int pos = placed(r, at[i]);
+      const uint32_t k = key_of(pos, w[i]);
+      if constexpr (KEEP) keys[r] = k;
+      if (!few) atomicAdd(&hist[(k >> 24) * kCopies + (lane & (kCopies - 1))], 1u);
+      if (r < p.budget) {
+        if (w_in != w_out) w_out[r] = w[i];
+        if (at[i] < 0 || p_in != p_out) p_out[r] = pos;
+      }
+    }
+  }
   __syncthreads();
 
-  uint32_t prefix = 0, mask = 0;
-  uint32_t want = (uint32_t)p.budget;  // of the keys that share the prefix, the want-th largest is the last to stay
-  int2 all;
-#pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int low = pass == 0 ? 24 : pass == 1 ? 12 : 0;
-    if (pass == 0) {
-      // rows below the budget are written as if they stayed; what moves into the others follows
-      for (int r8 = tid; r8 < L; r8 += 8 * THREADS) {
-        float w[8];
-        int at[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = min(r8 + i * THREADS, L - 1);
-          w[i] = w_in[r];
-          at[i] = p_in[r];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = r8 + i * THREADS;
-          if (r >= L) break;
-          const int pos = placed(r, at[i]);
-          const uint32_t k = key_of(pos, w[i]);
-          if constexpr (KEEP) keys[r] = k;
-          atomicAdd(&hist[(k >> 24) * kCopies + (lane & (kCopies - 1))], 1u);
-          if (r < p.budget) {
-            if (w_in != w_out) w_out[r] = w[i];
-            if (at[i] < 0 || p_in != p_out) p_out[r] = pos;
-          }
-        }
-      }
-    } else {
-#pragma unroll 4
-      for (int r = tid; r < L; r += THREADS) {
-        const uint32_t k = key(r);
-        if ((k & mask) == prefix) atomicAdd(&hist[(k >> low) & (kBins - 1)], 1u);
-      }
-    }
-    __syncthreads();
-    // from the largest digit down: the first digit one a thread, the others kBins / THREADS
-    constexpr int PER = kBins / THREADS;
-    uint32_t c[PER], sum = 0;
-    if (pass == 0) {
-      if (tid < 256)
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-          const int at = (255 - tid) * kCopies + ((tid + i) & (kCopies - 1));
-          sum += hist[at];
-          hist[at] = 0;
-        }
-    } else {
-      u32x4* const mine = reinterpret_cast<u32x4*>(hist + kBins - PER * (tid + 1));
-#pragma unroll
-      for (int i = 0; i < PER / 4; ++i) {
-        const u32x4 x = mine[PER / 4 - 1 - i];
-        mine[PER / 4 - 1 - i] = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          c[4 * i + e] = x[3 - e];
-          sum += x[3 - e];
-        }
-      }
-    }
-    uint32_t before = (uint32_t)scan_before<WAVES>((int)sum, 0, sums[pass], &all).x;
-    if (before < want && want <= before + sum) {
-      int digit = 255 - tid;
-      if (pass > 0) {
-        digit = kBins - 1 - PER * tid;
-        sum = c[0];
-#pragma unroll
-        for (int i = 0; i < PER - 1; ++i)
-          if (kBins - 1 - PER * tid - i == digit && want > before + c[i]) {
-            before += c[i];
-            sum = c[i + 1];
-            --digit;
-          }
-      }
-      found[pass][0] = (uint32_t)digit;
-      found[pass][1] = want - before;
-      if (pass == 2) ties = sum != want - before;
-    }
-    __syncthreads();
-    prefix |= found[pass][0] << low;
-    mask |= (pass == 0 ? 255u : kBins - 1u) << low;
-    want = found[pass][1];
-  }
-
-  // the thread's rows: an odd number of them, so that the threads' keys lie in different banks
-  const int each = ((L + THREADS - 1) / THREADS) | 1;
-  const int r0 = (int)min((int64_t)tid * each, (int64_t)L), r1 = (int)min((int64_t)r0 + each, (int64_t)L);
-  int rank0 = 0;
-  if (ties) {
-    int equal = 0;
-#pragma unroll 4
-    for (int r = r0; r < r1; ++r) equal += key(r) == prefix;
-    rank0 = scan_before<WAVES>(equal, 0, sums[3], &all).x;
-  } else {
-    want = (uint32_t)L;  // a thread's rows are fewer
-  }
-  int rank = rank0, holes = 0, late = 0;
-#pragma unroll 4
-  for (int r = r0; r < r1; ++r) {
-    const uint32_t k = key(r);
-    const bool stays = k > prefix || (k == prefix && rank < (int)want);
-    rank += k == prefix;
-    holes += !stays && r < p.budget;
-    late += stays && r >= p.budget;
-  }
-  const int2 first = scan_before<WAVES>(holes, late, sums[4], &all);
-  const int count = min(all.x, p.most);
   // rows that move, listed within the sequence first
-  const bool in_lds = count <= kListed;
-  int32_t* to = in_lds ? reinterpret_cast<int32_t*>(hist) : moves + 1;
-  int32_t* from = in_lds ? to + kListed : moves + 1 + p.most;
-  if (holes + late > 0) {
-    rank = rank0;
-    int hole = first.x, mover = first.y;
+  int count;
+  int32_t* to = reinterpret_cast<int32_t*>(hist);
+  int32_t* from = to + kListed;
+  if (few) {
+    // One row after the other: the smallest key above the last one's, of equal ones the highest row.
+    uint64_t last = 0;  // key and the row's complement; a row has one above 0
+    for (int e = 0; e < evicted; ++e) {
+      uint64_t least = ~(uint64_t)0;
+      for (int r = tid; r < L; r += THREADS) {
+        const uint64_t x = (uint64_t)key(r) << 32 | (uint32_t)~r;
+        least = x > last && x < least ? x : least;
+      }
+      least = least_of_row(least);
+      {
+        const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)least, (uint32_t)least, false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(least >> 32), (uint32_t)(least >> 32), false, false);
+        least = std::min((uint64_t)hi[0] << 32 | lo[0], (uint64_t)hi[1] << 32 | lo[1]);
+      }
+      {
+        const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)least, (uint32_t)least, false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(least >> 32), (uint32_t)(least >> 32), false, false);
+        least = std::min((uint64_t)hi[0] << 32 | lo[0], (uint64_t)hi[1] << 32 | lo[1]);
+      }
+      if (lane == 0) lows[e & 1][tid >> 6] = least;
+      __syncthreads();
+      last = least_of_row(lows[e & 1][lane & (WAVES - 1)]);
+      if (tid == 0) gone[e] = (int)~(uint32_t)last;
+    }
+    __syncthreads();
+    // lane e: of the evicted rows the e-th found, and row budget + e
+    const int mine = lane < evicted ? gone[lane] : -1;
+    int hole = 0, before = 0;
+    bool stays = lane < evicted;
+    for (int e = 0; e < evicted; ++e) {
+      hole += gone[e] < mine;
+      stays = stays && gone[e] != p.budget + lane;
+    }
+    const uint64_t holes = __ballot(mine >= 0 && mine < p.budget), movers = __ballot(stays);
+    before = __builtin_popcountll(movers & (((uint64_t)1 << lane) - 1));
+    if (tid < 64 && mine >= 0 && mine < p.budget) to[hole] = mine;
+    if (tid < 64 && stays) from[before] = p.budget + lane;
+    count = __builtin_popcountll(holes);
+  } else {
+    uint32_t prefix = 0, mask = 0;
+    uint32_t want = (uint32_t)p.budget;  // of the keys that share the prefix, the want-th largest is the last to stay
+    int2 all;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int low = pass == 0 ? 24 : pass == 1 ? 12 : 0;
+      if (pass > 0) {
+#pragma unroll 4
+        for (int r = tid; r < L; r += THREADS) {
+          const uint32_t k = key(r);
+          if ((k & mask) == prefix) atomicAdd(&hist[(k >> low) & (kBins - 1)], 1u);
+        }
+        __syncthreads();
+      }
+      // from the largest digit down: the first digit one a thread, the others kBins / THREADS
+      constexpr int PER = kBins / THREADS;
+      uint32_t c[PER], sum = 0;
+      if (pass == 0) {
+        if (tid < 256)
+#pragma unroll
+          for (int i = 0; i < kCopies; ++i) {
+            const int at = (255 - tid) * kCopies + ((tid + i) & (kCopies - 1));
+            sum += hist[at];
+            hist[at] = 0;
+          }
+      } else {
+        u32x4* const mine = reinterpret_cast<u32x4*>(hist + kBins - PER * (tid + 1));
+#pragma unroll
+        for (int i = 0; i < PER / 4; ++i) {
+          const u32x4 x = mine[PER / 4 - 1 - i];
+          mine[PER / 4 - 1 - i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            c[4 * i + e] = x[3 - e];
+            sum += x[3 - e];
+          }
+        }
+      }
+      uint32_t before = (uint32_t)scan_before<WAVES>((int)sum, 0, sums[pass], &all).x;
+      if (before < want && want <= before + sum) {
+        int digit = 255 - tid;
+        if (pass > 0) {
+          digit = kBins - 1 - PER * tid;
+          sum = c[0];
+#pragma unroll
+          for (int i = 0; i < PER - 1; ++i)
+            if (kBins - 1 - PER * tid - i == digit && want > before + c[i]) {
+              before += c[i];
+              sum = c[i + 1];
+              --digit;
+            }
+        }
+        found[pass][0] = (uint32_t)digit;
+        found[pass][1] = want - before;
+        if (pass == 2) ties = sum != want - before;
+      }
+      __syncthreads();
+      prefix |= found[pass][0] << low;
+      mask |= (pass == 0 ? 255u : kBins - 1u) << low;
+      want = found[pass][1];
+    }
+
+    // the thread's rows: an odd number of them, so that the threads' keys lie in different banks
+    const int each = ((L + THREADS - 1) / THREADS) | 1;
+    const int r0 = (int)min((int64_t)tid * each, (int64_t)L), r1 = (int)min((int64_t)r0 + each, (int64_t)L);
+    int rank0 = 0;
+    if (ties) {
+      int equal = 0;
+#pragma unroll 4
+      for (int r = r0; r < r1; ++r) equal += key(r) == prefix;
+      rank0 = scan_before<WAVES>(equal, 0, sums[3], &all).x;
+    } else {
+      want = (uint32_t)L;  // a thread's rows are fewer
+    }
+    int rank = rank0, holes = 0, late = 0;
+#pragma unroll 4
     for (int r = r0; r < r1; ++r) {
       const uint32_t k = key(r);
       const bool stays = k > prefix || (k == prefix && rank < (int)want);
       rank += k == prefix;
-      if (r < p.budget && !stays) {
-        if (hole < count) to[hole] = r;
-        ++hole;
-      }
-      if (r >= p.budget && stays) {
-        if (mover < count) from[mover] = r;
-        ++mover;
+      holes += !stays && r < p.budget;
+      late += stays && r >= p.budget;
+    }
+    const int2 first = scan_before<WAVES>(holes, late, sums[4], &all);
+    count = min(all.x, p.most);
+    if (count > kListed) {
+      to = moves + 1;
+      from = moves + 1 + p.most;
+    }
+    if (holes + late > 0) {
+      rank = rank0;
+      int hole = first.x, mover = first.y;
+      for (int r = r0; r < r1; ++r) {
+        const uint32_t k = key(r);
+        const bool stays = k > prefix || (k == prefix && rank < (int)want);
+        rank += k == prefix;
+        if (r < p.budget && !stays) {
+          if (hole < count) to[hole] = r;
+          ++hole;
+        }
+        if (r >= p.budget && stays) {
+          if (mover < count) from[mover] = r;
+          ++mover;
+        }
       }
     }
   }
   __syncthreads();
-  if (tid == 0) moves[0] = count;
+  if (tid == 0 && !p.arrivals) moves[0] = count;
   auto pool_row = [&](int r) {
     const int j = div_by(r, p.div_page);
     const int page = p.block_table[(int64_t)b * p.max_pages + j];
@@ -430,8 +557,19 @@ __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
     const int d = to[i], s = from[i];
     w_out[d] = w_in[s];
     p_out[d] = placed(s, p_in[s]);
-    moves[1 + i] = pool_row(d);
-    moves[1 + p.most + i] = pool_row(s);
+    if (!p.arrivals) {
+      moves[1 + i] = pool_row(d);
+      moves[1 + p.most + i] = pool_row(s);
+    }
+  }
+  if (p.arrivals) {
+    for (int i = tid; i < 32 * count; i += THREADS) {  // 16 lanes a row of K, 16 of V
+      const int d = pool_row(to[i / 32]), s = pool_row(from[i / 32]);
+      uint16_t* const pool = (i & 16 ? p.v : p.k) + (int64_t)(unit - b * p.H_KV) * D + 8 * (i & 15);
+      u32x4 x = {0u, 0u, 0u, 0u};  // a page outside the pool reads as zeros
+      if (s >= 0) x = *reinterpret_cast<const u32x4*>(pool + (int64_t)s * p.H_KV * D);
+      if (d >= 0) *reinterpret_cast<u32x4*>(pool + (int64_t)d * p.H_KV * D) = x;
+    }
   }
   __syncthreads();
   for (int r = p.budget + tid; r < L; r += THREADS) {
@@ -440,12 +578,28 @@ __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
   }
 }
 
+// With `arrivals` the rows that move are few, and there is no second launch: each
+// workgroup moves its own, and the last one to end (nobody waits) does the rest.
+template <int THREADS, bool KEEP>
+__global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
+  select_rows<THREADS, KEEP>(p);
+  if (!p.arrivals) return;
+  __shared__ int last;
+  __syncthreads();  // every thread is done with the lengths
+  if (threadIdx.x == 0) {
+    last = __hip_atomic_fetch_add(p.arrivals, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    if (last) __hip_atomic_store(p.arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (last) give_back<THREADS>(p);
+}
+
 // The rows into their places, and (block 0) the lengths and the pages that come
 // free.  A head's row of K or V is 16 lanes of 16 bytes; a wave moves four rows
 // of both at a time.  Targets lie below the budget and sources above it, so no
 // move meets another.
 __global__ void __launch_bounds__(256) move_kernel(EvictParams p) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (blockIdx.x > 0) {
     const int blk = (int)blockIdx.x - 1;
     const int unit = div_by(blk, p.div_groups), part = blk - unit * p.groups;
@@ -479,53 +633,7 @@ __global__ void __launch_bounds__(256) move_kernel(EvictParams p) {
     }
     return;
   }
-  // Sequences in order, 256 at a time: their pages past the budget by one scan,
-  // then a page a thread, its sequence by bisection.
-  __shared__ int32_t wave_sum[4];
-  __shared__ int32_t starts[256];
-  const int first_page = (p.budget + p.page_size - 1) / p.page_size;
-  auto length = [&](int b) { return b < p.B ? max(0, min(p.seq_lens[b], p.L_K)) : 0; };
-  auto pages_gone = [&](int L) { return L > p.budget ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
-  int all = 0;
-  if (p.taken_out) {
-    for (int b = tid; b < p.B; b += 256) all += pages_gone(length(b));
-    all = __builtin_amdgcn_readlane(wave_scan(all), 63);
-    if (lane == 0) wave_sum[wave] = all;
-    __syncthreads();
-    all = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
-    __syncthreads();
-  }
-  const int taken = p.taken_out ? max(0, min(*p.taken, p.num_free)) : 0;
-  int at0 = taken - all;  // the place of the first page; the list has none for those below 0
-  for (int b0 = 0; b0 < p.B; b0 += 256) {
-    const int L = length(b0 + tid);
-    if (p.taken_out) {
-      const int n = pages_gone(L), upto = wave_scan(n);
-      if (lane == 63) wave_sum[wave] = upto;
-      __syncthreads();
-      int before = upto - n;
-      for (int w = 0; w < wave; ++w) before += wave_sum[w];
-      starts[tid] = before;
-      const int sum = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
-      __syncthreads();
-      for (int e = tid; e < sum; e += 256) {
-        int lo = 0, hi = 256;  // the last sequence that starts at or before e
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (starts[mid] <= e)
-            lo = mid;
-          else
-            hi = mid;
-        }
-        if (at0 + e >= 0)
-          p.free_pages[at0 + e] = p.block_table[(int64_t)(b0 + lo) * p.max_pages + first_page + (e - starts[lo])];
-      }
-      at0 += sum;
-      __syncthreads();
-    }
-    if (b0 + tid < p.B) p.lens_out[b0 + tid] = min(L, p.budget);
-  }
-  if (p.taken_out && tid == 0) *p.taken_out = max(0, taken - all);
+  give_back<256>(p);
 }
 
 // ---------------------------------------------------------------- host side
@@ -694,6 +802,9 @@ int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const 
   p.taken_out = taken_out;
   p.num_free = num_free;
   const int64_t units = (int64_t)B * H_KV;
+  // one launch where a sequence has few rows to move
+  if (p.most <= kMovedAtOnce)
+    p.arrivals = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + da::arrival_offset(workspace_bytes));
   void* args[] = {&p};
   const int threads = L_K_max <= 512 ? 256 : L_K_max <= 1024 ? 512 : 1024;
   const void* fn = threads == 256         ? reinterpret_cast<const void*>(&select_kernel<256, true>)
@@ -703,12 +814,12 @@ int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const 
   const int smem = L_K_max <= kMostKeys ? 4 * L_K_max : 0;
   hipStream_t s = static_cast<hipStream_t>(stream);
   rc = launched(hipLaunchKernel(fn, dim3((uint32_t)units), dim3(threads), args, smem, s), "select");
-  if (rc) return rc;
+  if (rc || p.arrivals) return rc;
   // eight workgroups a CU at most; a workgroup that finds nothing to move ends at once
   const int64_t parts = (p.most + kMoveRows - 1) / kMoveRows;
   p.groups = (int)std::max<int64_t>(1, std::min<int64_t>(parts, (8ll * cus + units - 1) / units));
   p.div_groups = make_div((uint32_t)p.groups);
-  const int64_t grid = 1 + (p.most ? units * p.groups : 0);
+  const int64_t grid = 1 + units * p.groups;
   return launched(hipLaunchKernel(reinterpret_cast<const void*>(&move_kernel), dim3((uint32_t)grid), dim3(256), args, 0, s),
                   "move");
 }

@@ -164,6 +164,47 @@ def test_weights_that_tie_or_are_not_numbers(kind):
     e.run(300, 3, 20, what=kind)
 
 
+@pytest.mark.parametrize("over", [1, 2, 7, 8, 9, 63, 64, 65])
+@pytest.mark.parametrize("kind", ["mixed", "alike", "nan", "late"])
+def test_a_few_rows_past_the_budget(over, kind):
+    """Rows found one after the other up to 8, moved by the first launch up to 64; sequences with fewer and without."""
+    n = 700
+    e = Evict([n + over, n + 1, n, n + (over + 1) // 2, 0, 5], 2, 32, seed=30 + over, settled=400)
+    if kind == "alike":
+        e.weights[...] = 0.25
+    elif kind == "nan":
+        e.weights[:, :, ::3] = np.nan
+        e.weights[:, :, 1::5] = np.inf
+    elif kind == "late":
+        e.weights[:, :, n:] = -1
+    e.run(n, 4, 0 if kind == "late" else 33, what=f"{over} past, {kind}")
+    e.run(n, 0, 0, in_place=False, what=f"{over} past, {kind}, nothing protected")
+
+
+@pytest.mark.parametrize("L", [300, 900, 5000, 32768, 32769, 40000])
+def test_a_few_rows_in_every_kernel_variant(L):
+    for over in (1, 8, 9, 64):
+        Evict([L, L - 1], 2, 64, seed=over, settled=100).run(L - over, 10, 50, over % 2 == 0, what=f"{over} of {L} rows")
+
+
+def test_many_sequences_in_one_launch():
+    rng = np.random.default_rng(31)
+    e = Evict([int(x) for x in rng.integers(90, 130, 1500)], 1, 32, seed=31)
+    for taken in (4700, 3):
+        e.taken = taken
+        e.run(96, 4, 16, what="1500 sequences")
+    e.run(1, 0, 1, what="a budget of one")
+
+
+def test_a_few_pages_outside_the_pool():
+    e = Evict([300, 299], 2, 32, seed=32)
+    e.weights[:, :, :290] = 1
+    e.weights[:, :, 40:44] = 0
+    e.weights[:, :, 260:] = 2
+    e.table[0, 1], e.table[1, 9] = -1, 10 ** 6  # a target, a source
+    e.run(296, what="pages outside")
+
+
 def test_a_free_list_with_few_pages_in_use_and_none():
     e = Evict([900, 400, 1000], 1, 32, seed=9)
     for taken in (0, 1, 5, 17, 5000):
@@ -280,6 +321,7 @@ def test_a_callers_workspace_and_stream():
     e = Evict([300, 120], 2, 32, seed=17)
     need = da.da_evict_workspace_bytes(2, 2, e.L, 100)
     ws = torch.full((need,), 3, dtype=torch.uint8, device="cuda")
+    ws[-(1 << 20):] = 0
     other = torch.cuda.Stream()
     torch.cuda.synchronize()
 
@@ -289,7 +331,8 @@ def test_a_callers_workspace_and_stream():
         other.synchronize()
         return got
 
-    e.run(100, 1, 2, what="own workspace", call=call)
-    assert (ws[-(1 << 20):] == 3).all()  # the other calls' counters
+    for budget in (100, 295, 20, 299):  # two launches, one, two, one
+        e.run(budget, 1, 2, what=f"own workspace, {budget}", call=call)
+        assert not ws[-(1 << 20):].any()
     with pytest.raises(da.DecodeAttnError):
         e.run(100, what="short workspace", call=lambda *a, **kw: da.da_evict_kv(*a, workspace=ws[:need - 256], **kw))
