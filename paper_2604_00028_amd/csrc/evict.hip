@@ -235,18 +235,22 @@ __device__ __forceinline__ int2 scan_before(int x, int y, int2* sums, int2* tota
   return make_int2(sx - x + row_sum_before(s.x, wave), sy - y + row_sum_before(s.y, wave));
 }
 
+__device__ __forceinline__ int length_of(const EvictParams& p, int b) {
+  return b < p.B ? max(0, min(p.seq_lens[b], p.L_K)) : 0;
+}
+
 // The lengths after the eviction, and the pages that come free: sequences in order,
 // THREADS at a time, their pages past the budget by one scan, then a page a
 // thread, its sequence by bisection.  One workgroup, after all others have read
-// the lengths.
+// the lengths; length0: that of sequence `thread`, in_use: pages of the list.
 template <int THREADS>
-__device__ __forceinline__ void give_back(const EvictParams& p) {
+__device__ __forceinline__ void give_back(const EvictParams& p, int length0, int in_use) {
   constexpr int WAVES = THREADS / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __shared__ int32_t wave_sum[WAVES];
   __shared__ int32_t starts[THREADS];
   const int first_page = (p.budget + p.page_size - 1) / p.page_size;
-  auto length = [&](int b) { return b < p.B ? max(0, min(p.seq_lens[b], p.L_K)) : 0; };
+  auto length = [&](int b) { return b < THREADS ? length0 : length_of(p, b); };
   auto pages_gone = [&](int L) { return L > p.budget ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
   int all = 0;
   if (p.taken_out) {
@@ -258,7 +262,7 @@ __device__ __forceinline__ void give_back(const EvictParams& p) {
     for (int w = 0; w < WAVES; ++w) all += wave_sum[w];
     __syncthreads();
   }
-  const int taken = p.taken_out ? max(0, min(*p.taken, p.num_free)) : 0;
+  const int taken = p.taken_out ? max(0, min(in_use, p.num_free)) : 0;
   int at0 = taken - all;  // the place of the first page; the list has none for those below 0
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int L = length(b0 + tid);
@@ -334,6 +338,7 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
   __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
   __shared__ int2 sums[5][WAVES];
   __shared__ uint32_t found[3][2];
+  __shared__ int32_t pages[KEEP ? kMostKeys / kKeysPerTile : 1];
   __shared__ uint64_t lows[2][WAVES];
   __shared__ int gone[kFew];
   __shared__ int ties;  // not all keys equal to the last that stays do
@@ -353,6 +358,33 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
       for (int r = tid; r < L; r += THREADS) p_out[r] = p_in[r];
     return;
   }
+  // the sequence's pages, for the way of rows at the end
+  if constexpr (KEEP)
+    for (int i = tid; i <= div_by(L - 1, p.div_page); i += THREADS) pages[i] = p.block_table[(int64_t)b * p.max_pages + i];
+  const int evicted = L - p.budget;
+  const bool few = evicted <= kFew, held = few && p.arrivals;
+  auto pool_row_of = [&](int r, const int32_t* table) {
+    const int j = div_by(r, p.div_page);
+    const int page = table[j];
+    return page >= 0 && page < p.num_pages ? page * p.page_size + (r - j * p.page_size) : -1;
+  };
+  // a sixteenth of a row of K or V: 16 lanes a row of K, 16 of V
+  const int64_t pitch = (int64_t)p.H_KV * D;
+  auto piece = [&](int i) { return (i & 16 ? p.v : p.k) + (int64_t)(unit - b * p.H_KV) * D + 8 * (i & 15); };
+  // the rows past the budget, if they are few, are there when it is known which of them stay
+  u32x4 held_row = {0u, 0u, 0u, 0u};  // a page outside the pool reads as zeros
+  float held_w = 0.f;
+  int held_at = 0;
+  if (held) {
+    if (tid < 32 * evicted) {
+      const int from = pool_row_of(p.budget + tid / 32, p.block_table + (int64_t)b * p.max_pages);
+      if (from >= 0) held_row = *reinterpret_cast<const u32x4*>(piece(tid) + from * pitch);
+    }
+    if (tid < evicted) {
+      held_w = w_in[p.budget + tid];
+      held_at = p_in[p.budget + tid];
+    }
+  }
   const int shift = (int)((uint32_t)total - (uint32_t)L);  // position of a row that no eviction has placed: row + shift
   auto placed = [&](int r, int at) { return at >= 0 ? at : (int)((uint32_t)r + (uint32_t)shift); };
   const int64_t newest = (int64_t)total - p.recent;
@@ -363,8 +395,6 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
     else
       return key_of(placed(r, p_in[r]), w_in[r]);
   };
-  const int evicted = L - p.budget;
-  const bool few = evicted <= kFew;
   if (!few) {
     for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
     __syncthreads();
@@ -396,7 +426,7 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
   __syncthreads();
 
   // rows that move, listed within the sequence first
-  int count;
+  int count, mover = -1;  // mover: this thread's row past the budget is the one that moves into the mover-th hole
   int32_t* to = reinterpret_cast<int32_t*>(hist);
   int32_t* from = to + kListed;
   if (few) {
@@ -427,16 +457,18 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
     __syncthreads();
     // lane e: of the evicted rows the e-th found, and row budget + e
     const int mine = lane < evicted ? gone[lane] : -1;
-    int hole = 0, before = 0;
+    int hole = 0;
     bool stays = lane < evicted;
     for (int e = 0; e < evicted; ++e) {
       hole += gone[e] < mine;
       stays = stays && gone[e] != p.budget + lane;
     }
     const uint64_t holes = __ballot(mine >= 0 && mine < p.budget), movers = __ballot(stays);
-    before = __builtin_popcountll(movers & (((uint64_t)1 << lane) - 1));
     if (tid < 64 && mine >= 0 && mine < p.budget) to[hole] = mine;
-    if (tid < 64 && stays) from[before] = p.budget + lane;
+    if (tid < 64 && stays) {
+      mover = __builtin_popcountll(movers & (((uint64_t)1 << lane) - 1));
+      from[mover] = p.budget + lane;
+    }
     count = __builtin_popcountll(holes);
   } else {
     uint32_t prefix = 0, mask = 0;
@@ -530,7 +562,7 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
     }
     if (holes + late > 0) {
       rank = rank0;
-      int hole = first.x, mover = first.y;
+      int hole = first.x, late_row = first.y;
       for (int r = r0; r < r1; ++r) {
         const uint32_t k = key(r);
         const bool stays = k > prefix || (k == prefix && rank < (int)want);
@@ -540,8 +572,8 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
           ++hole;
         }
         if (r >= p.budget && stays) {
-          if (mover < count) from[mover] = r;
-          ++mover;
+          if (late_row < count) from[late_row] = r;
+          ++late_row;
         }
       }
     }
@@ -549,10 +581,24 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
   __syncthreads();
   if (tid == 0 && !p.arrivals) moves[0] = count;
   auto pool_row = [&](int r) {
-    const int j = div_by(r, p.div_page);
-    const int page = p.block_table[(int64_t)b * p.max_pages + j];
-    return page >= 0 && page < p.num_pages ? page * p.page_size + (r - j * p.page_size) : -1;
+    if constexpr (KEEP)
+      return pool_row_of(r, pages);
+    else
+      return pool_row_of(r, p.block_table + (int64_t)b * p.max_pages);
   };
+  if (held) {
+    if (mover >= 0) {
+      const int d = to[mover];
+      w_out[d] = held_w;
+      p_out[d] = placed(p.budget + tid, held_at);
+    }
+    for (int i = 0; i < count; ++i) {
+      if (tid / 32 != from[i] - p.budget) continue;
+      const int d = pool_row(to[i]);
+      if (d >= 0) *reinterpret_cast<u32x4*>(piece(tid) + d * pitch) = held_row;
+    }
+    count = 0;  // done
+  }
   for (int i = tid; i < count; i += THREADS) {
     const int d = to[i], s = from[i];
     w_out[d] = w_in[s];
@@ -563,12 +609,11 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
     }
   }
   if (p.arrivals) {
-    for (int i = tid; i < 32 * count; i += THREADS) {  // 16 lanes a row of K, 16 of V
+    for (int i = tid; i < 32 * count; i += THREADS) {
       const int d = pool_row(to[i / 32]), s = pool_row(from[i / 32]);
-      uint16_t* const pool = (i & 16 ? p.v : p.k) + (int64_t)(unit - b * p.H_KV) * D + 8 * (i & 15);
-      u32x4 x = {0u, 0u, 0u, 0u};  // a page outside the pool reads as zeros
-      if (s >= 0) x = *reinterpret_cast<const u32x4*>(pool + (int64_t)s * p.H_KV * D);
-      if (d >= 0) *reinterpret_cast<u32x4*>(pool + (int64_t)d * p.H_KV * D) = x;
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (s >= 0) x = *reinterpret_cast<const u32x4*>(piece(i) + s * pitch);
+      if (d >= 0) *reinterpret_cast<u32x4*>(piece(i) + d * pitch) = x;
     }
   }
   __syncthreads();
@@ -582,6 +627,11 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
 // workgroup moves its own, and the last one to end (nobody waits) does the rest.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
+  int length0 = 0, in_use = 0;
+  if (p.arrivals) {  // there when the last workgroup needs them
+    length0 = length_of(p, threadIdx.x);
+    if (p.taken_out) in_use = *p.taken;
+  }
   select_rows<THREADS, KEEP>(p);
   if (!p.arrivals) return;
   __shared__ int last;
@@ -591,7 +641,7 @@ __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
     if (last) __hip_atomic_store(p.arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  if (last) give_back<THREADS>(p);
+  if (last) give_back<THREADS>(p, length0, in_use);
 }
 
 // The rows into their places, and (block 0) the lengths and the pages that come
@@ -633,7 +683,7 @@ __global__ void __launch_bounds__(256) move_kernel(EvictParams p) {
     }
     return;
   }
-  give_back<256>(p);
+  give_back<256>(p, length_of(p, threadIdx.x), p.taken_out ? *p.taken : 0);
 }
 
 // ---------------------------------------------------------------- host side
