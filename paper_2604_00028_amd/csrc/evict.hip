@@ -177,6 +177,7 @@ constexpr int kListed = kBins / 2;  // moves whose rows are listed in LDS, in th
 constexpr int kMostKeys = 32768;    // keys that stay in LDS
 constexpr int kMoveRows = 64;  // rows a workgroup of move_kernel takes at a time
 constexpr int kFew = 8;        // evicted rows that are found one after the other
+constexpr uint32_t kGates = 16;   // counters of workgroups that have ended
 constexpr int kMovedAtOnce = 64;  // moves of a (sequence, KV head) that select_kernel makes itself
 
 struct EvictParams {
@@ -246,37 +247,28 @@ __device__ __forceinline__ int length_of(const EvictParams& p, int b) {
 template <int THREADS>
 __device__ __forceinline__ void give_back(const EvictParams& p, int length0, int in_use) {
   constexpr int WAVES = THREADS / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  __shared__ int32_t wave_sum[WAVES];
+  const int tid = threadIdx.x;
+  __shared__ int2 sums[2][WAVES];
   __shared__ int32_t starts[THREADS];
   const int first_page = (p.budget + p.page_size - 1) / p.page_size;
   auto length = [&](int b) { return b < THREADS ? length0 : length_of(p, b); };
   auto pages_gone = [&](int L) { return L > p.budget ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
-  int all = 0;
-  if (p.taken_out) {
-    for (int b = tid; b < p.B; b += THREADS) all += pages_gone(length(b));
-    all = __builtin_amdgcn_readlane(wave_scan(all), 63);
-    if (lane == 0) wave_sum[wave] = all;
-    __syncthreads();
-    all = 0;
-    for (int w = 0; w < WAVES; ++w) all += wave_sum[w];
-    __syncthreads();
-  }
   const int taken = p.taken_out ? max(0, min(in_use, p.num_free)) : 0;
-  int at0 = taken - all;  // the place of the first page; the list has none for those below 0
+  int2 sum;
+  int all = 0, done = 0;  // pages of all sequences, and of those before b0
+  if (p.taken_out && p.B > THREADS) {
+    for (int b = tid; b < p.B; b += THREADS) all += pages_gone(length(b));
+    scan_before<WAVES>(all, 0, sums[0], &sum);
+    all = sum.x;
+  }
   for (int b0 = 0; b0 < p.B; b0 += THREADS) {
     const int L = length(b0 + tid);
     if (p.taken_out) {
-      const int n = pages_gone(L), upto = wave_scan(n);
-      if (lane == 63) wave_sum[wave] = upto;
+      starts[tid] = scan_before<WAVES>(pages_gone(L), 0, sums[1], &sum).x;
+      if (p.B <= THREADS) all = sum.x;
+      const int at0 = taken - all + done;  // the place of the first page; the list has none for those below 0
       __syncthreads();
-      int before = upto - n;
-      for (int w = 0; w < wave; ++w) before += wave_sum[w];
-      starts[tid] = before;
-      int sum = 0;
-      for (int w = 0; w < WAVES; ++w) sum += wave_sum[w];
-      __syncthreads();
-      for (int e = tid; e < sum; e += THREADS) {
+      for (int e = tid; e < sum.x; e += THREADS) {
         int lo = 0, hi = THREADS;  // the last sequence that starts at or before e
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
@@ -288,7 +280,7 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int length0, int
         if (at0 + e >= 0)
           p.free_pages[at0 + e] = p.block_table[(int64_t)(b0 + lo) * p.max_pages + first_page + (e - starts[lo])];
       }
-      at0 += sum;
+      done += sum.x;
       __syncthreads();
     }
     if (b0 + tid < p.B) p.lens_out[b0 + tid] = min(L, p.budget);
@@ -637,8 +629,16 @@ __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
   __shared__ int last;
   __syncthreads();  // every thread is done with the lengths
   if (threadIdx.x == 0) {
-    last = __hip_atomic_fetch_add(p.arrivals, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    if (last) __hip_atomic_store(p.arrivals, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // the last at one of kGates counters goes on to the one of all: additions to one address go one after the other (256
+    // workgroups at one 2.9 us)
+    auto last_at = [](uint32_t* counter, uint32_t members) {
+      const bool is = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == members - 1;
+      if (is) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      return is;
+    };
+    const uint32_t gate = blockIdx.x % kGates;
+    last = last_at(p.arrivals + (1 + gate) * da::kArrivalStride, (gridDim.x - gate + kGates - 1) / kGates) &&
+           last_at(p.arrivals, min(gridDim.x, kGates));
   }
   __syncthreads();
   if (last) give_back<THREADS>(p, length0, in_use);
