@@ -176,7 +176,7 @@ constexpr int kCopies = 16;
 constexpr int kListed = kBins / 2;  // moves whose rows are listed in LDS, in the histogram's place
 constexpr int kMostKeys = 32768;    // keys that stay in LDS
 constexpr int kMoveRows = 64;  // rows a workgroup of move_kernel takes at a time
-constexpr int kFew = 8;        // evicted rows that are found one after the other
+constexpr int kFew = 5;        // evicted rows that are found one after the other
 constexpr uint32_t kGates = 16;   // counters of workgroups that have ended
 constexpr int kMovedAtOnce = 64;  // moves of a (sequence, KV head) that select_kernel makes itself
 
@@ -316,15 +316,23 @@ __device__ __forceinline__ uint64_t least_of_row(uint64_t x) {
 // (holes) and the kept ones above it: the i-th of these moves into the i-th
 // hole, in place and without an order among the moves.
 //
+// Up to kFew evicted rows, as where every step of a decode brings one, are found
+// one after the other as the smallest key left, 1 us each where the histograms
+// take 6; they lie within the kernel's reach, so what stays of the rows past the
+// budget is loaded before the choice.
+//
 // Bound by latency: one pass over weights and positions, coalesced, whose keys
-// stay in LDS (KEEP; longer sequences read both anew for each step), about ten
-// barriers, two lookups a move (32 sequences of 8 heads one key past 4096: 12.1
-// us; with the rows in registers, loaded and stored `each` apart, and one copy of
-// the first histogram 18.0, a third of it for the stores; eight of 16000 rows
-// 36.6, a third for that histogram).
+// stay in LDS (KEEP; longer sequences read both anew for each step), two lookups
+// a move.  32 sequences of 8 heads one key past 4096, in a graph: 8.8 us with all
+// that follows (an empty kernel 2.5, the pass over the keys 2.6, the choice 1.3,
+// the moves 0.8, the last workgroup's part the rest); eight past it 13.8 (about
+// ten barriers).  With a thread's rows in registers, loaded and stored `each`
+// apart, and one copy of the first histogram the choice by histograms took half as
+// long again.
 template <int THREADS, bool KEEP>
 __device__ __forceinline__ void select_rows(const EvictParams& p) {
   constexpr int WAVES = THREADS / 64;
+  static_assert(32 * kFew <= THREADS, "32 threads hold a row past the budget");
   static_assert(WAVES <= 16 && THREADS >= 256, "the waves' sums are scanned by 16 lanes; 256 threads have a first digit each");
   extern __shared__ uint32_t keys[];  // KEEP: [L_K]
   __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
@@ -617,6 +625,8 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
 
 // With `arrivals` the rows that move are few, and there is no second launch: each
 // workgroup moves its own, and the last one to end (nobody waits) does the rest.
+// 256 sequences and heads with 64 rows past the budget 16.4 us in a graph, with a
+// second launch 17.0; with 128 19.5 both; with 256 25.1 and 24.7.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
   int length0 = 0, in_use = 0;

@@ -164,10 +164,10 @@ def test_weights_that_tie_or_are_not_numbers(kind):
     e.run(300, 3, 20, what=kind)
 
 
-@pytest.mark.parametrize("over", [1, 2, 7, 8, 9, 63, 64, 65])
+@pytest.mark.parametrize("over", [1, 2, 4, 5, 6, 7, 63, 64, 65])
 @pytest.mark.parametrize("kind", ["mixed", "alike", "nan", "late"])
 def test_a_few_rows_past_the_budget(over, kind):
-    """Rows found one after the other up to 8, moved by the first launch up to 64; sequences with fewer and without."""
+    """Rows found one after the other up to 5, moved by the first launch up to 64; sequences with fewer and without."""
     n = 700
     e = Evict([n + over, n + 1, n, n + (over + 1) // 2, 0, 5], 2, 32, seed=30 + over, settled=400)
     if kind == "alike":
@@ -183,7 +183,7 @@ def test_a_few_rows_past_the_budget(over, kind):
 
 @pytest.mark.parametrize("L", [300, 900, 5000, 32768, 32769, 40000])
 def test_a_few_rows_in_every_kernel_variant(L):
-    for over in (1, 8, 9, 64):
+    for over in (1, 5, 6, 64):
         Evict([L, L - 1], 2, 64, seed=over, settled=100).run(L - over, 10, 50, over % 2 == 0, what=f"{over} of {L} rows")
 
 
