@@ -696,11 +696,12 @@ size_t da_kv4_workspace_bytes(int B, int H_Q, int H_KV, int L_K_max, int64_t poo
  *   chunk_keys   0: chosen.  A batch that holds few keys (B L_K_max of at most 384
  *                MiB of K and V, 768 for more than 16 heads a KV head) is not worth
  *                sharing: it takes the launch of da_decode_attn_window with nothing
- *                hidden, if da_prefix_workspace_bytes holds its states.  Others are cut into chunks of lengths chosen on the device
- *                by the batch's lengths and groups.  Negative: the latter whatever
- *                the size.  Positive: chunks of that many keys, in whole tiles of 32
- *                (at most 64 chunks of a prefix or of a sequence's own keys, and
- *                longer ones where the workspace holds no more)
+ *                hidden, if da_prefix_workspace_bytes holds its states.  Others are
+ *                cut into chunks of lengths chosen on the device by the batch's
+ *                lengths and groups.  Negative: the latter whatever the size.
+ *                Positive: chunks of that many keys, in whole tiles of 32 (at most 64
+ *                chunks of a prefix or of a sequence's own keys, and longer ones
+ *                where the workspace holds no more)
  *   workspace    >= da_prefix_workspace_bytes(B, G, H_Q, H_KV, 0), counters in its
  *                last DA_ARRIVAL_BYTES zero before the first call, as for
  *                da_decode_attn

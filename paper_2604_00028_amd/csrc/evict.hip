@@ -318,8 +318,7 @@ __device__ __forceinline__ uint64_t least_of_row(uint64_t x) {
 //
 // Up to kFew evicted rows, as where every step of a decode brings one, are found
 // one after the other as the smallest key left, 1 us each where the histograms
-// take 6; they lie within the kernel's reach, so what stays of the rows past the
-// budget is loaded before the choice.
+// take 6, and the rows past the budget are loaded before it is known which stay.
 //
 // Bound by latency: one pass over weights and positions, coalesced, whose keys
 // stay in LDS (KEEP; longer sequences read both anew for each step), two lookups

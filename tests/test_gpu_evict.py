@@ -336,3 +336,24 @@ def test_a_callers_workspace_and_stream():
         assert not ws[-(1 << 20):].any()
     with pytest.raises(da.DecodeAttnError):
         e.run(100, what="short workspace", call=lambda *a, **kw: da.da_evict_kv(*a, workspace=ws[:need - 256], **kw))
+
+
+def test_two_streams_at_once():
+    """Each stream has its own counters; one launch a call, of many workgroups."""
+    ints = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    streams, state = [torch.cuda.Stream() for _ in range(2)], []
+    e = Evict([900 + b % 7 for b in range(60)], 8, 32, seed=33)
+    for _ in range(6):
+        state.append(dict(k=to_dev(e.k), v=to_dev(e.v), lens=e.seq_lens(), w=ints(e.weights), p=ints(e.positions),
+                          free=ints(e.free), taken=ints(np.array([e.taken], np.int32))))
+    table, totals = ints(e.table), ints(e.totals)
+    torch.cuda.synchronize()
+    say("evict on two streams")
+    for i, s in enumerate(state):
+        da.da_evict_kv(s["k"], s["v"], table, s["lens"], totals, s["w"], s["p"], 899, e.L, sinks=4, recent=40,
+                       free_pages=s["free"], taken=s["taken"], stream=streams[i % 2])
+    torch.cuda.synchronize()
+    s = state[0]
+    e.check((s["lens"], s["w"], s["p"], s["taken"]), (s["k"], s["v"], s["free"]), 899, 4, 40, True, True, "two streams")
+    for other in state[1:]:
+        assert all(torch.equal(other[name].view(torch.uint8), s[name].view(torch.uint8)) for name in s)

@@ -301,6 +301,17 @@ def test_same_as_the_paged_call_without_groups():
     assert torch.allclose(a, b, rtol=0, atol=2.0 ** -12)
 
 
+def test_no_keys_at_all():
+    Groups([(3, 0), (1, 0)], [None], 16, 2, 32, seed=27).check("no keys")
+    g = Groups([(3, 64)], [5], 16, 2, 32, seed=28)
+    for chunk in (-1, 0, 32):
+        say(f"prefix without a bound {chunk}")
+        lse = g.lse()
+        out = g.call(lse, L=0, chunk_keys=chunk)
+        torch.cuda.synchronize()
+        assert not out.any() and torch.isneginf(lse).all()
+
+
 @pytest.mark.parametrize("chunk", [-1, 0])
 def test_captured_replays_follow_lengths_and_groups(chunk):
     g = Groups([(9, 640), (3, 100)], [100], 16, 2, 32, seed=20)
