@@ -756,11 +756,15 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
  * the i-th; no other row of the pool is written.  Decode attention does not
  * depend on the order of a sequence's keys (a window over them does), and keys
  * carry their rotation with them.
- *   block_table, seq_lens, page_size, max_pages, num_pages, L_K_max  as for
+ *   block_table, seq_lens, page_size, max_pages, num_pages  as for
  *                da_decode_attn_paged; num_pages * page_size < 2^31, B <=
  *                DA_MAX_REQUESTS.  A sequence's rows below `sinks` stay where
  *                they are, so sequences may share pages that hold only such
  *                rows (a common prompt), and no others
+ *   L_K_max      max_pages * page_size at most.  A sequence of more keys stays as
+ *                it is, its length, rows, weights, positions and pages, whatever
+ *                the budget (one whose totals are L_K_max or less has no more
+ *                keys than L_K_max)
  *   totals       int32 [B]: tokens the sequence has had, evicted ones included:
  *                the position of its next token
  *   weights      fp32 [B, H_KV, weight_stride], weight_stride >= L_K_max
@@ -771,7 +775,8 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
  *   weights_out, positions_out  the same after the moves (0 and -1 in rows [budget,
  *                seq_lens), other rows past the sequence not written); may be
  *                weights and positions
- *   lens_out     int32 [B]: min(seq_lens, budget); may be seq_lens
+ *   lens_out     int32 [B]: min(seq_lens, budget), or seq_lens where that is more
+ *                than L_K_max; may be seq_lens
  *   free_pages, taken, taken_out, num_free  NULL, or da_extend_tables's list of
  *                free pages [num_free], of which *taken are in use: the pages
  *                that hold rows at `budget` and beyond only, in order of

@@ -193,14 +193,15 @@ def key_weights(q, ks, lse, old, decay, scale=None):
     return out, tol
 
 
-def evict(lens, totals, weights, positions, table, page, budget, sinks, recent, free_pages=None, taken=0):
+def evict(lens, totals, weights, positions, table, page, budget, sinks, recent, free_pages=None, taken=0, bound=None):
     """(lens, weights, positions, moves, free_pages, taken) after the step; moves: (sequence, head, target row, source
-    row) with rows counted within the sequence."""
+    row) with rows counted within the sequence.  A sequence longer than `bound` stays as it is."""
     weights, positions = weights.copy(), positions.copy()
     out, moves, back = [], [], []
     for b, L in enumerate(lens):
-        out.append(min(L, budget))
-        if L <= budget:
+        past = bound is not None and L > bound
+        out.append(L if past else min(L, budget))
+        if past or L <= budget:
             continue
         back += [int(x) for x in table[b, -(-budget // page):-(-L // page)]]
         for h in range(weights.shape[1]):

@@ -1268,7 +1268,8 @@ def da_evict_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch
     taken_out), which are seq_lens, weights, positions and taken where none are
     passed.  totals int32 [B]: tokens each sequence has had; weights fp32 and
     positions int32 [B, H_KV, at least L_K_max] (-1: where no eviction has placed
-    the row); free_pages and taken: da_extend_tables's, to which pages go back."""
+    the row); free_pages and taken: da_extend_tables's, to which pages go back.  A
+    sequence of more than L_K_max keys stays as it is."""
     dev = k_cache.device
     if not k_cache.is_cuda:
         raise ValueError("k_cache must be on the GPU")

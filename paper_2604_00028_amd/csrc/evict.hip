@@ -236,8 +236,14 @@ __device__ __forceinline__ int2 scan_before(int x, int y, int2* sums, int2* tota
   return make_int2(sx - x + row_sum_before(s.x, wave), sy - y + row_sum_before(s.y, wave));
 }
 
+// Keys of sequence b.  Where they are more than L_K, the rows past them may have no
+// weights (whose stride need only hold L_K) and the sequence stays as it is: cut to
+// L_K rows it would take later tokens' positions for its first ones, and lose the
+// pages behind.  One that has had no more than L_K tokens holds no more keys.
 __device__ __forceinline__ int length_of(const EvictParams& p, int b) {
-  return b < p.B ? max(0, min(p.seq_lens[b], p.L_K)) : 0;
+  if (b >= p.B) return 0;
+  const int L = max(0, p.seq_lens[b]);
+  return L > p.L_K && p.totals[b] <= p.L_K ? p.L_K : L;
 }
 
 // The lengths after the eviction, and the pages that come free: sequences in order,
@@ -252,7 +258,7 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int length0, int
   __shared__ int32_t starts[THREADS];
   const int first_page = (p.budget + p.page_size - 1) / p.page_size;
   auto length = [&](int b) { return b < THREADS ? length0 : length_of(p, b); };
-  auto pages_gone = [&](int L) { return L > p.budget ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
+  auto pages_gone = [&](int L) { return L > p.budget && L <= p.L_K ? div_by(L - 1, p.div_page) + 1 - first_page : 0; };
   const int taken = p.taken_out ? max(0, min(in_use, p.num_free)) : 0;
   int2 sum;
   int all = 0, done = 0;  // pages of all sequences, and of those before b0
@@ -283,7 +289,7 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int length0, int
       done += sum.x;
       __syncthreads();
     }
-    if (b0 + tid < p.B) p.lens_out[b0 + tid] = min(L, p.budget);
+    if (b0 + tid < p.B) p.lens_out[b0 + tid] = L > p.L_K ? L : min(L, p.budget);
   }
   if (p.taken_out && tid == 0) *p.taken_out = max(0, taken - all);
 }
@@ -343,18 +349,19 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
   __shared__ int ties;  // not all keys equal to the last that stays do
   const int tid = threadIdx.x, lane = tid & 63;
   const int unit = blockIdx.x, b = div_by(unit, p.div_heads);
-  const int L = max(0, min(p.seq_lens[b], p.L_K)), total = p.totals[b];
+  const int L = length_of(p, b), total = p.totals[b];
   const float* w_in = p.w_in + unit * p.stride;
   const int32_t* p_in = p.p_in + unit * p.stride;
   float* w_out = p.w_out + unit * p.stride;
   int32_t* p_out = p.p_out + unit * p.stride;
   int32_t* moves = p.moves + unit * p.move_ints;
-  if (L <= p.budget) {
+  if (L <= p.budget || L > p.L_K) {
+    const int rows = (int)min((int64_t)L, p.stride);
     if (tid == 0 && !p.arrivals) moves[0] = 0;
     if (w_in != w_out)
-      for (int r = tid; r < L; r += THREADS) w_out[r] = w_in[r];
+      for (int r = tid; r < rows; r += THREADS) w_out[r] = w_in[r];
     if (p_in != p_out)
-      for (int r = tid; r < L; r += THREADS) p_out[r] = p_in[r];
+      for (int r = tid; r < rows; r += THREADS) p_out[r] = p_in[r];
     return;
   }
   // the sequence's pages, for the way of rows at the end

@@ -138,6 +138,58 @@ def test_bounds_other_than_the_longest():
     e.check((*got[:3], None), (k, v, ints(e.free)), 100, 0, 0, True, False, "cut")
 
 
+@pytest.mark.parametrize("budget", [100, 252, 300])
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("captured", [False, True])
+def test_sequences_past_the_bound_stay_as_they_are(budget, in_place, captured):
+    """Lengths above L_K_max, below, at and above the budget: two launches, one, and nothing to evict within the
+    bound.  Sequences 0 and 2 share the page of their sinks."""
+    L, sinks, recent = 256, 32, 10
+    e = Evict([700, 257, 256, 60, 200, 290], 2, 32, seed=34, settled=40)
+    e.positions[0] = -1  # never evicted: row 0 is token 0
+    e.totals[0] = 700
+    e.positions[2, :, :32] = np.arange(32)
+    e.positions[2, :, 32:40] = [33, 40, 50, 60, 70, 80, 90, 100]
+    e.table[2, 0] = e.table[0, 0]
+    ints = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    k, v, lens, w, p, f = to_dev(e.k), to_dev(e.v), e.seq_lens(), ints(e.weights), ints(e.positions), ints(e.free)
+    taken, table, totals = ints(np.array([e.taken], np.int32)), ints(e.table), ints(e.totals)
+    outs = {}
+    if not in_place:
+        outs = dict(lens_out=torch.full_like(lens, 9), weights_out=torch.full_like(w, 9),
+                    positions_out=torch.full_like(p, 9), taken_out=torch.full_like(taken, 9))
+    call = lambda: da.da_evict_kv(k, v, table, lens, totals, w, p, budget, L, sinks=sinks, recent=recent,  # noqa: E731
+                                  free_pages=f, taken=taken, **outs)
+    say(f"evict past the bound, budget {budget} in place {in_place} captured {captured}")
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        graph.replay()
+    else:
+        got = call()
+    torch.cuda.synchronize()
+    want, ww, wp, moves, wf, left = evict(e.lengths, e.totals, e.weights, e.positions, e.table, 32, budget, sinks, recent,
+                                          e.free, e.taken, bound=L)
+    assert want.tolist() == [n if n > L else min(n, budget) for n in e.lengths]
+    assert np.array_equal(got[0].cpu().numpy(), want) and got[3].item() == left
+    assert np.array_equal(f.cpu().numpy(), wf)
+    gw, gp = got[1].cpu().numpy(), got[2].cpu().numpy()
+    for b, n in enumerate(e.lengths):
+        assert np.array_equal(gp[b, :, :n], wp[b, :, :n]), f"positions of {b}"
+        assert np.array_equal(gw[b, :, :n], ww[b, :, :n]), f"weights of {b}"
+        rest = (e.weights[b, :, n:], e.positions[b, :, n:]) if in_place else (9, 9)
+        assert (gw[b, :, n:] == rest[0]).all() and (gp[b, :, n:] == rest[1]).all()
+    rows = e.k.shape[0] * 32
+    for x, was in ((k, e.k), (v, e.v)):
+        src = was.reshape(rows, 2, 128)
+        y = src.copy()
+        for b, h, d, s in moves:
+            assert e.lengths[b] <= L
+            y[e.pool_row(b, d), h] = src[e.pool_row(b, s), h]
+        assert np.array_equal(bits(x).reshape(y.shape), y), "rows of the cache"
+
+
 @pytest.mark.parametrize("kind", ["zeros", "one", "signs", "infinite", "nan", "all nan", "tiny", "negative"])
 def test_weights_that_tie_or_are_not_numbers(kind):
     e = Evict([700, 1200], 2, 32, seed=7)
