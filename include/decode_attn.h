@@ -240,7 +240,8 @@ int da_split_bounds(int L, int num_splits, int32_t* cuts);
  *                cu[0] = 0, non-decreasing, each length <= L_K_max
  *   out          bf16 [B, H_Q, d], normalised output
  *   lse_out      NULL or fp32 [B, H_Q]: natural-log log-sum-exp of the
- *                scaled scores (-inf for an empty sequence, whose O is 0)
+ *                scaled scores (-inf for an empty sequence, whose O is 0; a key
+ *                whose score is -inf counts as none)
  *   softmax_scale <= 0 selects 1/sqrt(d)
  *   num_splits   <= 0: chosen by da_choose_splits (policy MI355X); else 1..64
  *   pack_gqa     -1: chosen by the policy; 0, 1 or 2 forced (da_plan)

@@ -506,7 +506,7 @@ __device__ __forceinline__ void stream_unit(const PrefixParams& p, const Unit& u
     for (int w = 0; w < kUnitWaves; ++w) M = fmaxf(M, slot(w)[nt * SV * 64 + lane]);
 #pragma unroll
     for (int w = 0; w < kUnitWaves; ++w) {
-      wk[w] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(slot(w)[nt * SV * 64 + lane] - M);
+      wk[w] = __builtin_amdgcn_exp2f(slot(w)[nt * SV * 64 + lane] - M);
       l = fmaf(wk[w], slot(w)[(nt * SV + 1) * 64 + lane], l);
     }
     f32x4 o[2];
@@ -671,7 +671,7 @@ __device__ __forceinline__ void shared_unit(const PrefixParams& p, const Unit& u
     const uint16_t* row = p.q + place_of(p, u, kvh, min(wave * 16 * NT + nt * 16 + col, rows - 1)).out * D + 8 * quad;
 #pragma unroll
     for (int j = 0; j < 4; ++j) red.q[nt][j] = as_bf16x8(*reinterpret_cast<const u32x4*>(row + 32 * j));
-    red.m[nt] = -INFINITY;
+    red.m[nt] = kNoScore;
     red.l[nt] = 0.f;
 #pragma unroll
     for (int nn = 0; nn < 8; ++nn) red.o[nt][nn] = f32x4{0.f, 0.f, 0.f, 0.f};

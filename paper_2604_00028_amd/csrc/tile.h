@@ -482,6 +482,8 @@ __device__ __forceinline__ void merge_tile(const Params& p, float* lds, int64_t 
     merge_columns<W, IPT, CB, FIRST, NANS>(p, lds, srow0, cstride, s, orow0, tid, first_rows);
 }
 
+constexpr float kNoScore = -3.402823466e38f;  // -FLT_MAX
+
 // One wave's running state over the 32-key tiles of a chunk: the packed query
 // heads as the MFMA B operand and, per 16-head column tile, the online
 // softmax's max and row-summed l and NB 16-dim blocks of unnormalised output.
@@ -511,10 +513,13 @@ struct TileReducer {
                        qr, (uint32_t)(nt * 16 + col) * (D * 2) + 64u * j + 16u * quad, 0, 0)));
   }
 
+  // The maximum of no scores is the lowest finite number: scores of -inf (masked
+  // ones, infinite keys) then weigh 0 also before the first finite one, where
+  // -inf - (-inf) would be NaN.
   __device__ __forceinline__ void reset() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      m[nt] = -INFINITY;
+      m[nt] = kNoScore;
       l[nt] = 0.f;
 #pragma unroll
       for (int nn = 0; nn < NB; ++nn) o[nt][nn] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -713,7 +718,7 @@ __device__ __forceinline__ void finish_chunk(const Params& p, const float* slots
     float Lw = 0.f;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      wk[k] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk[k] - M);  // all empty: stays empty
+      wk[k] = __builtin_amdgcn_exp2f(mk[k] - M);  // all empty: sums of 0 stay 0
       Lw = fmaf(wk[k], slot(k)[(nt * SV + 1) * 64 + lane], Lw);
     }
     // lane (col, quad) owns dims 16(nb0 + nn) + 4quad + [0, 4) of head

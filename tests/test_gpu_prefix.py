@@ -262,6 +262,35 @@ def test_values_that_are_not_finite_reach_their_rows_only(n, chunk):
     assert np.max((np.abs(o - ref_o) / tol)[keep]) <= 1.0
 
 
+@pytest.mark.parametrize("n", [1, 2, 6, 9, 20])
+@pytest.mark.parametrize("chunk", [-1, 0, 32])
+def test_scores_of_minus_infinity_weigh_nothing(n, chunk):
+    """Whole tiles of them: the first of the shared keys and of each wave's own, chunks of nothing else, and a sequence
+    that has no other keys."""
+    g = Groups([(n, 320), (3, 0)], [40, 200], 16, 2, 32, seed=29)
+    g.q[:, :, 7] = 0x3F80  # 1
+    seen, first = [], 4 * 32
+    for b, rows in enumerate(g.rows(b) for b in range(n + 3)):
+        L = len(rows)
+        dead = np.zeros(L, bool)
+        if b < n:
+            dead[:first] = True                      # shared
+            dead[320:352] = True                     # the first of its own
+        elif b == n + 2:
+            dead[:] = True
+        else:
+            dead[:min(first, L - 1)] = True          # the first tile of each of four waves
+        g.k.reshape(-1, 2, 128)[rows[dead], :, 7] = 0xFF80
+        seen.append(rows[~dead])
+    k, v = (bf16_bits_to_f64(x).reshape(-1, 2, 128) for x in (g.k, g.v))
+    ref = attend(bf16_bits_to_f64(g.q), [k[r] for r in seen], [v[r] for r in seen], None)
+    say(f"prefix scores of -inf n={n} chunk_keys {chunk}")
+    lse = g.lse()
+    out = g.call(lse, chunk_keys=chunk)
+    torch.cuda.synchronize()
+    check_attention(out, lse, ref, f"scores of -inf n={n}, chunk_keys {chunk}")
+
+
 @pytest.mark.parametrize("scale", [0.01, 1.0])
 def test_scales(scale):
     g = Groups([(7, 300)], [33], 16, 2, 32, seed=17)
