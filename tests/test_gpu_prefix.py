@@ -182,6 +182,20 @@ def test_own_keys_by_single_waves(groups):
     Groups(groups, [1500, 1, 2900, 1700], 8, 8, 32, seed=25).check(f"own keys by waves, {groups}")
 
 
+@pytest.mark.parametrize("H_Q,H_KV,own", [(64, 1, [4000, 1, 2900, 3300]), (128, 2, [3000, 700, 64]), (32, 1, [4000, 33]),
+                                          (40, 8, [1200, 30])])
+def test_single_waves_of_many_heads_and_sequences_that_write_their_output(H_Q, H_KV, own):
+    """Enough own keys for a wave each (12288 tiles of units): 17 to 32 heads a unit, two units that read the same keys,
+    and sequences outside all groups, of which those of one chunk write their output themselves."""
+    prefix, readers = 64, H_KV * (2 if H_Q // H_KV > 32 else 1)
+    per = sum(-(-own[i % len(own)] // 32) for i in range(12)) / 12
+    B = -(-13500 // int(per * readers))
+    g = Groups([(B - 12, prefix), (12, 0)], own, H_Q, H_KV, 32, seed=30)
+    tiles = sum(-(-n // 32) - (prefix // 32 if b < B - 12 else 0) for b, n in enumerate(g.lens))
+    assert tiles * readers >= 24 * 512 and g.L < 8192
+    g.check(f"waves of {H_Q}/{H_KV} heads, {B} sequences", cu=g.cu[:2], pre=g.pre[:1])
+
+
 def test_groups_whose_chunks_fill_the_cus():
     """Chunk lengths that are weighed against each other: few groups, and one more than are weighed."""
     for n in (1, 3, 16, 17):
