@@ -742,7 +742,8 @@ size_t da_prefix_workspace_bytes(int B, int G, int H_Q, int H_KV, int num_cus);
  * da_evict_kv leaves zeros where keys were.  Scores, exponentials and sums in 32
  * bits; results are bit-identical across runs.  One launch, no workspace.
  * Errors as for da_decode_attn_paged (H_Q / H_KV up to 2^16), DA_ERR_SHAPE for
- * weight_stride, DA_ERR_ARG for decay. */
+ * weight_stride and where B H_KV ceil(L_K_max / 2048) reaches 2^24, DA_ERR_ARG
+ * for decay. */
 int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_table, const int32_t* seq_lens,
                        const float* lse, const float* weights, float* weights_out, int64_t weight_stride, int B,
                        int H_Q, int H_KV, int page_size, int max_pages, int num_pages, int L_K_max, int d,
@@ -790,8 +791,9 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
  *                its last DA_ARRIVAL_BYTES zero before the first call, as for
  *                da_decode_attn
  * One launch where L_K_max is a few keys past the budget (or the budget a few),
- * else two.  Errors as for da_decode_attn_paged, and DA_ERR_ARG for budget,
- * sinks and recent. */
+ * else two.  Errors as for da_decode_attn_paged, DA_ERR_ARG for budget, sinks
+ * and recent, and DA_ERR_SHAPE where B H_KV + 1 reaches 2^22 (2^23 for L_K_max up
+ * to 1024, 2^24 up to 512). */
 int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* seq_lens,
                 const int32_t* totals, const float* weights, const int32_t* positions, float* weights_out,
                 int32_t* positions_out, int64_t weight_stride, int32_t* lens_out, int32_t* free_pages,

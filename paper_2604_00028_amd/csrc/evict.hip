@@ -708,12 +708,17 @@ int launched(hipError_t e, const char* what) {
   return e == hipSuccess ? (int)DA_OK : da::fail(DA_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
 }
 
+constexpr int64_t kGridThreads = (int64_t)1 << 32;  // a launch has fewer
+
 int most_moves(int L_K_max, int budget) { return std::max(0, std::min(budget, L_K_max - budget)); }
 
 // Workspace bytes of an eviction, without the counters at its end.
 int64_t move_bytes(int B, int H_KV, int L_K_max, int budget) {
   return 4ll * B * H_KV * (1 + 2ll * most_moves(L_K_max, budget));
 }
+
+// Threads that choose the rows of a (sequence, KV head).
+int select_threads(int L_K_max) { return L_K_max <= 512 ? 256 : L_K_max <= 1024 ? 512 : 1024; }
 
 }  // namespace
 
@@ -740,6 +745,9 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
   if (!aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(lse, 4) || !aligned(weights, 4) ||
       !aligned(weights_out, 4))
     return da::fail(DA_ERR_ALIGN, "block_table, seq_lens, lse and weights must be 4-byte aligned");
+  const int64_t tiles = (L_K_max + kKeysPerTile - 1) / kKeysPerTile, units = (int64_t)B * H_KV;
+  if (units * ((tiles + kMostChunkTiles - 1) / kMostChunkTiles) * (64 * kWeightWaves) >= kGridThreads)
+    return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many workgroups", B, H_KV, L_K_max);
   int cus = 0;
   rc = ensure_gfx950(&cus);
   if (rc || L_K_max == 0) return rc;
@@ -762,16 +770,14 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
   p.num_pages = num_pages;
   p.div_page = make_div((uint32_t)page_size);
   p.div_heads = make_div((uint32_t)H_KV);
-  // sixteen workgroups a CU, of one tile a wave at least: they start as others end, so lengths even out
-  const int64_t tiles = (L_K_max + kKeysPerTile - 1) / kKeysPerTile, units = (int64_t)B * H_KV;
+  // sixteen workgroups a CU, of one tile a wave at least: they start as others end, so lengths even out.  Where they
+  // become more than that and one a unit, chunks have their greatest length
   int64_t each = (tiles * units + 16 * cus - 1) / (16 * cus);
   each = std::min<int64_t>(std::max<int64_t>(4, (each + 3) / 4 * 4), kMostChunkTiles);
   p.chunk_tiles = (int)each;
   const int64_t chunks = (tiles + each - 1) / each;
   p.chunks = (int)chunks;
   p.div_chunks = make_div((uint32_t)chunks);
-  if (units * chunks >= ((int64_t)1 << 31))
-    return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many workgroups", B, H_KV, L_K_max);
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * kLog2e;
   p.decay = decay;
   // keys that the caches cannot hold until the next call take the streaming hint (552 MB of keys and weights 104 ->
@@ -792,8 +798,12 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
 }
 
 size_t da_evict_workspace_bytes(int B, int H_KV, int L_K_max, int budget) {
-  if (B <= 0 || B > DA_MAX_REQUESTS || H_KV <= 0 || L_K_max < 0 || budget < 1 || (int64_t)B * H_KV > (1 << 24)) return 0;
+  // a workgroup a (sequence, KV head), and where those are many one more in move_kernel
+  if (B <= 0 || B > DA_MAX_REQUESTS || H_KV <= 0 || L_K_max < 0 || budget < 1 ||
+      ((int64_t)B * H_KV + 1) * select_threads(L_K_max) >= kGridThreads)
+    return 0;
   const int64_t bytes = move_bytes(B, H_KV, L_K_max, budget);
+  if (bytes >= ((int64_t)1 << 40)) return 0;
   return (size_t)((bytes + 255) / 256 * 256) + DA_ARRIVAL_BYTES;
 }
 
@@ -829,9 +839,8 @@ int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const 
                         (const void*)lens_out, (const void*)free_pages, (const void*)taken, (const void*)taken_out})
     if (!aligned(x, 4)) return da::fail(DA_ERR_ALIGN, "tables, lengths, weights and positions must be 4-byte aligned");
   if (workspace && !aligned(workspace, 16)) return da::fail(DA_ERR_ALIGN, "workspace must be 16-byte aligned");
-  if (move_bytes(B, H_KV, L_K_max, budget) >= ((int64_t)1 << 40))
-    return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many rows", B, H_KV, L_K_max);
   const size_t need = da_evict_workspace_bytes(B, H_KV, L_K_max, budget);
+  if (need == 0) return da::fail(DA_ERR_SHAPE, "B=%d H_KV=%d L_K_max=%d: too many rows", B, H_KV, L_K_max);
   if (!workspace || workspace_bytes < need)
     return da::fail(DA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
   int cus = 0;
@@ -872,7 +881,7 @@ int da_evict_kv(void* k_cache, void* v_cache, const int32_t* block_table, const 
   if (p.most <= kMovedAtOnce)
     p.arrivals = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + da::arrival_offset(workspace_bytes));
   void* args[] = {&p};
-  const int threads = L_K_max <= 512 ? 256 : L_K_max <= 1024 ? 512 : 1024;
+  const int threads = select_threads(L_K_max);
   const void* fn = threads == 256         ? reinterpret_cast<const void*>(&select_kernel<256, true>)
                    : threads == 512       ? reinterpret_cast<const void*>(&select_kernel<512, true>)
                    : L_K_max <= kMostKeys ? reinterpret_cast<const void*>(&select_kernel<1024, true>)

@@ -112,6 +112,26 @@ def test_evict_refusals(lib, kw, code):
     refused(evict_call(lib, **kw), code)
 
 
+BIG = 1 << 40
+
+
+def test_launches_of_2_32_threads_are_refused(lib):
+    """What the checks before let through, on both sides of the line; the side below reaches the device check."""
+    ok = (-7, UNSUP)
+    for B, H, L in ((4096, 1024, 2048), (4096, 2048, 1000), (4096, 4096, 500)):
+        kw = dict(L=L, budget=L - 1, sinks=0, recent=0, ws_bytes=BIG)
+        refused(evict_call(lib, B=B, H_KV=H, **kw), SHAPE)
+        assert da.da_evict_workspace_bytes(B, H, L, L - 1) == 0
+        assert da.da_evict_workspace_bytes(B - 1, H, L, L - 1) > 0
+        if not torch.cuda.is_available():
+            assert evict_call(lib, B=B - 1, H_KV=H, **kw) in ok
+    for B, H, L, mp in ((1 << 20, 16, 2048, 32), (1 << 17, 1, 1 << 18, 4096), ((1 << 23), 1, 2049, 33)):
+        kw = dict(H_Q=H, H_KV=H, L=L, max_pages=mp, stride=L)
+        refused(weights_call(lib, B=B, **kw), SHAPE)
+        if not torch.cuda.is_available():
+            assert weights_call(lib, B=B - 1, **kw) in ok
+
+
 def test_evict_workspace_bytes():
     # a count and two lists of the rows that may move, a sequence and head; counters of other calls behind
     assert da.da_evict_workspace_bytes(1, 1, 100, 60) == 512 + (1 << 20)      # 4 (1 + 80) bytes
