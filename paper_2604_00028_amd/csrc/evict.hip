@@ -236,14 +236,16 @@ __device__ __forceinline__ int2 scan_before(int x, int y, int2* sums, int2* tota
   return make_int2(sx - x + row_sum_before(s.x, wave), sy - y + row_sum_before(s.y, wave));
 }
 
-// Keys of sequence b.  Where they are more than L_K, the rows past them may have no
+// Keys of a sequence.  Where they are more than L_K, the rows past them may have no
 // weights (whose stride need only hold L_K) and the sequence stays as it is: cut to
 // L_K rows it would take later tokens' positions for its first ones, and lose the
 // pages behind.  One that has had no more than L_K tokens holds no more keys.
+__device__ __forceinline__ int counted(const EvictParams& p, int length, int total) {
+  return length > p.L_K && total <= p.L_K ? p.L_K : max(0, length);
+}
+
 __device__ __forceinline__ int length_of(const EvictParams& p, int b) {
-  if (b >= p.B) return 0;
-  const int L = max(0, p.seq_lens[b]);
-  return L > p.L_K && p.totals[b] <= p.L_K ? p.L_K : L;
+  return b < p.B ? counted(p, p.seq_lens[b], p.totals[b]) : 0;
 }
 
 // The lengths after the eviction, and the pages that come free: sequences in order,
@@ -349,7 +351,7 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
   __shared__ int ties;  // not all keys equal to the last that stays do
   const int tid = threadIdx.x, lane = tid & 63;
   const int unit = blockIdx.x, b = div_by(unit, p.div_heads);
-  const int L = length_of(p, b), total = p.totals[b];
+  const int total = p.totals[b], L = counted(p, p.seq_lens[b], total);
   const float* w_in = p.w_in + unit * p.stride;
   const int32_t* p_in = p.p_in + unit * p.stride;
   float* w_out = p.w_out + unit * p.stride;
