@@ -280,7 +280,7 @@ __device__ __forceinline__ float bf16_high(uint32_t two) { return __uint_as_floa
 //
 // AXES: pair i of the rotation turns by the token's position on axis a(i) of up
 // to four, so its coefficients come from row positions[a(i)] of the table: four
-// pairs a load where four have one axis each (8192 tokens with three axes 65 us, as with one;
+// pairs a load where four have one axis each (8192 tokens with three axes 63 us, as with one;
 // a wide load for each axis and a choice by pair, which takes 20 more registers,
 // 79), else one by one.
 template <bool KV4, int STREAM, bool AXES>

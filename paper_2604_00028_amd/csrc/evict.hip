@@ -330,9 +330,9 @@ __device__ __forceinline__ uint64_t least_of_row(uint64_t x) {
 //
 // Bound by latency: one pass over weights and positions, coalesced, whose keys
 // stay in LDS (KEEP; longer sequences read both anew for each step), two lookups
-// a move.  32 sequences of 8 heads one key past 4096, in a graph: 8.8 us with all
+// a move.  32 sequences of 8 heads one key past 4096, in a graph: 9.6 us with all
 // that follows (an empty kernel 2.5, the pass over the keys 2.6, the choice 1.3,
-// the moves 0.8, the last workgroup's part the rest); eight past it 13.8 (about
+// the moves 0.8, the last workgroup's part the rest); eight past it 15.1 (about
 // ten barriers).  With a thread's rows in registers, loaded and stored `each`
 // apart, and one copy of the first histogram the choice by histograms took half as
 // long again.
@@ -633,8 +633,8 @@ __device__ __forceinline__ void select_rows(const EvictParams& p) {
 
 // With `arrivals` the rows that move are few, and there is no second launch: each
 // workgroup moves its own, and the last one to end (nobody waits) does the rest.
-// 256 sequences and heads with 64 rows past the budget 16.4 us in a graph, with a
-// second launch 17.0; with 128 19.5 both; with 256 25.1 and 24.7.
+// 256 sequences and heads with 64 rows past the budget 16.7 us in a graph, with a
+// second launch 17.2; with 128 19.8 and 19.7; with 256 25.7 and 25.2.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS) select_kernel(EvictParams p) {
   int length0 = 0, in_use = 0;
@@ -782,8 +782,8 @@ int da_add_key_weights(const void* q, const void* k_cache, const int32_t* block_
   p.div_chunks = make_div((uint32_t)chunks);
   p.scale_log2 = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D)) * kLog2e;
   p.decay = decay;
-  // keys that the caches cannot hold until the next call take the streaming hint (552 MB of keys and weights 104 ->
-  // 91 us; 270 MB 40 -> 43, so not below)
+  // keys that the caches cannot hold until the next call take the streaming hint (552 MB of keys and weights 108 ->
+  // 94 us in a graph; 276 MB 44 -> 46, so not below)
   const int64_t keys = std::min((int64_t)num_pages * page_size, (int64_t)B * L_K_max);
   const bool stream_hint = (uint64_t)keys * H_KV * D * 2 > DA_RESIDENT_BYTES;
   auto pick = [&](auto hint) {

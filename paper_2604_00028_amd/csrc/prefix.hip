@@ -1,7 +1,8 @@
-// Decode attention of a batch whose sequences share prefixes, three launches:
-// the batch's work cut into units on the device (plan_kernel), the chunk states
-// of the units (unit_kernel), and their merge (merge_kernel).  Entry points at
-// the end.
+// Decode attention of a batch whose sequences share prefixes.  Where the batch
+// may hold enough keys for that to pay, three launches: its work cut into units on
+// the device (plan_kernel), the chunk states of the units (unit_kernel), and their
+// merge (merge_kernel).  Else the one launch of the windowed call, which reads
+// shared keys for each sequence.  Entry points at the end.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -177,6 +178,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(PrefixParams p) {
     // 100 to 1500 own keys, by two and by four: over 16384 shared ones 144 and 157 us, over 8192 134 and 117).  Chunks are
     // as long as two shares of the first waves (64 of 100 to 2000 keys over 8192: one share 87.5, two 84, four 110), or half
     // of one where there are two (the 144 us: 136).
+    // Few long sequences are few chunks and so few waves: one of 800 000 keys, 8/1 heads, takes 454 us (the windowed call
+    // 128), three of 20480, 64/16, 97 (90).
     waves = work_b < 24 * p.slots ? 0 : work_b > work_g ? 4 : 2;
     length_g = p.chunk_tiles > 0 ? p.chunk_tiles : min(max(work_g / (p.slots / 2), 4), 128);
     length_b = p.chunk_tiles > 0 ? p.chunk_tiles
@@ -409,9 +412,11 @@ __device__ __forceinline__ void load_rows(TileReducer<NT, 8>& red, const PrefixP
 }
 
 // One wave over the tiles t, t + STEP, ... of a unit of 16 NT rows or fewer: K
-// straight into the operand layout and V by way of LDS (`vstage`, the wave's
-// own), the next tile's loads in flight.  ready(): called between the first loads
-// and the first use of the LDS.
+// and V by way of LDS (`vstage`, the wave's own), the next tile's loads in flight.
+// ready(): called between the first loads and the first use of the LDS.
+// Single waves (STEP 1) stream: 64 sequences of 500 to 4000 own keys, 64/8 heads,
+// 140 -> 131 us.  Where several units read the same keys it costs instead: 128/1
+// heads and 64 sequences of 1000 to 8000 97 -> 105, 37/1 258 -> 435.
 template <int NT, typename Step, typename Ready>
 __device__ __forceinline__ void stream_tiles(const PrefixParams& p, const Unit& u, TileReducer<NT, 8>& red,
                                              unsigned char* vstage, int t, Step, int lane, Ready ready) {
@@ -1064,6 +1069,7 @@ int launched(hipError_t e, const char* what) {
 // those bytes, this call's sharing launches and the one launch (us; 64/8 heads): 5 MB 15 and 6.6, 75 MB 23 and 8.1, 276
 // MB 30 and 18, 330 MB 30 and 25, 598 MB 34 and 43, 1140 MB 41 and 79.  Groups of more than 16 heads need the matrix
 // cores twice as long for as many bytes: 32/1 heads 270 MB 42 and 27, 1080 MB 76 and 76.
+// The bound decides, not the lengths: two sequences of 530 keys under one of 131072 17.6 us, by the one launch 8.9.
 constexpr int64_t kUnsharedBytes = 384ll << 20;
 
 // Sizes of a call's workspace: room for what the plan may choose, and at the
